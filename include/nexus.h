@@ -288,6 +288,117 @@ size_t nexus_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const nexu
                                    int32_t max_seq_len);
 
 /*
+ * ---- 8-bit cache: a paged cache of half the bytes, with the calls that write it, read it back and attend to it.
+ *
+ * Every row (one token of one KV head of one layer, of K or of V) is head_dim E4M3 codes under a
+ * power-of-two scale of its own, kept as one E8M0 byte (so a token appended to a page never changes the
+ * tokens beside it):
+ *   amax    the row's largest magnitude;
+ *   e       the least integer with amax <= 448 * 2^e, held within [-100, 119];
+ *   code    x / 2^e rounded to the nearest E4M3 value, ties to even, at most 448 in magnitude;
+ *   value   code * 2^e: exact in bf16 and in f32;
+ *   byte    e + 127.
+ * An element is at most 2^-4 of its magnitude from its value where it is at least 2^-14 of amax, and at most
+ * 2^-18 of amax below that.  Rows below 2^-109 become zeros.  A row with an element that is not finite
+ * becomes NaN as a whole (byte 255, codes 0x7F): a query that sees its key or value gets NaN, the
+ * other queries nothing of it.
+ *   k, v              codes [n_layers][n_phys_pages][n_kv_heads][16][head_dim];
+ *   k_scale, v_scale  bytes [n_layers][n_phys_pages][n_kv_heads][16].
+ * All four pointers are 16-byte aligned (NEXUS_EINVAL); V is row-major; head_dim is 64, 128 or 256
+ * (NEXUS_ESHAPE).  A layer may hold any number of bytes (fewer than 2^31 tokens).  Caches of other origin have
+ * to keep bytes within [27, 246], or 255 with codes 0x7F.  Slots that no call wrote may hold
+ * anything: a call reads only tokens that its lengths name.  The checks of the other calls hold here too
+ * (layers, page table entries, page lifetimes); each call is one kernel launch, the attention calls one
+ * more where they split the keys.
+ */
+typedef struct nexus_kv8_cache {
+  void *k;
+  void *v;
+  void *k_scale;
+  void *v_scale;
+  int32_t n_layers, n_phys_pages, page_size, n_kv_heads, head_dim;
+  int32_t rope_style;   /* nexus_rope_style */
+  double rope_base;
+} nexus_kv8_cache;
+
+/*
+ * Append freshly computed tokens (nexus_rope_append for an 8-bit cache): k and v are
+ * [n_layers][n_tokens][n_kv_heads][head_dim] device arrays of `dtype` (nexus_dtype) holding UN-rotated keys
+ * and values, 16-byte aligned.  Key token j is rotated to absolute position pos0 + j as there, and its
+ * rotated fp32 values are quantised directly; row j goes to logical slot offset + j.  Nothing else is written.
+ * Checks: non-NULL aligned arrays, n_tokens > 0 (NEXUS_EINVAL); dtype (NEXUS_EDTYPE); offset >= 0,
+ * pos0 >= 0, offset + n_tokens within the mapped pages (NEXUS_ERANGE).
+ */
+nexus_status nexus_kv8_append(const nexus_kv8_cache *cache, const nexus_page_table *pt, const void *k,
+                              const void *v, int32_t dtype, int32_t n_tokens, int64_t offset, int64_t pos0,
+                              void *stream);
+
+/*
+ * The append of a decode step: one token for each of n_seqs sequences, k and v
+ * [n_layers][n_seqs][n_kv_heads][head_dim].  Sequence b holds seq_len[b] tokens with the new one
+ * counted, so its key is rotated to position seq_len[b] - 1 and both rows go to that slot through map row b
+ * (maps, map_stride, seq_len, max_seq_len as in nexus_kv8_decode_attn, which may follow at once).  A sequence
+ * whose length is not in [1, max_seq_len] writes nothing.  Lengths live on the device, so one captured
+ * launch serves every step.  Two sequences must not share the page that either writes to.
+ */
+nexus_status nexus_kv8_append_step(const nexus_kv8_cache *cache, const int32_t *maps, int32_t map_stride,
+                                   const int32_t *seq_len, int32_t n_seqs, int32_t max_seq_len,
+                                   const void *k, const void *v, int32_t dtype, void *stream);
+
+/*
+ * Splice a compiled block (bf16 or f32) into the cache with its keys re-anchored from block->base_pos to
+ * dst_pos (nexus_splice_rephase_pages for an 8-bit cache; the block is not modified).  The rotated fp32
+ * values are quantised directly.  Checks: those of nexus_splice_pages without the element type (the block has its
+ * own), the block's pointers 16-byte aligned (NEXUS_EINVAL), dst_pos >= 0 (NEXUS_ERANGE).
+ */
+nexus_status nexus_kv8_splice(const nexus_kv8_cache *cache, const nexus_page_table *pt,
+                              const nexus_block *block, int64_t offset, int64_t dst_pos, void *stream);
+
+/*
+ * Read logical tokens [offset, offset + n_tokens) back as values: k and v receive
+ * [n_layers][n_tokens][n_kv_heads][head_dim] of `dtype`, the layout of a block, keys as they are rotated in
+ * the cache.  Splicing what was read gives the same codes and scales when nothing rotates it.  Checks as
+ * nexus_kv8_append.
+ */
+nexus_status nexus_kv8_read(const nexus_kv8_cache *cache, const nexus_page_table *pt, int64_t offset,
+                            int32_t n_tokens, int32_t dtype, void *k, void *v, void *stream);
+
+/*
+ * nexus_suffix_attn and nexus_suffix_attn_varlen over an 8-bit cache: q and out are bf16, 16-byte
+ * aligned; layouts, positions, masks, softcap, scale, plan and workspace rules (16-byte aligned) as there.
+ * Scores are exact products of q with the keys' values (to 2^-22 of the largest |q| of a row),
+ * accumulated in fp32; probabilities are rounded to bf16 for their product with the values.
+ * The rows of the sequences of one launch must not overlap (NEXUS_EINVAL).
+ */
+nexus_status nexus_kv8_suffix_attn(const void *q, int32_t n_s, int32_t n_q_heads,
+                                   const nexus_kv8_cache *cache, const nexus_page_table *pt, int32_t layer,
+                                   int64_t n_past, float softcap, float scale, void *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+size_t nexus_kv8_suffix_attn_workspace(int32_t n_s, int32_t n_q_heads, const nexus_kv8_cache *cache,
+                                       int64_t n_past);
+nexus_status nexus_kv8_suffix_attn_varlen(const void *q, int32_t n_seqs, const int32_t *q_start,
+                                          const int32_t *seq_len, const int64_t *seq_n_past,
+                                          int32_t n_q_heads, const nexus_kv8_cache *cache,
+                                          const nexus_page_table *pt, int32_t layer, float softcap,
+                                          float scale, void *out, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+size_t nexus_kv8_suffix_attn_varlen_workspace(int32_t n_seqs, const int32_t *q_start,
+                                              const int32_t *seq_len, const int64_t *seq_n_past,
+                                              int32_t n_q_heads, const nexus_kv8_cache *cache);
+
+/*
+ * nexus_decode_attn over an 8-bit cache: q and out are bf16, 16-byte aligned; maps, lengths (0 gives a
+ * zero row), softcap and scale as there.  Pages that sequences share are read by each of them.
+ */
+nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_heads,
+                                   const nexus_kv8_cache *cache, const int32_t *maps, int32_t map_stride,
+                                   const int32_t *seq_len, int32_t max_seq_len, int32_t layer,
+                                   float softcap, float scale, void *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+size_t nexus_kv8_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const nexus_kv8_cache *cache,
+                                       int32_t max_seq_len);
+
+/*
  * Warm-prefix reuse on the paged cache (the exact-token prefix arena of Sec. VI-D, whose copy
  * within a pre-reserved arena becomes page-table work here).  Both calls take two DEVICE int32
  * page maps of one cache (n_map_pages entries each, logical page -> physical page) and move

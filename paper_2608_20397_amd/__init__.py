@@ -7,4 +7,6 @@ attention, as hand-written HIP kernels behind the C ABI of ``include/nexus.h``
 from . import nexus  # noqa: F401
 from .nexus import (Block, PagedKVCache, NexusError, splice_pages, rephase_k,  # noqa: F401
                     rephase_k_paged, suffix_attn, suffix_attn_varlen, redecode_len,
-                    check_page_table, lib)
+                    check_page_table, lib, KV8Cache, kv8_append, kv8_append_step,  # noqa: F401
+                    kv8_splice, kv8_read, kv8_suffix_attn, kv8_suffix_attn_varlen,  # noqa: F401
+                    kv8_decode_attn)  # noqa: F401

@@ -421,6 +421,7 @@ struct KernelShape {
 };
 
 KernelShape kernel_shape(const AttnLaunch &p) {
+  if (p.kv8 && p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.04};
   if (p.head_dim <= 128) return {kQB, 64, 2, kWaves, 0.03 * p.head_dim / 128.0};   // LDS DMA
   if (p.v_transposed) return {kQB, 32, 1, kWavesWide, 0.04};                       // LDS DMA
   return {kQB, 32, 1, kWaves, 0.06};
@@ -718,6 +719,20 @@ size_t attn_workspace_bytes(const AttnLaunch &p) {
   return plan.ws_bytes;
 }
 
+bool plan_attention(const AttnLaunch &p, AttnPlan &plan) { return make_plan(p, plan); }
+
+hipError_t launch_attn_combine(const AttnArgs &args, const AttnPlan &plan, int head_dim, hipStream_t stream) {
+  if (!plan.any_split) return hipSuccess;
+  const int64_t total = (int64_t)plan.total_rows * args.n_q_heads * (head_dim / 16);
+  const uint32_t blocks = (uint32_t)((total + 255) / 256);
+  switch (head_dim) {
+    case 64: hipLaunchKernelGGL(attn_combine_kernel<64>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
+    case 128: hipLaunchKernelGGL(attn_combine_kernel<128>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
+    case 256: hipLaunchKernelGGL(attn_combine_kernel<256>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_attention(const AttnLaunch &p, hipStream_t stream) {
   if (!p.is_bf16) return launch_attention_f32(p, stream);
   AttnPlan plan;
@@ -759,17 +774,7 @@ hipError_t launch_attention(const AttnLaunch &p, hipStream_t stream) {
   else
     e = run(attn_bf16_d256_kernel<false>);
   if (e != hipSuccess) return e;
-  if (plan.any_split) {
-    const int64_t total = (int64_t)plan.total_rows * p.n_q_heads * (p.head_dim / 16);
-    const uint32_t blocks = (uint32_t)((total + 255) / 256);
-    switch (p.head_dim) {
-      case 64: hipLaunchKernelGGL(attn_combine_kernel<64>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
-      case 128: hipLaunchKernelGGL(attn_combine_kernel<128>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
-      case 256: hipLaunchKernelGGL(attn_combine_kernel<256>, dim3(blocks), dim3(256), 0, stream, args, plan); break;
-    }
-    e = hipGetLastError();
-  }
-  return e;
+  return launch_attn_combine(args, plan, p.head_dim, stream);
 }
 
 }  // namespace nexus

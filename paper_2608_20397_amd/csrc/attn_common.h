@@ -2,6 +2,7 @@
 #pragma once
 
 #include "device_common.h"
+#include "launch.h"
 
 namespace nexus {
 
@@ -145,6 +146,7 @@ struct AttnArgs {
   float cap_in;         // scale / softcap
   float cap_out;        // softcap * log2(e)
   float cap_k;          // 2 * scale * log2(e) / softcap
+  const uint8_t *ks = nullptr, *vs = nullptr;   // 8-bit cache: layer bases of the scale bytes [NPP][Hkv][16]
 };
 
 __device__ __forceinline__ float tanh_fast(float x) {
@@ -220,5 +222,8 @@ __device__ __forceinline__ int vt_swz(int d) {
   return (d ^ (d >> 3)) & VSW;
 }
 
+// The plan of a launch, and the merge of its split partials (nothing enqueued when there are none).
+bool plan_attention(const AttnLaunch &p, AttnPlan &plan);
+hipError_t launch_attn_combine(const AttnArgs &args, const AttnPlan &plan, int head_dim, hipStream_t stream);
 
 }  // namespace nexus

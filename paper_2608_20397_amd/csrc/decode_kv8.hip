@@ -1,0 +1,380 @@
+// Decode step over an 8-bit paged cache (kv8_common.h has its format): one query for each of many
+// sequences, each with its own page map and a length on the device; optional tanh soft cap.
+//
+// The work decomposition is that of the bf16 decode (decode_attn.hip): a workgroup takes one (sequence, KV
+// head, group of up to 16 query heads, run of pages); its 4 waves take the run's page pairs in turn, a
+// pair in registers while the next one loads, and meet through LDS; a second kernel merges the runs.
+//   * S^T = K.Q^T on v_mfma_scale_f32_16x16x128_f8f6f4, the keys' codes straight from global memory into
+//     the A operand (lane l: row l % 16, 32 bytes from 32 (l / 16)); the query as two E4M3 terms
+//     (split_query).  head_dim 64: lane groups 2 and 3 hold the row's codes again, against zeros.
+//   * a lane holds the scores of keys 4 (l / 16) .. +3, whose 4 scale bytes are one word: the key's scale is
+//     multiplied to the score, the value's to the probability that it is weighed with (a power of two:
+//     exact), and V enters the PV product as its codes in bf16.
+// Keys past a sequence's end re-read its last key and weigh nothing.  HBM-bound: head_dim + 1 bytes of K and of
+// V per key and KV head, half the bf16 cache's.
+#include "attn_common.h"
+#include "attn_dma.h"
+#include "decode_common.h"
+#include "kv8_common.h"
+#include "launch_kv8.h"
+
+#include <algorithm>
+
+namespace nexus {
+
+namespace {
+
+template <int D, bool CAP>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const DecodeArgs a) {
+  constexpr int NP = 2;               // pages per step of a wave
+  constexpr int KS = D == 256 ? 2 : 1;   // 128-feature steps of S^T
+  constexpr int DT = D / 16;          // O^T tiles
+  constexpr int ROWB = 2 * D;         // bytes of a staged V row (bf16)
+  constexpr int VL = D / 64;          // 16-byte loads of V codes per lane and page
+  constexpr int MO_LD = D + 4;        // padded row of the merge buffer (floats)
+  constexpr int STAGE_BYTES = kDecWaves * NP * 16 * ROWB;
+  constexpr int MERGE_BYTES = 2 * 16 * MO_LD * 4 + 2 * 2 * 16 * 4;
+  __shared__ __align__(1024) char smem[STAGE_BYTES > MERGE_BYTES ? STAGE_BYTES : MERGE_BYTES];
+  __shared__ int32_t pgs[kMaxSplitPages];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qn = lane & 15, grp = lane >> 4;
+  const int split = blockIdx.x, hg = blockIdx.y, b = blockIdx.z;
+  const int len = seq_len_of(a, b);
+  const int qg = hg % a.n_qgroups;
+  const int h = hg / a.n_qgroups;
+  const int g_lo = qg * 16;
+  const int g_cnt = min(16, a.group - g_lo);     // query heads of this workgroup
+  const int hq0 = h * a.group + g_lo;            // first of them
+  uint16_t *out = reinterpret_cast<uint16_t *>(a.out);
+
+  if (len == 0) {
+    if (split == 0)
+      for (int i = tid; i < g_cnt * D; i += 256)
+        out[((size_t)b * a.n_q_heads + hq0) * D + i] = 0;
+    return;
+  }
+  const int n_pages = (len + 15) >> 4;
+  const int p_begin = split * a.split_pages;
+  if (p_begin >= n_pages) return;
+  const int p_end = min(p_begin + a.split_pages, n_pages);
+  const int n_splits = (n_pages + a.split_pages - 1) / a.split_pages;
+  const int n_sp = p_end - p_begin;
+  const int32_t *map = a.maps + (size_t)b * a.map_stride;
+  for (int i = tid; i < n_sp; i += 256) pgs[i] = map[p_begin + i];
+
+  // ---- the queries: column qn = query head hq0 + qn (columns past the group are zero)
+  const bool q_ok = qn < g_cnt;
+  i32x8 qhi[KS], qlo[KS];
+  int qs_hi, qs_lo;
+  {
+    const uint16_t *qrow =
+        reinterpret_cast<const uint16_t *>(a.q) + ((size_t)b * a.n_q_heads + hq0 + qn) * D;
+    u32x4 raw[KS][4];
+    uint32_t am = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int f = D == 64 ? 32 * (grp & 1) : 128 * s + 32 * grp;
+        raw[s][c] = q_ok ? *reinterpret_cast<const u32x4 *>(qrow + f + 8 * c) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          am = max(am, max((raw[s][c][e] << 16) & 0x7FFF0000u, raw[s][c][e] & 0x7FFF0000u));
+      }
+    am = max(am, (uint32_t)__shfl_xor((int)am, 16));
+    am = max(am, (uint32_t)__shfl_xor((int)am, 32));
+    const bool bad = am >= 0x7F800000u;
+    const int e = row_exp(am);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float x[8];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          x[2 * w] = __uint_as_float(raw[s][c][w] << 16);
+          x[2 * w + 1] = __uint_as_float(raw[s][c][w] & 0xFFFF0000u);
+        }
+        uint32_t hi[2], lo[2];
+        split_query<8>(x, e, bad, hi, lo);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          qhi[s][2 * c + w] = D == 64 && grp >= 2 ? 0u : hi[w];
+          qlo[s][2 * c + w] = D == 64 && grp >= 2 ? 0u : lo[w];
+        }
+      }
+    qs_hi = e + 127;
+    qs_lo = e + 127 - 4;
+  }
+  __syncthreads();   // pgs[]
+
+  // keys of entry i of the run: all but the sequence's last page are whole
+  const int last_keys = p_end == n_pages ? len - 16 * (n_pages - 1) : 16;
+  auto keys_of = [&](int i) { return i == n_sp - 1 ? last_keys : 16; };
+  const uint64_t page_bytes = (uint64_t)a.n_kv_heads * 16 * D;
+  const uint64_t page_scales = (uint64_t)a.n_kv_heads * 16;
+  const char *kbase = reinterpret_cast<const char *>(a.kc) + (size_t)h * 16 * D;
+  const char *vbase = reinterpret_cast<const char *>(a.vc) + (size_t)h * 16 * D;
+  const uint8_t *ksb = a.ks + h * 16 + 4 * grp, *vsb = a.vs + h * 16 + 4 * grp;
+  char *vstage = smem + wave * NP * 16 * ROWB;
+
+  struct Page {
+    u32x4 k[KS][2];
+    u32x4 v[VL];
+    uint32_t ks, vs;         // scale bytes of keys 4 grp .. +3
+  };
+  auto load_page = [&](int nvalid, uint32_t phys, Page &pg) {
+    const char *kp = kbase + phys * page_bytes + min(qn, nvalid - 1) * D;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        pg.k[s][c] = *reinterpret_cast<const u32x4 *>(
+            kp + (D == 64 ? 32 * (grp & 1) : 128 * s + 32 * grp) + 16 * c);
+    const char *vp = vbase + phys * page_bytes;
+#pragma unroll
+    for (int j = 0; j < VL; ++j) {
+      const int byte = 16 * lane + 1024 * j;
+      pg.v[j] = *reinterpret_cast<const u32x4 *>(vp + min(byte / D, nvalid - 1) * D + byte % D);
+    }
+    pg.ks = *reinterpret_cast<const uint32_t *>(ksb + phys * page_scales);
+    pg.vs = *reinterpret_cast<const uint32_t *>(vsb + phys * page_scales);
+  };
+
+  f32x4 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_ref = -INFINITY;   // reference of query column qn (equal across the 4 lane groups)
+  float lsum = 0.f;          // sum of this lane's rounded probabilities
+
+  struct Pair {
+    Page pg[NP];
+  };
+  auto compute_pair = [&](const int (&keys)[NP], bool two, const Pair &pr) {
+    float x[4 * NP], vf[4 * NP];
+#pragma unroll
+    for (int pp = 0; pp < NP; ++pp) {
+      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const u32x4 u = pr.pg[pp].k[st][0], w = pr.pg[pp].k[st][1];
+        const i32x8 ka = {(int)u[0], (int)u[1], (int)u[2], (int)u[3],
+                          (int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qhi[st], s, 0, 0, 0, 127, 0, qs_hi);
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qlo[st], s, 0, 0, 0, 127, 0, qs_lo);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool seen = 4 * grp + i < keys[pp] && (pp == 0 || two);
+        const float kf = scale_value(pr.pg[pp].ks >> (8 * i) & 255);
+        const float v = CAP ? a.cap_out * tanh_fast(s[i] * kf * a.cap_in) : s[i] * kf * a.scale_log2;
+        x[4 * pp + i] = seen ? v : -INFINITY;
+        vf[4 * pp + i] = seen ? scale_value(pr.pg[pp].vs >> (8 * i) & 255) : 0.f;
+      }
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < 4 * NP; ++e) mx = fmaxf(mx, x[e]);
+    mx = max_x32(max_x16(mx));
+    const bool need = mx > m_ref + kDecSlack;
+    if (__builtin_amdgcn_ballot_w64(need)) {
+      const float nm = need ? mx : m_ref;
+      const float alpha = need ? fast_exp2(m_ref - nm) : 1.f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] *= alpha;
+      lsum *= alpha;
+      m_ref = nm;
+    }
+    uint32_t w[2 * NP];
+#pragma unroll
+    for (int e = 0; e < 2 * NP; ++e) {
+      const uint32_t p = pack_bf16x2(fast_exp2(x[2 * e] - m_ref), fast_exp2(x[2 * e + 1] - m_ref));
+      const float p0 = __uint_as_float(p << 16), p1 = __uint_as_float(p & 0xFFFF0000u);
+      lsum += p0 + p1;
+      w[e] = pack_bf16x2(p0 * vf[2 * e], p1 * vf[2 * e + 1]);
+    }
+    // V codes as bf16 through the wave's own LDS slot (a page alone: zeros beside it, for 0 x NaN is NaN)
+#pragma unroll
+    for (int pp = 0; pp < NP; ++pp)
+#pragma unroll
+      for (int j = 0; j < VL; ++j) {
+        const int byte = 16 * lane + 1024 * j;
+        const int row = byte / D, c = 2 * ((byte % D) >> 4);
+        u32x2 f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = codes_to_bf16(pp == 0 || two ? pr.pg[pp].v[j][i] : 0u, 1.f);
+        char *dst = vstage + pp * 16 * ROWB + row * ROWB;
+        *reinterpret_cast<u32x4 *>(dst + 16 * (c ^ vswz<D>(row))) =
+            u32x4{f[0][0], f[0][1], f[1][0], f[1][1]};
+        *reinterpret_cast<u32x4 *>(dst + 16 * ((c + 1) ^ vswz<D>(row))) =
+            u32x4{f[2][0], f[2][1], f[3][0], f[3][1]};
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int r = 4 * grp + (qn >> 2);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const int c = 2 * t + ((qn & 3) >> 1);
+      const char *src = vstage + r * ROWB + 16 * (c ^ vswz<D>(r)) + 8 * (qn & 1);
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          tr_read_pair(src, src + 16 * ROWB), __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]}),
+          o[t], 0, 0, 0);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+
+  // ---- this wave's page pairs through two register buffers, as decode_attn.hip
+  {
+    const int n_pairs = (n_sp + NP - 1) / NP;
+    const int n_mine = wave < n_pairs ? (n_pairs - wave + kDecWaves - 1) / kDecWaves : 0;
+    if (n_mine > 0) {
+      auto entry = [&](int k) { return NP * (wave + kDecWaves * k); };
+      auto issue = [&](int k, Pair &pr) {
+#pragma unroll
+        for (int pp = 0; pp < NP; ++pp) {
+          const int e = min(entry(min(k, n_mine - 1)) + pp, n_sp - 1);
+          load_page(keys_of(e), (uint32_t)__builtin_amdgcn_readfirstlane(pgs[e]), pr.pg[pp]);
+        }
+      };
+      auto compute = [&](int k, const Pair &pr) {
+        const int e = entry(k);
+        int keys[NP];
+#pragma unroll
+        for (int pp = 0; pp < NP; ++pp) keys[pp] = keys_of(min(e + pp, n_sp - 1));
+        compute_pair(keys, e + 1 < n_sp, pr);
+      };
+      Pair b0, b1;
+      issue(0, b0);
+      int k = 0;
+      for (; k + 1 < n_mine; k += 2) {
+        issue(k + 1, b1);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(k, b0);
+        __builtin_amdgcn_sched_barrier(0);
+        issue(k + 2, b0);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(k + 1, b1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (k < n_mine) compute(k, b0);
+    }
+  }
+
+  // ---- merge the 4 waves' (m, l, O^T): waves 2 and 3 into 0 and 1, then 1 into 0, which writes
+  lsum = sum_x32(sum_x16(lsum));
+  float *mo = reinterpret_cast<float *>(smem);   // [2 slots][16 columns][MO_LD]
+  float *mml = mo + 2 * 16 * MO_LD;              // [2 slots][16 columns][m, l]
+  auto store_state = [&](int slot) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      *reinterpret_cast<f32x4 *>(mo + (slot * 16 + qn) * MO_LD + 16 * t + 4 * grp) = o[t];
+    if (grp == 0) {
+      mml[2 * (slot * 16 + qn)] = m_ref;
+      mml[2 * (slot * 16 + qn) + 1] = lsum;
+    }
+  };
+  auto merge_state = [&](int slot) {
+    const float mb = mml[2 * (slot * 16 + qn)];
+    const float lb = mml[2 * (slot * 16 + qn) + 1];
+    const float M = fmaxf(m_ref, mb);
+    // a wave that saw no page has m = -inf and contributes nothing
+    const float wa = m_ref > -INFINITY ? fast_exp2(m_ref - M) : 0.f;
+    const float wb = mb > -INFINITY ? fast_exp2(mb - M) : 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const f32x4 ob =
+          *reinterpret_cast<const f32x4 *>(mo + (slot * 16 + qn) * MO_LD + 16 * t + 4 * grp);
+      o[t] = o[t] * wa + ob * wb;
+    }
+    lsum = lsum * wa + lb * wb;
+    m_ref = M;
+  };
+  __syncthreads();   // the V staging slots are reused
+  if (wave >= 2) store_state(wave - 2);
+  __syncthreads();
+  if (wave < 2) merge_state(wave);
+  __syncthreads();
+  if (wave == 1) store_state(0);
+  __syncthreads();
+  if (wave != 0) return;
+  merge_state(0);
+  if (!q_ok) return;
+  const int row = b * a.n_q_heads + hq0 + qn;
+  if (n_splits == 1) {
+    const float inv = 1.0f / lsum;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      *reinterpret_cast<u32x2 *>(out + (size_t)row * D + 16 * t + 4 * grp) =
+          u32x2{pack_bf16x2(o[t][0] * inv, o[t][1] * inv),
+                pack_bf16x2(o[t][2] * inv, o[t][3] * inv)};
+  } else {
+    store_part<D>(a, row, split, o, m_ref, lsum, grp);
+  }
+}
+
+// Pages per split and splits of the longest sequence.
+void kv8_splits(const DecodeLaunch &p, int &split_pages, int &n_splits) {
+  const int group = p.n_q_heads / p.n_kv_heads;
+  split_pages = decode_split_pages(p.n_seqs, p.n_kv_heads, (group + 15) / 16, p.max_len);
+  const int64_t max_pages = ((int64_t)p.max_len + 15) / 16;
+  n_splits = (int)std::max<int64_t>(1, (max_pages + split_pages - 1) / split_pages);
+}
+
+}  // namespace
+
+size_t decode_kv8_workspace_bytes(const DecodeLaunch &p) {
+  int sp, ns;
+  kv8_splits(p, sp, ns);
+  return ns <= 1 ? 0 : (size_t)p.n_seqs * p.n_q_heads * ns * (p.head_dim + 2) * sizeof(float);
+}
+
+hipError_t launch_decode_kv8(const DecodeLaunch &p, hipStream_t stream) {
+  const int group = p.n_q_heads / p.n_kv_heads;
+  int ns;
+  DecodeArgs a{};
+  kv8_splits(p, a.split_pages, ns);
+  const size_t layer_rows = (size_t)p.layer * p.n_phys_pages * p.n_kv_heads * 16;
+  a.q = p.q;
+  a.out = p.out;
+  a.kc = static_cast<const char *>(p.cache_k) + layer_rows * p.head_dim;
+  a.vc = static_cast<const char *>(p.cache_v) + layer_rows * p.head_dim;
+  a.ks = p.k_scale + layer_rows;
+  a.vs = p.v_scale + layer_rows;
+  a.maps = p.maps;
+  a.lens = p.lens;
+  float *ws = static_cast<float *>(p.workspace);
+  a.part = ns > 1 ? ws : nullptr;
+  a.part_ml = ns > 1 ? ws + (size_t)p.n_seqs * p.n_q_heads * ns * p.head_dim : nullptr;
+  a.map_stride = p.map_stride;
+  a.max_len = p.max_len;
+  a.n_q_heads = p.n_q_heads;
+  a.n_kv_heads = p.n_kv_heads;
+  a.group = group;
+  a.n_qgroups = (group + 15) / 16;
+  a.max_splits = a.own_splits = ns;
+  a.n_seqs = p.n_seqs;
+  const float log2e = 1.4426950408889634f;
+  a.scale_log2 = p.scale * log2e;
+  a.cap_in = p.softcap > 0.f ? p.scale / p.softcap : 0.f;
+  a.cap_out = p.softcap * log2e;
+  const bool cap = p.softcap > 0.f;
+  const dim3 grid(ns, p.n_kv_heads * a.n_qgroups, p.n_seqs);
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
+    return hipGetLastError();
+  };
+  hipError_t e;
+  switch (p.head_dim) {
+    case 64: e = cap ? run(decode_kv8_kernel<64, true>) : run(decode_kv8_kernel<64, false>); break;
+    case 128: e = cap ? run(decode_kv8_kernel<128, true>) : run(decode_kv8_kernel<128, false>); break;
+    default: e = cap ? run(decode_kv8_kernel<256, true>) : run(decode_kv8_kernel<256, false>); break;
+  }
+  if (e != hipSuccess || ns <= 1) return e;
+  return launch_decode_combine(a, p.head_dim, true, stream);
+}
+
+}  // namespace nexus

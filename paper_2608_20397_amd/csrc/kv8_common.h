@@ -1,0 +1,102 @@
+// The 8-bit cache's row format on the device (internal, not part of the C ABI).
+//
+// A row (one token, KV head and layer of K or V) is head_dim E4M3 codes under one scale 2^e, kept as
+// the byte e + 127 (E8M0).  e is the least integer for which no element passes the largest code:
+// amax <= 448 * 2^e, held within [kMinExp, kMaxExp].  The scale is a power of two because a code times it
+// is then exact in bf16: what the attention multiplies is what a read returns, and the scale costs no
+// instruction (the conversion to bf16 and the scaled MFMA both take it).  Against a scale amax / 448
+// this loses nothing in the codes' normal range, 2^-14 of the row's largest element and up, where a
+// code's relative error is that of its three mantissa bits whatever the scale.
+#pragma once
+
+#include "device_common.h"
+
+namespace nexus {
+
+constexpr int kMinExp = -100;    // keeps every value and scale a normal fp32 number
+constexpr int kMaxExp = 119;     // 448 * 2^119 < 2^128: larger elements take the largest code
+constexpr uint32_t kBadScale = 255;           // the row had an element that is not finite
+constexpr uint32_t kBadCodes = 0x7F7F7F7Fu;   // its codes: NaN
+
+typedef __attribute__((ext_vector_type(8))) int32_t i32x8;
+
+// Exponent of a row from the bits of its largest magnitude (a finite one): adding 0x1FFFFF carries into
+// the exponent field exactly when the mantissa passes 1.75.
+__device__ __forceinline__ int row_exp(uint32_t amax_bits) {
+  const int e = (int)((amax_bits + 0x1FFFFFu) >> 23) - 135;
+  return min(max(e, kMinExp), kMaxExp);
+}
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// The value of a scale byte.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return byte == kBadScale ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
+}
+
+// Largest magnitude as bits: what is not finite compares above everything finite.
+template <int N>
+__device__ __forceinline__ uint32_t amax_bits(const float *x) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+  return m;
+}
+
+// Four values to four codes (nearest-even; |y| <= 448).
+__device__ __forceinline__ uint32_t pack_e4m3(float y0, float y1, float y2, float y3) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y2, y3, lo, true);
+}
+
+// Codes of N values (a multiple of 4) of a row whose largest magnitude has the bits `am`.
+template <int N>
+__device__ __forceinline__ void quantise(const float *x, uint32_t am, uint32_t *codes) {
+  const float inv = exp2i(-row_exp(am));
+  float y[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = x[e] * inv;
+  if (am > 0x7F600000u) {   // past 448 * 2^kMaxExp, or not finite
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = fminf(fmaxf(y[e], -448.f), 448.f);
+  }
+#pragma unroll
+  for (int e = 0; e < N / 4; ++e) {
+    codes[e] = pack_e4m3(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+    if (am >= 0x7F800000u) codes[e] = kBadCodes;
+  }
+}
+__device__ __forceinline__ uint32_t scale_byte(uint32_t am) {
+  return am >= 0x7F800000u ? kBadScale : (uint32_t)(row_exp(am) + 127);
+}
+
+// Four codes (a word) times a power-of-two scale, as two words of bf16: exact.
+__device__ __forceinline__ u32x2 codes_to_bf16(uint32_t w, float scale) {
+  return u32x2{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+}
+
+// A row's part of a bf16 query as two E4M3 terms, q = (hi + lo / 16) 2^e exactly where |q| is at least
+// 2^-14 of the row's largest magnitude and to 2^-22 of that below: a bf16 has 8 significant bits, hi
+// takes the upper 4 and the remainder needs no more than 4.  Two fp8 products with keys as they are
+// stored then give the bf16 product at the matrix cores' same cost, with no conversion of the keys and
+// half the bytes read from LDS.  `n` values in x; e: of the whole row (row_exp); bad: the row is not finite.
+template <int N>
+__device__ __forceinline__ void split_query(const float *x, int e, bool bad, uint32_t *hi, uint32_t *lo) {
+  const float inv = exp2i(-e);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    float y[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] = fminf(fmaxf(x[4 * i + c] * inv, -448.f), 448.f);
+    const uint32_t h = pack_e4m3(y[0], y[1], y[2], y[3]);
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)h, false);
+    const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)h, true);
+    hi[i] = bad ? kBadCodes : h;
+    lo[i] = bad ? kBadCodes
+                : pack_e4m3((y[0] - a[0]) * 16.f, (y[1] - a[1]) * 16.f, (y[2] - b[0]) * 16.f,
+                            (y[3] - b[1]) * 16.f);
+  }
+}
+
+}  // namespace nexus

@@ -70,6 +70,9 @@ struct AttnLaunch {
   // Largest workspace the plan may use: the planner then only considers key splits whose
   // partials fit (SIZE_MAX: no limit, the plan of least estimated time).
   size_t ws_cap = SIZE_MAX;
+  // 8-bit cache (launch_attention_kv8): cache_k and cache_v hold E4M3 codes, rows of head_dim bytes
+  bool kv8 = false;
+  const uint8_t *k_scale = nullptr, *v_scale = nullptr;   // E8M0 bytes [L][NPP][Hkv][16]
 };
 
 // Workspace bytes an attention launch with these sequences needs.

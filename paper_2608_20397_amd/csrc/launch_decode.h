@@ -22,6 +22,8 @@ struct DecodeLaunch {
   float softcap;            // 0 = off
   void *workspace;
   size_t workspace_bytes;
+  // 8-bit cache (launch_decode_kv8): cache_k and cache_v hold E4M3 codes, rows of head_dim bytes
+  const uint8_t *k_scale = nullptr, *v_scale = nullptr;   // E8M0 bytes [L][NPP][Hkv][16]
 };
 
 // Pages per key split of a decode launch (fixed by the shape, not by the device lengths).

@@ -45,6 +45,13 @@ class CKvCache(C.Structure):
                 ("rope_style", C.c_int32), ("rope_base", C.c_double)]
 
 
+class CKv8Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("n_layers", C.c_int32), ("n_phys_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rope_style", C.c_int32), ("rope_base", C.c_double)]
+
+
 class CPageTable(C.Structure):
     _fields_ = [("map", C.c_void_p), ("n_logical_pages", C.c_int32)]
 
@@ -62,6 +69,7 @@ def lib():
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, f32, f64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_size_t
     pB, pC, pT = C.POINTER(CBlock), C.POINTER(CKvCache), C.POINTER(CPageTable)
+    p8, pI32, pI64 = C.POINTER(CKv8Cache), C.POINTER(C.c_int32), C.POINTER(C.c_int64)
     sigs = {
         "nexus_abi_version": (i32, []),
         "nexus_status_str": (C.c_char_p, [i32]),
@@ -85,6 +93,18 @@ def lib():
         "nexus_decode_attn": (i32, [vp, i32, i32, pC, vp, i32, vp, i32, i32, f32, i32, f32, vp,
                                     vp, sz, vp]),
         "nexus_decode_attn_workspace": (sz, [i32, i32, pC, i32]),
+        "nexus_kv8_append": (i32, [p8, pT, vp, vp, i32, i32, i64, i64, vp]),
+        "nexus_kv8_append_step": (i32, [p8, vp, i32, vp, i32, i32, vp, vp, i32, vp]),
+        "nexus_kv8_splice": (i32, [p8, pT, pB, i64, i64, vp]),
+        "nexus_kv8_read": (i32, [p8, pT, i64, i32, i32, vp, vp, vp]),
+        "nexus_kv8_suffix_attn": (i32, [vp, i32, i32, p8, pT, i32, i64, f32, f32, vp, vp, sz, vp]),
+        "nexus_kv8_suffix_attn_workspace": (sz, [i32, i32, p8, i64]),
+        "nexus_kv8_suffix_attn_varlen": (i32, [vp, i32, pI32, pI32, pI64, i32, p8, pT, i32, f32,
+                                               f32, vp, vp, sz, vp]),
+        "nexus_kv8_suffix_attn_varlen_workspace": (sz, [i32, pI32, pI32, pI64, i32, p8]),
+        "nexus_kv8_decode_attn": (i32, [vp, i32, i32, p8, vp, i32, vp, i32, i32, f32, f32, vp, vp,
+                                        sz, vp]),
+        "nexus_kv8_decode_attn_workspace": (sz, [i32, i32, p8, i32]),
         "nexus_kv_copy_tokens": (i32, [pC, vp, vp, i32, i64, i32, vp]),
         "nexus_kv_share_prefix": (i32, [pC, vp, vp, i32, i32, vp]),
         "nexus_l0_longest_prefix": (i32, [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int32),
@@ -152,6 +172,26 @@ def _on_device(*named):
     return dev
 
 
+def _on_current_device(*named):
+    """_on_device, and that device must be the current one: the launch goes to its stream."""
+    dev = _on_device(*named)
+    if dev is not None and dev.index != torch.cuda.current_device():
+        raise NexusError(EINVAL, f"operands are on {dev}, the current device is "
+                                 f"{torch.cuda.current_device()}")
+
+
+def _checked_map(cache, k: torch.Tensor, pm: torch.Tensor) -> CPageTable:
+    if pm.dtype != torch.int32 or pm.dim() != 1 or not pm.is_contiguous():
+        raise NexusError(EINVAL, "page_map must be a contiguous int32 vector")
+    _on_device(("cache k", k), ("page_map", pm))
+    npp = k.shape[1]
+    key = (pm.data_ptr(), pm._version, pm.numel(), npp)
+    if cache._map_checked != key:
+        check_page_table(pm.cpu().numpy(), npp)      # raises NexusError(ERANGE)
+        cache._map_checked = key
+    return CPageTable(pm.data_ptr(), pm.numel())
+
+
 @dataclass
 class Block:
     """A compiled KV block in HBM: k, v [n_layers][n_tokens][n_kv_heads][head_dim]."""
@@ -201,16 +241,7 @@ class PagedKVCache:
                         _dtype_code(self.k), self.v_layout, self.rope_style, self.rope_base)
 
     def pt(self) -> CPageTable:
-        pm = self.page_map
-        if pm.dtype != torch.int32 or pm.dim() != 1 or not pm.is_contiguous():
-            raise NexusError(EINVAL, "page_map must be a contiguous int32 vector")
-        _on_device(("cache k", self.k), ("page_map", pm))
-        npp = self.k.shape[1]
-        key = (pm.data_ptr(), pm._version, pm.numel(), npp)
-        if self._map_checked != key:
-            check_page_table(pm.cpu().numpy(), npp)      # raises NexusError(ERANGE)
-            self._map_checked = key
-        return CPageTable(pm.data_ptr(), pm.numel())
+        return _checked_map(self, self.k, self.page_map)
 
     @property
     def n_layers(self):
@@ -420,6 +451,231 @@ def decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, seq_le
                                    cache.v_layout if v_layout is None else v_layout, scale,
                                    _ptr(out), _ptr(ws), nbytes, _stream()),
            "nexus_decode_attn")
+    return out
+
+
+@dataclass
+class KV8Cache:
+    """A paged cache in 8 bits: k, v [L][n_phys_pages][H][16][D] of torch.float8_e4m3fn (or the
+    same bytes as uint8), k_scale, v_scale uint8 [L][n_phys_pages][H][16], one scale 2^(byte - 127)
+    for each row (token and head); page_map as PagedKVCache, checked the same way.  V is row-major.
+
+    :meth:`empty` allocates one.  Pages are written by kv8_append, kv8_append_step and kv8_splice,
+    read back by kv8_read and attended to by kv8_suffix_attn(_varlen) and kv8_decode_attn."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    page_map: torch.Tensor
+    rope_base: float
+    rope_style: int = ROPE_NEOX
+    _map_checked: tuple | None = field(default=None, init=False, repr=False, compare=False)
+
+    @classmethod
+    def empty(cls, n_layers: int, n_phys_pages: int, n_kv_heads: int, head_dim: int,
+              page_map: torch.Tensor, rope_base: float, rope_style: int = ROPE_NEOX):
+        """A cache of unwritten pages on page_map's device."""
+        rows = (n_layers, n_phys_pages, n_kv_heads, PAGE)
+        new = lambda shape, dt: torch.empty(shape, dtype=dt, device=page_map.device)
+        return cls(new((*rows, head_dim), torch.float8_e4m3fn), new((*rows, head_dim), torch.float8_e4m3fn),
+                   new(rows, torch.uint8), new(rows, torch.uint8), page_map, rope_base, rope_style)
+
+    def c(self) -> CKv8Cache:
+        if self.k.dim() != 5:
+            raise NexusError(ESHAPE, "cache k must be [L][pages][H][16][D]")
+        L, npp, H, P, D = self.k.shape
+        parts = (("cache k", self.k), ("cache v", self.v), ("k_scale", self.k_scale),
+                 ("v_scale", self.v_scale))
+        _on_current_device(*parts, ("page_map", self.page_map))
+        for name, t in parts:
+            scale = name.endswith("scale")
+            if t.dtype != torch.uint8 and (scale or t.dtype != torch.float8_e4m3fn):
+                raise NexusError(EDTYPE, f"{name}: unsupported dtype {t.dtype}")
+            if tuple(t.shape) != ((L, npp, H, P) if scale else (L, npp, H, P, D)) or P != PAGE \
+                    or not t.is_contiguous():
+                raise NexusError(ESHAPE, f"{name} must be contiguous [L][pages][H][16]"
+                                         f"{'' if scale else '[D]'}, got {tuple(t.shape)}")
+        return CKv8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                         self.v_scale.data_ptr(), L, npp, P, H, D, self.rope_style, self.rope_base)
+
+    def pt(self) -> CPageTable:
+        return _checked_map(self, self.k, self.page_map)
+
+
+def _kv8_rows(cc: CKv8Cache, k: torch.Tensor, v: torch.Tensor):
+    """Checks rows [L][n][H][D] beside an 8-bit cache; returns n and their dtype's code."""
+    if k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (cc.n_layers, cc.n_kv_heads, cc.head_dim) \
+            or v.shape != k.shape or not (k.is_contiguous() and v.is_contiguous()):
+        raise NexusError(ESHAPE, "k/v must be contiguous [L][T][H][D] with the cache's L, H and D")
+    if v.dtype != k.dtype:
+        raise NexusError(EDTYPE, "k and v dtypes differ")
+    _on_current_device(("k", k), ("v", v))
+    return k.shape[1], _dtype_code(k)
+
+
+def kv8_append(cache: KV8Cache, k: torch.Tensor, v: torch.Tensor, offset: int, pos0: int):
+    """Quantise un-rotated keys ``k`` (rotated here to positions pos0 + j) and values ``v``, both
+    [L][T][H][D] bf16 or fp32, into logical slots offset .. offset + T - 1."""
+    cc, pt = cache.c(), cache.pt()
+    n, dt = _kv8_rows(cc, k, v)
+    _check(lib().nexus_kv8_append(C.byref(cc), C.byref(pt), _ptr(k), _ptr(v), dt, n, offset, pos0,
+                                  _stream()), "nexus_kv8_append")
+
+
+def kv8_append_step(cache: KV8Cache, maps: torch.Tensor, seq_len: torch.Tensor, max_seq_len: int,
+                    k: torch.Tensor, v: torch.Tensor):
+    """One new token for each sequence, k, v [L][n_seqs][H][D]: rotated to position seq_len[b] - 1
+    and written to that slot of map row b (device int32 ``maps`` [n_seqs][stride] and ``seq_len``
+    [n_seqs]; lengths outside [1, max_seq_len] write nothing)."""
+    cc = cache.c()
+    n, dt = _kv8_rows(cc, k, v)
+    _kv8_maps(maps, seq_len, n)
+    _check(lib().nexus_kv8_append_step(C.byref(cc), _ptr(maps), maps.shape[1], _ptr(seq_len), n,
+                                       max_seq_len, _ptr(k), _ptr(v), dt, _stream()),
+           "nexus_kv8_append_step")
+
+
+def kv8_splice(cache: KV8Cache, block: Block, offset: int, dst_pos: int):
+    """Splice ``block`` (bf16 or fp32) at ``offset``, its keys re-anchored from block.base_pos to
+    ``dst_pos`` and quantised in the same pass (the block itself is left as it is)."""
+    cc, pt, cb = cache.c(), cache.pt(), block.c()
+    if block.v.dtype != block.k.dtype:
+        raise NexusError(EDTYPE, "block k and v dtypes differ")
+    _on_current_device(("block k", block.k))
+    _check(lib().nexus_kv8_splice(C.byref(cc), C.byref(pt), C.byref(cb), offset, dst_pos, _stream()),
+           "nexus_kv8_splice")
+
+
+def kv8_read(cache: KV8Cache, offset: int, n_tokens: int, dtype: torch.dtype = torch.bfloat16,
+             out=None):
+    """The values of logical tokens offset .. offset + n_tokens - 1 as (k, v), [L][T][H][D] of
+    ``dtype`` (bf16 or fp32; both hold them exactly); ``out`` may hold preallocated (k, v)."""
+    cc, pt = cache.c(), cache.pt()
+    shape = (cc.n_layers, max(0, n_tokens), cc.n_kv_heads, cc.head_dim)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    k, v = out
+    if tuple(k.shape) != shape or k.dtype != dtype:
+        raise NexusError(ESHAPE, f"out must be two {shape} tensors of {dtype}")
+    n, dt = _kv8_rows(cc, k, v)
+    _check(lib().nexus_kv8_read(C.byref(cc), C.byref(pt), offset, n_tokens, dt, _ptr(k), _ptr(v),
+                                _stream()), "nexus_kv8_read")
+    return k, v
+
+
+def _kv8_maps(maps: torch.Tensor, seq_len: torch.Tensor, n: int):
+    _on_current_device(("maps", maps), ("seq_len", seq_len))
+    if maps.dtype != torch.int32 or maps.dim() != 2 or maps.shape[0] != n or not maps.is_contiguous():
+        raise NexusError(EINVAL, "maps must be a contiguous int32 [n_seqs][stride] device tensor")
+    if seq_len.dtype != torch.int32 or tuple(seq_len.shape) != (n,) or not seq_len.is_contiguous():
+        raise NexusError(EINVAL, "seq_len must be a contiguous int32 [n_seqs] device tensor")
+
+
+def _kv8_query(q: torch.Tensor, cc: CKv8Cache, out, workspace):
+    """Checks q [rows][n_q_heads][D] (bf16), out and workspace; returns out."""
+    if q.dim() != 3 or q.shape[2] != cc.head_dim:
+        raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
+    if not q.is_contiguous():
+        raise NexusError(EINVAL, "q must be contiguous")
+    if q.dtype != torch.bfloat16:
+        raise NexusError(EDTYPE, "q must be bf16 over an 8-bit cache")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
+    if workspace is not None and not workspace.is_contiguous():
+        raise NexusError(EINVAL, "workspace must be contiguous")
+    _on_current_device(("q", q), ("out", out), ("workspace", workspace))
+    return out
+
+
+def _kv8_workspace(nbytes: int, q: torch.Tensor, workspace):
+    """(pointer, bytes) of the caller's workspace, or of one allocated here."""
+    if nbytes == (1 << 64) - 1:
+        return None, 0             # invalid arguments: the call itself reports which check failed
+    ws = _workspace(nbytes, q.device, workspace)
+    return ws, ws.numel() * ws.element_size() if ws is not None else 0
+
+
+def kv8_suffix_attn_workspace_bytes(cache: KV8Cache, n_s: int, n_q_heads: int, n_past: int) -> int:
+    cc = cache.c()
+    n = lib().nexus_kv8_suffix_attn_workspace(n_s, n_q_heads, C.byref(cc), n_past)
+    if n == (1 << 64) - 1:
+        raise NexusError(EINVAL, "nexus_kv8_suffix_attn_workspace")
+    return n
+
+
+def kv8_suffix_attn(q: torch.Tensor, cache: KV8Cache, layer: int, n_past: int, softcap: float = 0.0,
+                    scale: float = 0.0, out: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None):
+    """suffix_attn over an 8-bit cache: q [n_s][n_q_heads][D] bf16 -> out, alike."""
+    cc, pt = cache.c(), cache.pt()
+    out = _kv8_query(q, cc, out, workspace)
+    n_s, hq, _ = q.shape
+    need = lib().nexus_kv8_suffix_attn_workspace(n_s, hq, C.byref(cc), n_past)
+    ws, nbytes = _kv8_workspace(need, q, workspace)
+    _check(lib().nexus_kv8_suffix_attn(_ptr(q), n_s, hq, C.byref(cc), C.byref(pt), layer, n_past,
+                                       softcap, scale, _ptr(out), _ptr(ws), nbytes, _stream()),
+           "nexus_kv8_suffix_attn")
+    return out
+
+
+def kv8_suffix_attn_varlen(q: torch.Tensor, q_start, seq_len, seq_n_past, cache: KV8Cache,
+                           layer: int, softcap: float = 0.0, scale: float = 0.0,
+                           out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """suffix_attn_varlen over an 8-bit cache."""
+    n = len(seq_len)
+    if len(q_start) != n or len(seq_n_past) != n:
+        raise NexusError(EINVAL, "q_start, seq_len and seq_n_past differ in length")
+    cc, pt = cache.c(), cache.pt()
+    out = _kv8_query(q, cc, out, workspace)
+    _, hq, _ = q.shape
+    if any(s + m > q.shape[0] for s, m in zip(q_start, seq_len)):
+        raise NexusError(ERANGE, "a sequence's rows lie past q")
+    qs, ls, ps = (C.c_int32 * n)(*q_start), (C.c_int32 * n)(*seq_len), (C.c_int64 * n)(*seq_n_past)
+    need = lib().nexus_kv8_suffix_attn_varlen_workspace(n, qs, ls, ps, hq, C.byref(cc))
+    ws, nbytes = _kv8_workspace(need, q, workspace)
+    _check(lib().nexus_kv8_suffix_attn_varlen(_ptr(q), n, qs, ls, ps, hq, C.byref(cc), C.byref(pt),
+                                              layer, softcap, scale, _ptr(out), _ptr(ws), nbytes,
+                                              _stream()), "nexus_kv8_suffix_attn_varlen")
+    return out
+
+
+def kv8_suffix_attn_varlen_workspace_bytes(cache: KV8Cache, q_start, seq_len, seq_n_past,
+                                           n_q_heads: int) -> int:
+    n = len(seq_len)
+    cc = cache.c()
+    nbytes = lib().nexus_kv8_suffix_attn_varlen_workspace(n, (C.c_int32 * n)(*q_start),
+                                                          (C.c_int32 * n)(*seq_len),
+                                                          (C.c_int64 * n)(*seq_n_past), n_q_heads,
+                                                          C.byref(cc))
+    if nbytes == (1 << 64) - 1:
+        raise NexusError(EINVAL, "nexus_kv8_suffix_attn_varlen_workspace")
+    return nbytes
+
+
+def kv8_decode_attn_workspace_bytes(cache: KV8Cache, n_seqs: int, n_q_heads: int,
+                                    max_seq_len: int) -> int:
+    cc = cache.c()
+    n = lib().nexus_kv8_decode_attn_workspace(n_seqs, n_q_heads, C.byref(cc), max_seq_len)
+    if n == (1 << 64) - 1:
+        raise NexusError(EINVAL, "nexus_kv8_decode_attn_workspace")
+    return n
+
+
+def kv8_decode_attn(q: torch.Tensor, cache: KV8Cache, maps: torch.Tensor, seq_len: torch.Tensor,
+                    max_seq_len: int, layer: int, softcap: float = 0.0, scale: float = 0.0,
+                    out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """decode_attn over an 8-bit cache: q [n_seqs][n_q_heads][D] bf16 -> out, alike."""
+    cc = cache.c()
+    out = _kv8_query(q, cc, out, workspace)
+    n, hq, _ = q.shape
+    _kv8_maps(maps, seq_len, n)
+    need = lib().nexus_kv8_decode_attn_workspace(n, hq, C.byref(cc), max_seq_len)
+    ws, nbytes = _kv8_workspace(need, q, workspace)
+    _check(lib().nexus_kv8_decode_attn(_ptr(q), n, hq, C.byref(cc), _ptr(maps), maps.shape[1],
+                                       _ptr(seq_len), max_seq_len, layer, softcap, scale, _ptr(out),
+                                       _ptr(ws), nbytes, _stream()), "nexus_kv8_decode_attn")
     return out
 
 
