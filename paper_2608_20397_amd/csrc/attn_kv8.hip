@@ -10,8 +10,8 @@
 //   * V is converted to bf16 on its way to LDS, its scale applied by the conversion: exact.  P is rounded to
 //     bf16 as in the bf16 kernels and the PV product is theirs (transposed LDS reads, 32x32x16 MFMA).
 //   * A token whose key or value row is not finite (scale byte 255) gives NaN to the queries that see it
-//     and nothing to the others: its scores are set to NaN, then masked like any other, and its values
-//     enter the product as zeros.
+//     and nothing to the others: 255 is its keys' scale operand, which makes its scores NaN; they are masked
+//     like any other, and its values enter the product as zeros.
 //   * Slots past the last key of a workgroup are never read: their rows repeat the last key and are masked.
 // LDS: K row r, 16-byte chunk c at c ^ kswz(r); V (bf16) chunk c at c ^ vswz(r), as the bf16 kernels.
 #include "attn_common.h"
@@ -19,10 +19,12 @@
 #include "kv8_common.h"
 #include "launch_kv8.h"
 
+#include <type_traits>
+
 namespace nexus {
 
 template <int D, bool CAP>
-__global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const AttnArgs a,
+__global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv8_kernel(const AttnArgs a,
                                                                            const AttnPlan plan) {
   static_assert(D == 64 || D == 128 || D == 256, "head_dim");
   constexpr int W = D == 256 ? kWavesWide : kWaves;
@@ -37,6 +39,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
   constexpr int VTILEB = KT * VROWB;
   constexpr int NVC = KT * CH / NT;                // V chunks a thread converts
   constexpr float kSlack = 8.0f;                   // lazy rescale: p <= 2^8 between rescales
+  constexpr int kPrioPV = 2;                       // wave priority of the PV phase (attn_bf16_dma.hip)
   static_assert(NI >= 1 && NVC >= 1 && RPI <= kPage, "tile shape");
   __shared__ __align__(1024) char smem[2 * KTILEB + 2 * VTILEB];
   __shared__ __align__(16) int32_t pg[kMaxSplitKeys / kPage + 8];
@@ -123,7 +126,13 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
 
   // ---- LDS layouts
   auto kswz = [](int row) { return D == 64 ? (row >> 2) & 3 : D == 128 ? (row >> 1) & 7 : row & 15; };
-  auto vswz = [](int row) { return D == 64 ? 4 * ((row >> 1) & 1) : 4 * (row & 3); };
+  // V chunk c of row r: rows that one transposed read covers, and the two halves of a row's chunks that one
+  // conversion writes, on distinct banks
+  auto vchunk = [](int c, int r) {
+    return D == 64    ? c ^ (5 * ((r >> 1) & 1))
+           : D == 128 ? c ^ (4 * (r & 3) + (r & 1))
+                      : c ^ (4 * (r & 3)) ^ ((c >> 4) & 1);
+  };
   // S^T A operand: K row j (+ 32 kb, whose swizzle is the same), features 64 s + 32 hh .. + 31
   uint32_t offk[NS2][2];
 #pragma unroll
@@ -136,13 +145,13 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
     const int h2 = gg >> 1, dh = gg & 1;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
-      offv[db] = (4 * h2 + e) * VROWB + 32 * dh + 8 * q + 64 * (db ^ (D == 64 ? e >> 1 : e));
+      offv[db] = (4 * h2 + e) * VROWB + 16 * vchunk(4 * db + 2 * dh + (q >> 1), e) + 8 * (q & 1);
   }
   auto kbuf = [&](int i) { return smem + i * KTILEB; };
   auto vbuf = [&](int i) { return smem + 2 * KTILEB + i * VTILEB; };
   const uint32_t smem_base = (uint32_t)(uintptr_t)smem;
   const uint64_t pbytes = (uint64_t)a.n_kv_heads * kPage * D;      // one physical page of codes
-  const uint64_t sbytes = (uint64_t)a.n_kv_heads * kPage;          // and of scales
+  const uint32_t sbytes = (uint32_t)a.n_kv_heads * kPage;          // and of scales
   const char *kbytes = reinterpret_cast<const char *>(a.kc) + (uint64_t)kvh * kPage * D;
   const char *vbytes = reinterpret_cast<const char *>(a.vc) + (uint64_t)kvh * kPage * D;
   const uint8_t *ksb = a.ks + kvh * kPage, *vsb = a.vs + kvh * kPage;
@@ -151,67 +160,103 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
   wait_vm<0>();
   __syncthreads();   // pg[] visible
 
-  auto page_at = [&](int lp) -> uint64_t {    // wave-uniform logical page, counted from pg0
+  auto page_at = [&](int lp) -> uint32_t {    // wave-uniform logical page, counted from pg0
     return (uint32_t)__builtin_amdgcn_readfirstlane(pg[lp]);
   };
-  // DMA of K tile `it`: instruction i of the wave fills rows (wave NI + i) RPI ..
-  auto dma_k = [&](int it) {
-    const int kt = k_begin + it * KT;
-    const uint32_t dst = smem_base + (it & 1) * KTILEB + wave * NI * 1024;
+  auto full = [&](int it) { return k_begin + it * KT + KT <= k_end; };
+  // Pages of a wave's share of a whole tile: one per DMA instruction and per chunk of V codes.
+  struct Pages {
+    uint32_t k[NI], v[NVC];
+  };
+  auto k_pages = [&](int it, Pages &p) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int row0 = (wave * NI + i) * RPI;
-      const int row = row0 + lane / CH;
-      const uint32_t c = (lane % CH) ^ kswz(row);
-      if (kt + KT <= k_end) {
-        const char *ps = kbytes + page_at(it * (KT / kPage) + row0 / kPage) * pbytes;
-        dma_s<0>(dst + i * 1024, ps, (uint32_t)(row & (kPage - 1)) * D + 16 * c);
-      } else {
-        const int t = min(kt + row, k_end - 1);
+    for (int i = 0; i < NI; ++i) p.k[i] = page_at(it * (KT / kPage) + (wave * NI + i) * RPI / kPage);
+  };
+  auto v_pages = [&](int it, Pages &p) {
+#pragma unroll
+    for (int k = 0; k < NVC; ++k) p.v[k] = page_at(it * (KT / kPage) + (64 * wave + NT * k) / CH / kPage);
+  };
+  // DMA of K tile `it`: instruction i of the wave fills rows (wave NI + i) RPI ..
+  uint32_t kdo[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int row = (wave * NI + i) * RPI + lane / CH;
+    kdo[i] = (row & (kPage - 1)) * D + 16 * ((lane % CH) ^ kswz(row));
+  }
+  auto dma_k = [&](int it, const Pages &p) {
+    const uint32_t dst = smem_base + (it & 1) * KTILEB + wave * NI * 1024;
+    if (full(it)) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) dma_s<0>(dst + i * 1024, kbytes + p.k[i] * pbytes, kdo[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int row = (wave * NI + i) * RPI + lane / CH;
+        const int t = min(k_begin + it * KT + row, k_end - 1);
         const uint64_t pp = (uint32_t)pg[(t >> kPageShift) - pg0];
-        dma_v(dst + i * 1024, kbytes + pp * pbytes + (uint32_t)(t & (kPage - 1)) * D + 16 * c);
+        dma_v(dst + i * 1024, kbytes + pp * pbytes + (uint32_t)(t & (kPage - 1)) * D +
+                                  16 * ((lane % CH) ^ kswz(row)));
       }
     }
   };
-  struct Stage {
-    u32x4 v[NVC];                              // V codes on their way to LDS
-    uint32_t vs[NVC];                          // their rows' scale bytes
-    uint32_t ks, vt;                           // key and value scale bytes of token `lane` of the tile
+  // V codes on their way to LDS: chunk lane % CH of rows (64 wave + NT k) / CH + lane / CH
+  struct Codes {
+    u32x4 v[NVC];
   };
-  auto load_tile = [&](int it, Stage &sg) {
-    const int kt = k_begin + it * KT;
-    const bool full = kt + KT <= k_end;
+  const uint32_t vdo = ((64 * wave / CH + lane / CH) & (kPage - 1)) * D + 16 * (lane % CH);
+  auto load_v = [&](int it, const Pages &p, Codes &cd) {
+    if (full(it)) {
 #pragma unroll
-    for (int k = 0; k < NVC; ++k) {
-      const int row0 = (64 * wave + NT * k) / CH;
-      const int row = row0 + lane / CH;
-      const int t = full ? kt + row : min(kt + row, k_end - 1);
-      const uint64_t pp = full ? page_at(it * (KT / kPage) + row0 / kPage)
-                               : (uint64_t)(uint32_t)pg[(t >> kPageShift) - pg0];
-      const uint32_t slot = t & (kPage - 1);
-      sg.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + pp * pbytes + slot * D + 16 * (lane % CH));
-      sg.vs[k] = vsb[pp * sbytes + slot];
+      for (int k = 0; k < NVC; ++k)
+        cd.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + p.v[k] * pbytes + vdo);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NVC; ++k) {
+        const int t = min(k_begin + it * KT + (64 * wave + NT * k) / CH + lane / CH, k_end - 1);
+        const uint64_t pp = (uint32_t)pg[(t >> kPageShift) - pg0];
+        cd.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + pp * pbytes +
+                                                   (uint32_t)(t & (kPage - 1)) * D + 16 * (lane % CH));
+      }
     }
-    const int t = min(kt + (lane & (KT - 1)), k_end - 1);
-    const uint64_t pp = (uint32_t)pg[(t >> kPageShift) - pg0];
-    sg.ks = ksb[pp * sbytes + (t & (kPage - 1))];
-    sg.vt = vsb[pp * sbytes + (t & (kPage - 1))];
   };
-  // V codes of a tile to bf16 in LDS; a row that is not finite as zeros
-  auto store_v = [&](int it, const Stage &sg) {
+  // key and value scale bytes of token `lane` of tile `it` (a layer's scales lie within 32-bit offsets)
+  struct Scales {
+    uint32_t k, v;
+  };
+  auto load_scales = [&](int it, Scales &s) {
+    const int t = min(k_begin + it * KT + (lane & (KT - 1)), k_end - 1);
+    const uint32_t at = (uint32_t)pg[(t >> kPageShift) - pg0] * sbytes + (t & (kPage - 1));
+    s.k = ksb[at];
+    s.v = vsb[at];
+  };
+  // the MFMA's scale operands of a tile's keys
+  auto operands = [&](const Scales &s, int (&ks)[2]) {
+    const uint32_t k = s.v == kBadScale ? kBadScale : s.k;
+    const auto r = __builtin_amdgcn_permlane32_swap(k, k, false, false);
+    ks[0] = (int)r[0];
+    ks[1] = (int)r[1];
+  };
+  // V codes of a tile to bf16 in LDS, `vs`: the value scale byte of token `lane`; a row that is not finite
+  // as zeros
+  auto store_v = [&](int it, Codes cd, uint32_t vs) {
     char *vl = vbuf(it & 1);
+    const bool any_bad = __builtin_amdgcn_ballot_w64(vs == kBadScale) != 0;
 #pragma unroll
     for (int k = 0; k < NVC; ++k) {
       const int row = (64 * wave + NT * k) / CH + lane / CH;
       const int c = 2 * (lane % CH);
-      const bool bad = sg.vs[k] == kBadScale;
-      const float s = bad ? 1.f : exp2i((int)sg.vs[k] - 127);
+      uint32_t byte = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)vs);
+      if (any_bad && byte == kBadScale) {
+        cd.v[k] = u32x4{0u, 0u, 0u, 0u};
+        byte = 127;
+      }
+      const float s = __uint_as_float(byte << 23);
       u32x2 w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = codes_to_bf16(bad ? 0u : sg.v[k][i], s);
-      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * (c ^ vswz(row))) =
+      for (int i = 0; i < 4; ++i) w[i] = codes_to_bf16(cd.v[k][i], s);
+      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * vchunk(c, row)) =
           u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
-      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * ((c + 1) ^ vswz(row))) =
+      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * vchunk(c + 1, row)) =
           u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
     }
   };
@@ -219,72 +264,57 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
   const float c_scale = CAP ? 1.0f : a.scale_log2;
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
 
-  Stage sg{};
-  if (n_tiles > 0) {
-    dma_k(0);
-    load_tile(0, sg);
-  }
-  for (int it = 0; it < n_tiles; ++it) {
-    const int kt = k_begin + it * KT;
-    wait_vm<0>();
-    store_v(it, sg);
-    // scales of this tile's tokens, and which of them are not finite
-    const uint64_t bad = __builtin_amdgcn_ballot_w64(sg.ks == kBadScale || sg.vt == kBadScale);
-    const auto ksw = __builtin_amdgcn_permlane32_swap(sg.ks, sg.ks, false, false);
-    tile_barrier();   // K and V of tile `it` are in LDS; the other buffers are free
-    if (it + 1 < n_tiles) {
-      load_tile(it + 1, sg);
-      dma_k(it + 1);
-    }
-    if (!active) continue;
-    const char *kl = kbuf(it & 1), *vl = vbuf(it & 1);
-    // ---- S^T = K . Q^T
-    f32x16 sc[NKB];
+  // S^T of the tile in K buffer `kl`, whose tokens' scale bytes are the operands ks (raw scores)
+  auto qk = [&](const char *kl, const int (&ks)[2], f32x16 *sc) {
 #pragma unroll
-    for (int kb = 0; kb < NKB; ++kb) {
+    for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
       for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
 #pragma unroll
-      for (int s = 0; s < NS2; ++s) {
+    for (int s = 0; s < NS2; ++s)
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb) {
         const u32x4 x = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][0]);
         const u32x4 y = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][1]);
         const i32x8 ka = {(int)x[0], (int)x[1], (int)x[2], (int)x[3],
                           (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        const int ks = (int)ksw[kb];
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qhi[s], sc[kb], 0, 0, 0, ks, 0,
+        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qhi[s], sc[kb], 0, 0, 0, ks[kb], 0,
                                                                  qscale_hi);
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qlo[s], sc[kb], 0, 0, 0, ks, 0,
+        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qlo[s], sc[kb], 0, 0, 0, ks[kb], 0,
                                                                  qscale_lo);
       }
-    }
+  };
+  auto cap = [&](f32x16 *sc) {
     if constexpr (CAP) {
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
         for (int v = 0; v < 16; ++v) sc[kb][v] = a.cap_out * tanh_fast(sc[kb][v] * a.cap_in);
     }
-    if (bad) {
+  };
+  // S(t) needs the causal / tail mask when its tile crosses this wave's diagonal or the split end
+  auto needs_mask = [&](int t) {
+    const int kt = k_begin + t * KT;
+    return (kt + KT > k_end) || (kt + KT - 1 > qpos0);
+  };
+  auto mask = [&](f32x16 *sc, int t) {
+    const int lim = min(qpos0 + j, k_end - 1) - (k_begin + t * KT) - 4 * hh;   // last visible key
 #pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
+    for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (bad >> (32 * kb + 8 * (v >> 2) + 4 * hh + (v & 3)) & 1) sc[kb][v] = __builtin_nanf("");
-    }
-    if ((kt + KT > k_end) || (kt + KT - 1 > qpos0)) {
-      const int lim = min(qpos0 + j, k_end - 1) - kt - 4 * hh;   // last visible key - base
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (32 * kb + 8 * (v >> 2) + (v & 3) > lim) sc[kb][v] = -INFINITY;
-    }
-    // ---- online softmax (log2 units), lazily rescaled
+      for (int v = 0; v < 16; ++v)
+        if (32 * kb + 8 * (v >> 2) + (v & 3) > lim) sc[kb][v] = -INFINITY;
+  };
+  auto row_max = [&](const f32x16 *sc) -> float {
     float mt = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
       for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sc[kb][v]);
-    mt = max_halves(mt) * c_scale;
+    return max_halves(mt) * c_scale;
+  };
+  // moves the reference to a maximum that has left it behind; returns the exponent's addend
+  auto rescale = [&](float mt) -> float {
     if (__builtin_amdgcn_ballot_w64(mt > m_ref + kSlack) != 0) {
       const float m_new = fmaxf(m_ref, mt);
       const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m_ref - m_new);
@@ -295,28 +325,174 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, 2) void attn_kv8_kernel(const
         for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
       m_ref = m_new;
     }
-    const float nm = (m_ref == -INFINITY) ? 0.f : -m_ref;
+    return (m_ref == -INFINITY) ? 0.f : -m_ref;
+  };
+  // P of 16 keys (half hf of a score block) as a PV operand; adds their sum to l
+  auto softmax_half = [&](const f32x16 &sc, int hf, float nm) -> bf16x8 {
+    uint32_t w[4];
 #pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
+    for (int e = 0; e < 4; ++e) {
+      const float p0 = fast_exp2(fmaf(sc[8 * hf + 2 * e], c_scale, nm));
+      const float p1 = fast_exp2(fmaf(sc[8 * hf + 2 * e + 1], c_scale, nm));
+      w[e] = pack_bf16x2(p0, p1);
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), ones, l, false);
+    }
+    return __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+  };
+  // O^T += V^T P^T over the 16 keys of step ks of the V tile at vl
+  auto pv_step = [&](const char *vl, int ks, const bf16x8 &pb) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        uint32_t w[4];
+    for (int db = 0; db < NDB; ++db) {
+      const char *p = vl + ks * 16 * VROWB + offv[db];
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_read_pair(p, p + 8 * VROWB), pb, o[db], 0, 0, 0);
+    }
+  };
+
+  Codes cd{};
+  Scales sn{};                               // scales of the tile that loads
+  Pages pn{};                                // pages of the tiles to load next
+  if constexpr (D == 256) {
+    // ---- a tile at a time: K by DMA and V codes in registers while the one before is computed
+    if (n_tiles > 0) {
+      if (full(0)) {
+        k_pages(0, pn);
+        v_pages(0, pn);
+      }
+      load_v(0, pn, cd);
+      load_scales(0, sn);
+      dma_k(0, pn);
+    }
+    for (int it = 0; it < n_tiles; ++it) {
+      wait_vm<0>();
+      store_v(it, cd, sn.v);
+      int ks[2];
+      operands(sn, ks);
+      if (it + 1 < n_tiles && full(it + 1)) {
+        k_pages(it + 1, pn);
+        v_pages(it + 1, pn);
+      }
+      tile_barrier();   // K and V of tile `it` are in LDS; the other buffers are free
+      if (it + 1 < n_tiles) {
+        load_v(it + 1, pn, cd);
+        load_scales(it + 1, sn);
+        dma_k(it + 1, pn);
+      }
+      if (!active) continue;
+      f32x16 sc[NKB];
+      qk(kbuf(it & 1), ks, sc);
+      cap(sc);
+      if (needs_mask(it)) mask(sc, it);
+      const float nm = rescale(row_max(sc));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p0 = fast_exp2(fmaf(sc[kb][8 * hf + 2 * e], c_scale, nm));
-          const float p1 = fast_exp2(fmaf(sc[kb][8 * hf + 2 * e + 1], c_scale, nm));
-          w[e] = pack_bf16x2(p0, p1);
-          l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), ones, l, false);
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) pv_step(vbuf(it & 1), 2 * kb + hf, softmax_half(sc[kb], hf, nm));
+    }
+  } else {
+    // ---- the schedule of attn_bf16_dma.hip: per iteration t the wave computes S(t + 1) = K[t + 1] Q^T
+    // beside the exponentials of S(t), then O += V[t] P(t) beside the maximum of S(t + 1), while K[t + 2]
+    // travels by DMA and the codes of V[t + 1] to registers, from which they go to LDS as bf16 at the end
+    f32x16 sa[NKB], sb[NKB];
+    int ks[2] = {127, 127};                 // scale operands of tile t + 1's keys
+    uint32_t vs = 127;                      // value scale of its token `lane`
+    if (n_tiles > 0) {
+      if (full(0)) {
+        k_pages(0, pn);
+        v_pages(0, pn);
+      }
+      load_v(0, pn, cd);
+      load_scales(0, sn);
+      dma_k(0, pn);
+      wait_vm<0>();
+      store_v(0, cd, sn.v);
+      operands(sn, ks);
+      if (n_tiles > 1) {
+        if (full(1)) {
+          k_pages(1, pn);
+          v_pages(1, pn);
         }
-        const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-        // ---- O^T += V^T . P^T over the 16 keys of this step
+        load_scales(1, sn);
+        dma_k(1, pn);
+      }
+    }
+    tile_barrier();
+    float mt_cur = -INFINITY;               // row maximum of S(t), log2 units
+    if (active && n_tiles > 0) {
+      qk(kbuf(0), ks, sa);
+      cap(sa);
+      mt_cur = row_max(sa);                 // unmasked: step 0 masks S(0) and takes its maximum again
+    }
+    wait_vm<0>();
+    operands(sn, ks);
+    vs = sn.v;
+    if (n_tiles > 2 && full(2)) k_pages(2, pn);
+    tile_barrier();                         // K buffer 0 is refilled in iteration 0; K[1] has landed
+
+    auto step = [&](int t, auto parity, f32x16 *s_cur, f32x16 *s_nxt) {
+      constexpr int P = decltype(parity)::value;     // t & 1
+      if (t + 1 < n_tiles) load_v(t + 1, pn, cd);
+      if (t + 2 < n_tiles) {
+        load_scales(t + 2, sn);
+        dma_k(t + 2, pn);
+      }
+      if (active) {
+        if (needs_mask(t)) {
+          mask(s_cur, t);
+          mt_cur = row_max(s_cur);
+        }
+        const float nm = rescale(mt_cur);
+        const char *vl = vbuf(P);
+        bf16x8 pb[4];
+        qk(kbuf(P ^ 1), ks, s_nxt);
+        pb[0] = softmax_half(s_cur[0], 0, nm);
+        pb[1] = softmax_half(s_cur[0], 1, nm);
+        pb[2] = softmax_half(s_cur[1], 0, nm);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          const char *p = vl + (2 * kb + hf) * 16 * VROWB + offv[db];
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_read_pair(p, p + 8 * VROWB), pb, o[db], 0,
-                                                          0, 0);
+        for (int i = 0; i < 2 * NKB * NS2; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 20 : 10, 0);
+        }
+        __builtin_amdgcn_s_setprio(kPrioPV);
+        pv_step(vl, 0, pb[0]);
+        pv_step(vl, 1, pb[1]);
+        pv_step(vl, 2, pb[2]);
+        pb[3] = softmax_half(s_cur[1], 1, nm);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+        for (int i = 0; i < 3 * NDB; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 4 : 2, 1);
+        }
+        pv_step(vl, 3, pb[3]);
+        cap(s_nxt);
+        mt_cur = row_max(s_nxt);
+#pragma unroll
+        for (int i = 0; i < NDB; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 2);
+          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 12 : 6, 2);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
+      // pages of the next iteration's loads (their LDS reads overlap the wait)
+      if (t + 3 < n_tiles && full(t + 3)) k_pages(t + 3, pn);
+      if (t + 2 < n_tiles && full(t + 2)) v_pages(t + 2, pn);
+      // K[t + 2] and the codes of V[t + 1], asked for above, have had the iteration to arrive
+      wait_vm<0>();
+      if (t + 1 < n_tiles) store_v(t + 1, cd, vs);
+      operands(sn, ks);
+      vs = sn.v;
+      tile_barrier();
+    };
+    // Every iteration computes S(t + 1), on the last tile from a stale buffer, never used (a branch there
+    // would split the scheduled region).
+    for (int t = 0; t < n_tiles; t += 2) {
+      step(t, std::integral_constant<int, 0>{}, sa, sb);
+      if (t + 1 < n_tiles) step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
   }
 
   // ---- epilogue

@@ -23,6 +23,8 @@ nexus_status check_kv8(const nexus_kv8_cache *c) {
   // token positions are 32-bit, and so are offsets within a page; a layer may be of any size
   if ((int64_t)c->n_phys_pages * kPageSize >= kMaxElems32) return NEXUS_ESHAPE;
   if ((int64_t)kPageSize * c->n_kv_heads * c->head_dim >= kMaxElems32) return NEXUS_ESHAPE;
+  // ... and offsets among a layer's scales (2^32 rows of K and of V would not fit the memory)
+  if ((int64_t)c->n_phys_pages * kPageSize * c->n_kv_heads >= ((int64_t)1 << 32)) return NEXUS_ESHAPE;
   if (!(c->rope_base > 1.0) || !isfinite(c->rope_base)) return NEXUS_EROPE;
   return NEXUS_OK;
 }
