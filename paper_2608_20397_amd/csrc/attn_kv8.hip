@@ -126,12 +126,12 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
 
   // ---- LDS layouts
   auto kswz = [](int row) { return D == 64 ? (row >> 2) & 3 : D == 128 ? (row >> 1) & 7 : row & 15; };
-  // V chunk c of row r: rows that one transposed read covers, and the two halves of a row's chunks that one
-  // conversion writes, on distinct banks
+  // V chunk c of row r.  Bits 2 and 3 put the rows of one transposed read on distinct banks; bit 0 does so
+  // with the chunks of one conversion's writes, every second of a row, over 128 and over 256 bytes.
   auto vchunk = [](int c, int r) {
-    return D == 64    ? c ^ (5 * ((r >> 1) & 1))
-           : D == 128 ? c ^ (4 * (r & 3) + (r & 1))
-                      : c ^ (4 * (r & 3)) ^ ((c >> 4) & 1);
+    return D == 64    ? c ^ (4 * ((r >> 1) & 1)) ^ ((r ^ (r >> 1)) & 1)
+           : D == 128 ? c ^ (4 * (r & 3)) ^ ((r ^ (c >> 3)) & 1)
+                      : c ^ (4 * (r & 3)) ^ (((c >> 3) ^ (c >> 4)) & 1);
   };
   // S^T A operand: K row j (+ 32 kb, whose swizzle is the same), features 64 s + 32 hh .. + 31
   uint32_t offk[NS2][2];
@@ -209,6 +209,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
 #pragma unroll
       for (int k = 0; k < NVC; ++k)
         cd.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + p.v[k] * pbytes + vdo);
+      // (keeps these loads apart from the others below, whose addresses are the lanes' own)
+      asm volatile("" ::: "memory");
     } else {
 #pragma unroll
       for (int k = 0; k < NVC; ++k) {
@@ -236,28 +238,37 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     ks[0] = (int)r[0];
     ks[1] = (int)r[1];
   };
-  // V codes of a tile to bf16 in LDS, `vs`: the value scale byte of token `lane`; a row that is not finite
-  // as zeros
-  auto store_v = [&](int it, Codes cd, uint32_t vs) {
-    char *vl = vbuf(it & 1);
-    const bool any_bad = __builtin_amdgcn_ballot_w64(vs == kBadScale) != 0;
+  // V codes of a tile to bf16 in V buffer `buf`, `vs`: the value scale byte of token `lane`; a row that is
+  // not finite as zeros
+  uint32_t vrow[NVC], vdst[NVC][2];
+#pragma unroll
+  for (int k = 0; k < NVC; ++k) {
+    const int row = (64 * wave + NT * k) / CH + lane / CH, c = 2 * (lane % CH);
+    vrow[k] = 4 * row;
+    vdst[k][0] = row * VROWB + 16 * vchunk(c, row);
+    vdst[k][1] = row * VROWB + 16 * vchunk(c + 1, row);
+  }
+  auto store_v = [&](int buf, Codes &cd, uint32_t vs) {
+    char *vl = vbuf(buf);
+    uint32_t byte[NVC];
+#pragma unroll
+    for (int k = 0; k < NVC; ++k) byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(vrow[k], (int)vs);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(vs == kBadScale) != 0, 0)) {
+#pragma unroll
+      for (int k = 0; k < NVC; ++k)
+        if (byte[k] == kBadScale) {
+          cd.v[k] = u32x4{0u, 0u, 0u, 0u};
+          byte[k] = 127;
+        }
+    }
 #pragma unroll
     for (int k = 0; k < NVC; ++k) {
-      const int row = (64 * wave + NT * k) / CH + lane / CH;
-      const int c = 2 * (lane % CH);
-      uint32_t byte = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)vs);
-      if (any_bad && byte == kBadScale) {
-        cd.v[k] = u32x4{0u, 0u, 0u, 0u};
-        byte = 127;
-      }
-      const float s = __uint_as_float(byte << 23);
+      const float s = __uint_as_float(byte[k] << 23);
       u32x2 w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = codes_to_bf16(cd.v[k][i], s);
-      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * vchunk(c, row)) =
-          u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
-      *reinterpret_cast<u32x4 *>(vl + row * VROWB + 16 * vchunk(c + 1, row)) =
-          u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
+      *reinterpret_cast<u32x4 *>(vl + vdst[k][0]) = u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
+      *reinterpret_cast<u32x4 *>(vl + vdst[k][1]) = u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
     }
   };
 
@@ -270,19 +281,24 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
       for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
+    // (the terms of one score block stand apart: a product waits for the one before it on its accumulators)
 #pragma unroll
-    for (int s = 0; s < NS2; ++s)
+    for (int s = 0; s < NS2; ++s) {
+      i32x8 ka[NKB];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb) {
         const u32x4 x = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][0]);
         const u32x4 y = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][1]);
-        const i32x8 ka = {(int)x[0], (int)x[1], (int)x[2], (int)x[3],
-                          (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qhi[s], sc[kb], 0, 0, 0, ks[kb], 0,
-                                                                 qscale_hi);
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qlo[s], sc[kb], 0, 0, 0, ks[kb], 0,
-                                                                 qscale_lo);
+        ka[kb] = i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3],
+                       (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[kb], qhi[s], sc[kb], 0, 0, 0, ks[kb],
+                                                                 0, qscale_hi);
       }
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[kb], qlo[s], sc[kb], 0, 0, 0, ks[kb],
+                                                                 0, qscale_lo);
+    }
   };
   auto cap = [&](f32x16 *sc) {
     if constexpr (CAP) {
@@ -364,7 +380,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     }
     for (int it = 0; it < n_tiles; ++it) {
       wait_vm<0>();
-      store_v(it, cd, sn.v);
+      store_v(it & 1, cd, sn.v);
       int ks[2];
       operands(sn, ks);
       if (it + 1 < n_tiles && full(it + 1)) {
@@ -482,7 +498,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
       if (t + 2 < n_tiles && full(t + 2)) v_pages(t + 2, pn);
       // K[t + 2] and the codes of V[t + 1], asked for above, have had the iteration to arrive
       wait_vm<0>();
-      if (t + 1 < n_tiles) store_v(t + 1, cd, vs);
+      if (t + 1 < n_tiles) store_v(P ^ 1, cd, vs);
       operands(sn, ks);
       vs = sn.v;
       tile_barrier();
