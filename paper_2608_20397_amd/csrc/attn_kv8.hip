@@ -248,28 +248,40 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     vdst[k][0] = row * VROWB + 16 * vchunk(c, row);
     vdst[k][1] = row * VROWB + 16 * vchunk(c + 1, row);
   }
-  auto store_v = [&](int buf, Codes &cd, uint32_t vs) {
-    char *vl = vbuf(buf);
+  struct RowScales {
     uint32_t byte[NVC];
+  };
+  auto row_scales = [&](uint32_t vs, RowScales &rs) {
 #pragma unroll
-    for (int k = 0; k < NVC; ++k) byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(vrow[k], (int)vs);
+    for (int k = 0; k < NVC; ++k) rs.byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(vrow[k], (int)vs);
+  };
+  auto clear_bad = [&](Codes &cd, uint32_t vs, RowScales &rs) {
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(vs == kBadScale) != 0, 0)) {
 #pragma unroll
       for (int k = 0; k < NVC; ++k)
-        if (byte[k] == kBadScale) {
+        if (rs.byte[k] == kBadScale) {
           cd.v[k] = u32x4{0u, 0u, 0u, 0u};
-          byte[k] = 127;
+          rs.byte[k] = 127;
         }
     }
+  };
+  auto store_v = [&](int buf, const Codes &cd, const RowScales &rs) {
+    char *vl = vbuf(buf);
 #pragma unroll
     for (int k = 0; k < NVC; ++k) {
-      const float s = __uint_as_float(byte[k] << 23);
+      const float s = __uint_as_float(rs.byte[k] << 23);
       u32x2 w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = codes_to_bf16(cd.v[k][i], s);
       *reinterpret_cast<u32x4 *>(vl + vdst[k][0]) = u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
       *reinterpret_cast<u32x4 *>(vl + vdst[k][1]) = u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
     }
+  };
+  auto convert_v = [&](int buf, Codes &cd, uint32_t vs) {
+    RowScales rs;
+    row_scales(vs, rs);
+    clear_bad(cd, vs, rs);
+    store_v(buf, cd, rs);
   };
 
   const float c_scale = CAP ? 1.0f : a.scale_log2;
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     }
     for (int it = 0; it < n_tiles; ++it) {
       wait_vm<0>();
-      store_v(it & 1, cd, sn.v);
+      convert_v(it & 1, cd, sn.v);
       int ks[2];
       operands(sn, ks);
       if (it + 1 < n_tiles && full(it + 1)) {
@@ -407,29 +419,32 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   } else {
     // ---- the schedule of attn_bf16_dma.hip: per iteration t the wave computes S(t + 1) = K[t + 1] Q^T
     // beside the exponentials of S(t), then O += V[t] P(t) beside the maximum of S(t + 1), while K[t + 2]
-    // travels by DMA and the codes of V[t + 1] to registers, from which they go to LDS as bf16 at the end
+    // travels by DMA.  The codes of V[t + 1], in registers since the iteration before, go to LDS as bf16
+    // beside the PV products, which leave the vector units idle half their time (at the end of the
+    // iteration, before its barrier, the conversion took 14% of the launch).
     f32x16 sa[NKB], sb[NKB];
     int ks[2] = {127, 127};                 // scale operands of tile t + 1's keys
     uint32_t vs = 127;                      // value scale of its token `lane`
-    if (n_tiles > 0) {
-      if (full(0)) {
-        k_pages(0, pn);
-        v_pages(0, pn);
+    // what is asked for at the end of an iteration: codes of V[t], scales of tile s
+    auto ask = [&](int t, int s) {
+      if (t < n_tiles) {
+        if (full(t)) v_pages(t, pn);
+        load_v(t, pn, cd);
       }
-      load_v(0, pn, cd);
-      load_scales(0, sn);
+      if (s < n_tiles) load_scales(s, sn);
+    };
+    if (n_tiles > 0) {
+      if (full(0)) k_pages(0, pn);
+      ask(0, 0);
       dma_k(0, pn);
       wait_vm<0>();
-      store_v(0, cd, sn.v);
+      convert_v(0, cd, sn.v);
       operands(sn, ks);
       if (n_tiles > 1) {
-        if (full(1)) {
-          k_pages(1, pn);
-          v_pages(1, pn);
-        }
-        load_scales(1, sn);
+        if (full(1)) k_pages(1, pn);
         dma_k(1, pn);
       }
+      ask(1, 1);
     }
     tile_barrier();
     float mt_cur = -INFINITY;               // row maximum of S(t), log2 units
@@ -441,66 +456,122 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     wait_vm<0>();
     operands(sn, ks);
     vs = sn.v;
-    if (n_tiles > 2 && full(2)) k_pages(2, pn);
+    if (n_tiles > 2) {
+      load_scales(2, sn);
+      if (full(2)) k_pages(2, pn);
+    }
     tile_barrier();                         // K buffer 0 is refilled in iteration 0; K[1] has landed
 
     auto step = [&](int t, auto parity, f32x16 *s_cur, f32x16 *s_nxt) {
       constexpr int P = decltype(parity)::value;     // t & 1
-      if (t + 1 < n_tiles) load_v(t + 1, pn, cd);
-      if (t + 2 < n_tiles) {
-        load_scales(t + 2, sn);
-        dma_k(t + 2, pn);
-      }
+      if (t + 2 < n_tiles) dma_k(t + 2, pn);
+      RowScales rs;
+      row_scales(vs, rs);
+      clear_bad(cd, vs, rs);
       if (active) {
         if (needs_mask(t)) {
           mask(s_cur, t);
           mt_cur = row_max(s_cur);
         }
         const float nm = rescale(mt_cur);
-        const char *vl = vbuf(P);
-        bf16x8 pb[4];
-        qk(kbuf(P ^ 1), ks, s_nxt);
-        pb[0] = softmax_half(s_cur[0], 0, nm);
-        pb[1] = softmax_half(s_cur[0], 1, nm);
-        pb[2] = softmax_half(s_cur[1], 0, nm);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        const char *kl = kbuf(P ^ 1), *vl = vbuf(P);
+        // Both phases are chunks of one MFMA, the operand reads of a later one and a few vector
+        // instructions, in the order written here (the sched_barriers hold it).
+        // P(t), two scores of this lane at a time: pair i of 16, keys of 4 pairs per PV step
+        uint32_t pw[8 * NKB];
+        auto p_pair = [&](int i) {
+          const float p0 = fast_exp2(fmaf(s_cur[i >> 3][2 * (i & 7)], c_scale, nm));
+          const float p1 = fast_exp2(fmaf(s_cur[i >> 3][2 * (i & 7) + 1], c_scale, nm));
+          pw[i] = pack_bf16x2(p0, p1);
+          l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[i]), ones, l, false);
+        };
+        // ---- S(t + 1), beside the first 12 pairs
+        constexpr int NQ = NS2 * NKB;         // K operands: block q % NKB, features 64 (q / NKB) ..
+        auto k_operand = [&](int q) {
+          const char *at = kl + (q % NKB) * 32 * D;
+          const u32x4 x = *reinterpret_cast<const u32x4 *>(at + offk[q / NKB][0]);
+          const u32x4 y = *reinterpret_cast<const u32x4 *>(at + offk[q / NKB][1]);
+          return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        };
+        i32x8 ka[2];
+        ka[0] = k_operand(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2 * NKB * NS2; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 20 : 10, 0);
+        for (int q = 0; q < NQ; ++q) {
+          const int kb = q % NKB, s = q / NKB;
+          if (q + 1 < NQ) ka[(q + 1) & 1] = k_operand(q + 1);
+          if (q < NKB) {
+            f32x16 zero;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+            s_nxt[kb] = zero;
+          }
+          s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[q & 1], qhi[s], s_nxt[kb], 0, 0, 0,
+                                                                      ks[kb], 0, qscale_hi);
+#pragma unroll
+          for (int i = 24 * q / (2 * NQ); i < 12 * (2 * q + 1) / (2 * NQ); ++i) p_pair(i);
+          __builtin_amdgcn_sched_barrier(0);
+          s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[q & 1], qlo[s], s_nxt[kb], 0, 0, 0,
+                                                                      ks[kb], 0, qscale_lo);
+#pragma unroll
+          for (int i = 12 * (2 * q + 1) / (2 * NQ); i < 12 * (2 * q + 2) / (2 * NQ); ++i) p_pair(i);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        // ---- O += V P, beside the last 4 pairs, the conversion of V[t + 1] (past the last tile: to a
+        // buffer that nothing reads any more) and the cap and maximum of S(t + 1)
         __builtin_amdgcn_s_setprio(kPrioPV);
-        pv_step(vl, 0, pb[0]);
-        pv_step(vl, 1, pb[1]);
-        pv_step(vl, 2, pb[2]);
-        pb[3] = softmax_half(s_cur[1], 1, nm);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+        constexpr int NM = 4 * NDB;           // MFMA m: step m / NDB, features 32 (m % NDB) ..
+        auto v_operand = [&](int m) {
+          const char *at = vl + (m / NDB) * 16 * VROWB + offv[m % NDB];
+          return tr_read_pair(at, at + 8 * VROWB);
+        };
+        bf16x8 va[3];
+        va[0] = v_operand(0);
+        va[1] = v_operand(1);
+        u32x2 cw[4];
+        float mt = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 3 * NDB; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 4 : 2, 1);
-        }
-        pv_step(vl, 3, pb[3]);
-        cap(s_nxt);
-        mt_cur = row_max(s_nxt);
+        for (int m = 0; m < NM; ++m) {
+          const int step_m = m / NDB, db = m % NDB;
+          if (m + 2 < NM) va[(m + 2) % 3] = v_operand(m + 2);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              va[m % 3],
+              __builtin_bit_cast(bf16x8, u32x4{pw[4 * step_m], pw[4 * step_m + 1], pw[4 * step_m + 2],
+                                               pw[4 * step_m + 3]}),
+              o[db], 0, 0, 0);
+          // the pairs before the step that takes them, a word of codes in two of three chunks
 #pragma unroll
-        for (int i = 0; i < NDB; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 2);
-          __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 12 : 6, 2);
+          for (int i = 4 * m / (3 * NDB); i < 4 * (m + 1) / (3 * NDB) && i < 4; ++i) p_pair(12 + i);
+#pragma unroll
+          for (int w = 4 * NVC * m / NM; w < 4 * NVC * (m + 1) / NM; ++w) {
+            const int k = w >> 2, i = w & 3;
+            cw[i] = codes_to_bf16(cd.v[k][i], __uint_as_float(rs.byte[k] << 23));
+            if (i & 1)
+              *reinterpret_cast<u32x4 *>(vbuf(P ^ 1) + vdst[k][i >> 1]) =
+                  u32x4{cw[i - 1][0], cw[i - 1][1], cw[i][0], cw[i][1]};
+          }
+          // (the last products of S(t + 1) are still on their way in the first chunks)
+          constexpr int M0 = NM / 4;
+#pragma unroll
+          for (int i = m < M0 ? 0 : 16 * NKB * (m - M0) / (NM - M0);
+               i < (m < M0 ? 0 : 16 * NKB * (m - M0 + 1) / (NM - M0)); ++i) {
+            if constexpr (CAP)
+              s_nxt[i >> 4][i & 15] = a.cap_out * tanh_fast(s_nxt[i >> 4][i & 15] * a.cap_in);
+            mt = fmaxf(mt, s_nxt[i >> 4][i & 15]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
+        mt_cur = max_halves(mt) * c_scale;
+      } else {
+        store_v(P ^ 1, cd, rs);
       }
       __builtin_amdgcn_s_setprio(0);
-      // pages of the next iteration's loads (their LDS reads overlap the wait)
       if (t + 3 < n_tiles && full(t + 3)) k_pages(t + 3, pn);
-      if (t + 2 < n_tiles && full(t + 2)) v_pages(t + 2, pn);
-      // K[t + 2] and the codes of V[t + 1], asked for above, have had the iteration to arrive
+      // K[t + 2] and the scales of tile t + 2 have had the iteration to arrive
       wait_vm<0>();
-      if (t + 1 < n_tiles) store_v(P ^ 1, cd, vs);
       operands(sn, ks);
       vs = sn.v;
+      ask(t + 2, t + 3);
       tile_barrier();
     };
     // Every iteration computes S(t + 1), on the last tile from a stale buffer, never used (a branch there
