@@ -75,7 +75,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
 
   // ---- the query as two E4M3 terms: lane (hh, j) holds features 64 s + 32 hh .. + 31 of query q0 + j
   i32x8 qhi[NS2], qlo[NS2];
-  int qscale_hi = 127, qscale_lo = 127;
+  int qscale;              // scale bytes of hi (byte 0) and lo (byte 1)
   {
     const int qi = min(q0 + j, sp.len - 1);
     const uint16_t *qrow = a.q + ((int64_t)(sp.q_start + qi) * a.n_q_heads + qhead) * D;
@@ -95,8 +95,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     am = max((uint32_t)r[0], (uint32_t)r[1]);
     const bool bad = am >= 0x7F800000u;
     const int e = row_exp(am);
-    qscale_hi = e + 127;
-    qscale_lo = e + 127 - 4;
+    qscale = (e + 127) | (e + 127 - 4) << 8;
 #pragma unroll
     for (int s = 0; s < NS2; ++s)
 #pragma unroll
@@ -183,9 +182,9 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     const int row = (wave * NI + i) * RPI + lane / CH;
     kdo[i] = (row & (kPage - 1)) * D + 16 * ((lane % CH) ^ kswz(row));
   }
-  auto dma_k = [&](int it, const Pages &p) {
+  auto dma_k = [&](int it, const Pages &p, bool whole = false) {
     const uint32_t dst = smem_base + (it & 1) * KTILEB + wave * NI * 1024;
-    if (full(it)) {
+    if (whole || full(it)) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) dma_s<0>(dst + i * 1024, kbytes + p.k[i] * pbytes, kdo[i]);
     } else {
@@ -204,8 +203,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     u32x4 v[NVC];
   };
   const uint32_t vdo = ((64 * wave / CH + lane / CH) & (kPage - 1)) * D + 16 * (lane % CH);
-  auto load_v = [&](int it, const Pages &p, Codes &cd) {
-    if (full(it)) {
+  auto load_v = [&](int it, const Pages &p, Codes &cd, bool whole = false) {
+    if (whole || full(it)) {
 #pragma unroll
       for (int k = 0; k < NVC; ++k)
         cd.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + p.v[k] * pbytes + vdo);
@@ -232,28 +231,24 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     s.v = vsb[at];
   };
   // the MFMA's scale operands of a tile's keys
-  auto operands = [&](const Scales &s, int (&ks)[2]) {
+  auto operands = [&](const Scales &s) -> int {      // of block kb in byte kb
     const uint32_t k = s.v == kBadScale ? kBadScale : s.k;
     const auto r = __builtin_amdgcn_permlane32_swap(k, k, false, false);
-    ks[0] = (int)r[0];
-    ks[1] = (int)r[1];
+    return (int)(r[0] | r[1] << 8);
   };
   // V codes of a tile to bf16 in V buffer `buf`, `vs`: the value scale byte of token `lane`; a row that is
   // not finite as zeros
-  uint32_t vrow[NVC], vdst[NVC][2];
-#pragma unroll
-  for (int k = 0; k < NVC; ++k) {
-    const int row = (64 * wave + NT * k) / CH + lane / CH, c = 2 * (lane % CH);
-    vrow[k] = 4 * row;
-    vdst[k][0] = row * VROWB + 16 * vchunk(c, row);
-    vdst[k][1] = row * VROWB + 16 * vchunk(c + 1, row);
-  }
+  // (the rows of a thread's chunks are 32 or 64 apart and swizzled alike)
+  const uint32_t vrow = 64 * wave / CH + lane / CH;
+  const uint32_t vdst[2] = {vrow * VROWB + 16 * vchunk(2 * (lane % CH), vrow),
+                            vrow * VROWB + 16 * vchunk(2 * (lane % CH) + 1, vrow)};
   struct RowScales {
     uint32_t byte[NVC];
   };
   auto row_scales = [&](uint32_t vs, RowScales &rs) {
 #pragma unroll
-    for (int k = 0; k < NVC; ++k) rs.byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(vrow[k], (int)vs);
+    for (int k = 0; k < NVC; ++k) 
+      rs.byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (vrow + NT / CH * k), (int)vs);
   };
   auto clear_bad = [&](Codes &cd, uint32_t vs, RowScales &rs) {
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(vs == kBadScale) != 0, 0)) {
@@ -273,8 +268,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
       u32x2 w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = codes_to_bf16(cd.v[k][i], s);
-      *reinterpret_cast<u32x4 *>(vl + vdst[k][0]) = u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
-      *reinterpret_cast<u32x4 *>(vl + vdst[k][1]) = u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
+      *reinterpret_cast<u32x4 *>(vl + NT / CH * VROWB * k + vdst[0]) = u32x4{w[0][0], w[0][1], w[1][0], w[1][1]};
+      *reinterpret_cast<u32x4 *>(vl + NT / CH * VROWB * k + vdst[1]) = u32x4{w[2][0], w[2][1], w[3][0], w[3][1]};
     }
   };
   auto convert_v = [&](int buf, Codes &cd, uint32_t vs) {
@@ -287,8 +282,18 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   const float c_scale = CAP ? 1.0f : a.scale_log2;
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
 
+  // one product of 64 features: keys of block kb, whose scales are byte kb of ks, with hi (0) or lo (1)
+  auto mfma8 = [&](const i32x8 &ka, const i32x8 &q, const f32x16 &c, int ks, int kb, int term) {
+    // (the selectors are part of the instruction)
+    if (kb == 0 && term == 0)
+      return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 0, ks, 0, qscale);
+    if (kb == 0) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 0, ks, 1, qscale);
+    if (term == 0)
+      return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 1, ks, 0, qscale);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 1, ks, 1, qscale);
+  };
   // S^T of the tile in K buffer `kl`, whose tokens' scale bytes are the operands ks (raw scores)
-  auto qk = [&](const char *kl, const int (&ks)[2], f32x16 *sc) {
+  auto qk = [&](const char *kl, int ks, f32x16 *sc) {
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -303,13 +308,11 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         const u32x4 y = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][1]);
         ka[kb] = i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3],
                        (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[kb], qhi[s], sc[kb], 0, 0, 0, ks[kb],
-                                                                 0, qscale_hi);
+        sc[kb] = mfma8(ka[kb], qhi[s], sc[kb], ks, kb, 0);
       }
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
-        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[kb], qlo[s], sc[kb], 0, 0, 0, ks[kb],
-                                                                 0, qscale_lo);
+        sc[kb] = mfma8(ka[kb], qlo[s], sc[kb], ks, kb, 1);
     }
   };
   auto cap = [&](f32x16 *sc) {
@@ -393,8 +396,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     for (int it = 0; it < n_tiles; ++it) {
       wait_vm<0>();
       convert_v(it & 1, cd, sn.v);
-      int ks[2];
-      operands(sn, ks);
+      const int ks = operands(sn);
       if (it + 1 < n_tiles && full(it + 1)) {
         k_pages(it + 1, pn);
         v_pages(it + 1, pn);
@@ -423,28 +425,28 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     // beside the PV products, which leave the vector units idle half their time (at the end of the
     // iteration, before its barrier, the conversion took 14% of the launch).
     f32x16 sa[NKB], sb[NKB];
-    int ks[2] = {127, 127};                 // scale operands of tile t + 1's keys
+    int ks = 0;                             // scale operands of tile t + 1's keys
     uint32_t vs = 127;                      // value scale of its token `lane`
     // what is asked for at the end of an iteration: codes of V[t], scales of tile s
-    auto ask = [&](int t, int s) {
-      if (t < n_tiles) {
-        if (full(t)) v_pages(t, pn);
-        load_v(t, pn, cd);
+    auto ask = [&](int t, int s, bool inner) {
+      if (inner || t < n_tiles) {
+        if (inner || full(t)) v_pages(t, pn);
+        load_v(t, pn, cd, inner);
       }
-      if (s < n_tiles) load_scales(s, sn);
+      if (inner || s < n_tiles) load_scales(s, sn);
     };
     if (n_tiles > 0) {
       if (full(0)) k_pages(0, pn);
-      ask(0, 0);
+      ask(0, 0, false);
       dma_k(0, pn);
       wait_vm<0>();
       convert_v(0, cd, sn.v);
-      operands(sn, ks);
+      ks = operands(sn);
       if (n_tiles > 1) {
         if (full(1)) k_pages(1, pn);
         dma_k(1, pn);
       }
-      ask(1, 1);
+      ask(1, 1, false);
     }
     tile_barrier();
     float mt_cur = -INFINITY;               // row maximum of S(t), log2 units
@@ -454,7 +456,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
       mt_cur = row_max(sa);                 // unmasked: step 0 masks S(0) and takes its maximum again
     }
     wait_vm<0>();
-    operands(sn, ks);
+    ks = operands(sn);
     vs = sn.v;
     if (n_tiles > 2) {
       load_scales(2, sn);
@@ -462,14 +464,17 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     }
     tile_barrier();                         // K buffer 0 is refilled in iteration 0; K[1] has landed
 
-    auto step = [&](int t, auto parity, f32x16 *s_cur, f32x16 *s_nxt) {
+    // INNER: the wave has a task, tile t needs no mask and tiles to t + 3 are whole: no branches but the
+    // rescale's and the one for tokens that are not finite
+    auto step = [&](int t, auto parity, auto inner, f32x16 *s_cur, f32x16 *s_nxt) {
       constexpr int P = decltype(parity)::value;     // t & 1
-      if (t + 2 < n_tiles) dma_k(t + 2, pn);
+      constexpr bool INNER = decltype(inner)::value;
+      if (INNER || t + 2 < n_tiles) dma_k(t + 2, pn, INNER);
       RowScales rs;
       row_scales(vs, rs);
       clear_bad(cd, vs, rs);
-      if (active) {
-        if (needs_mask(t)) {
+      if (INNER || active) {
+        if (!INNER && needs_mask(t)) {
           mask(s_cur, t);
           mt_cur = row_max(s_cur);
         }
@@ -506,13 +511,11 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
             for (int v = 0; v < 16; ++v) zero[v] = 0.f;
             s_nxt[kb] = zero;
           }
-          s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[q & 1], qhi[s], s_nxt[kb], 0, 0, 0,
-                                                                      ks[kb], 0, qscale_hi);
+          s_nxt[kb] = mfma8(ka[q & 1], qhi[s], s_nxt[kb], ks, kb, 0);
 #pragma unroll
           for (int i = 24 * q / (2 * NQ); i < 12 * (2 * q + 1) / (2 * NQ); ++i) p_pair(i);
           __builtin_amdgcn_sched_barrier(0);
-          s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka[q & 1], qlo[s], s_nxt[kb], 0, 0, 0,
-                                                                      ks[kb], 0, qscale_lo);
+          s_nxt[kb] = mfma8(ka[q & 1], qlo[s], s_nxt[kb], ks, kb, 1);
 #pragma unroll
           for (int i = 12 * (2 * q + 1) / (2 * NQ); i < 12 * (2 * q + 2) / (2 * NQ); ++i) p_pair(i);
           __builtin_amdgcn_sched_barrier(0);
@@ -547,7 +550,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
             const int k = w >> 2, i = w & 3;
             cw[i] = codes_to_bf16(cd.v[k][i], __uint_as_float(rs.byte[k] << 23));
             if (i & 1)
-              *reinterpret_cast<u32x4 *>(vbuf(P ^ 1) + vdst[k][i >> 1]) =
+              *reinterpret_cast<u32x4 *>(vbuf(P ^ 1) + NT / CH * VROWB * k + vdst[i >> 1]) =
                   u32x4{cw[i - 1][0], cw[i - 1][1], cw[i][0], cw[i][1]};
           }
           // (the last products of S(t + 1) are still on their way in the first chunks)
@@ -566,19 +569,28 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         store_v(P ^ 1, cd, rs);
       }
       __builtin_amdgcn_s_setprio(0);
-      if (t + 3 < n_tiles && full(t + 3)) k_pages(t + 3, pn);
+      if (INNER || (t + 3 < n_tiles && full(t + 3))) k_pages(t + 3, pn);
       // K[t + 2] and the scales of tile t + 2 have had the iteration to arrive
       wait_vm<0>();
-      operands(sn, ks);
+      ks = operands(sn);
       vs = sn.v;
-      ask(t + 2, t + 3);
+      ask(t + 2, t + 3, INNER);
       tile_barrier();
     };
     // Every iteration computes S(t + 1), on the last tile from a stale buffer, never used (a branch there
     // would split the scheduled region).
-    for (int t = 0; t < n_tiles; t += 2) {
-      step(t, std::integral_constant<int, 0>{}, sa, sb);
-      if (t + 1 < n_tiles) step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
+    const int n_inner =
+        active ? min((k_end - k_begin) / KT - 3, (qpos0 + 1 - k_begin) / KT) : 0;
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int t = 0;
+    for (; t + 1 < n_inner; t += 2) {
+      step(t, even, std::true_type{}, sa, sb);
+      step(t + 1, odd, std::true_type{}, sb, sa);
+    }
+    for (; t < n_tiles; t += 2) {
+      step(t, even, std::false_type{}, sa, sb);
+      if (t + 1 < n_tiles) step(t + 1, odd, std::false_type{}, sb, sa);
     }
   }
 
