@@ -41,7 +41,10 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   constexpr float kSlack = 8.0f;                   // lazy rescale: p <= 2^8 between rescales
   constexpr int kPrioPV = 2;                       // wave priority of the PV phase (attn_bf16_dma.hip)
   static_assert(NI >= 1 && NVC >= 1 && RPI <= kPage, "tile shape");
-  __shared__ __align__(1024) char smem[2 * KTILEB + 2 * VTILEB];
+  // head_dim 256: O^T takes 128 of a wave's 256 registers and Q's upper terms 32; the lower terms wait in LDS
+  constexpr bool QLDS = D == 256;
+  constexpr int QLB = QLDS ? 64 * 32 * NS2 : 0;    // bytes of a wave's lower terms
+  __shared__ __align__(1024) char smem[2 * KTILEB + 2 * VTILEB + W * QLB];
   __shared__ __align__(16) int32_t pg[kMaxSplitKeys / kPage + 8];
 
   const int tid = threadIdx.x;
@@ -74,7 +77,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   for (int i = tid; i < n_pg; i += NT) pg[i] = a.map[pg0 + i];
 
   // ---- the query as two E4M3 terms: lane (hh, j) holds features 64 s + 32 hh .. + 31 of query q0 + j
-  i32x8 qhi[NS2], qlo[NS2];
+  i32x8 qhi[NS2], qlo[QLDS ? 1 : NS2];
+  char *const ql_lds = smem + 2 * KTILEB + 2 * VTILEB + wave * QLB + 16 * lane;   // 16-byte piece i at + 1024 i
   int qscale;              // scale bytes of hi (byte 0) and lo (byte 1)
   {
     const int qi = min(q0 + j, sp.len - 1);
@@ -110,8 +114,12 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         split_query<8>(x, e, bad, hi, lo);
         qhi[s][2 * c] = hi[0];
         qhi[s][2 * c + 1] = hi[1];
-        qlo[s][2 * c] = lo[0];
-        qlo[s][2 * c + 1] = lo[1];
+        if constexpr (QLDS) {
+          *reinterpret_cast<u32x2 *>(ql_lds + 1024 * (2 * s + (c >> 1)) + 8 * (c & 1)) = u32x2{lo[0], lo[1]};
+        } else {
+          qlo[s][2 * c] = lo[0];
+          qlo[s][2 * c + 1] = lo[1];
+        }
       }
   }
 
@@ -132,18 +140,18 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
            : D == 128 ? c ^ (4 * (r & 3)) ^ ((r ^ (c >> 3)) & 1)
                       : c ^ (4 * (r & 3)) ^ (((c >> 3) ^ (c >> 4)) & 1);
   };
-  // S^T A operand: K row j (+ 32 kb, whose swizzle is the same), features 64 s + 32 hh .. + 31
-  uint32_t offk[NS2][2];
-#pragma unroll
-  for (int s = 0; s < NS2; ++s)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) offk[s][c] = j * D + 16 * ((4 * s + 2 * hh + c) ^ kswz(j));
-  uint32_t offv[NDB];                          // PV A operand, as attn_bf16_dma.hip
+  // S^T A operand: K row j (+ 32 kb, whose swizzle is the same), features 64 s + 32 hh .. + 31,
+  // in chunks 4 s + 2 hh + c: the XOR of one offset with constants (few registers hold offsets in the loop)
+  const uint32_t offk = j * D + 16 * ((2 * hh) ^ kswz(j));
+  // PV A operand, as attn_bf16_dma.hip: key 4 h2 + e of a half step, features 32 db + 16 dh + 4 q .. + 3;
+  // head_dim 256: db and db + 4 differ by a constant XOR
+  constexpr int NOV = NDB < 4 ? NDB : 4;
+  uint32_t offv[NOV];
   {
     const int gg = lane >> 4, r = lane & 15, e = r >> 2, q = r & 3;
     const int h2 = gg >> 1, dh = gg & 1;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+    for (int db = 0; db < NOV; ++db)
       offv[db] = (4 * h2 + e) * VROWB + 16 * vchunk(4 * db + 2 * dh + (q >> 1), e) + 8 * (q & 1);
   }
   auto kbuf = [&](int i) { return smem + i * KTILEB; };
@@ -292,27 +300,34 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
       return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 1, ks, 0, qscale);
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, q, c, 0, 0, 1, ks, 1, qscale);
   };
+  auto two = [](const u32x4 &x, const u32x4 &y) {
+    return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+  };
+  // K operand q of a tile: block q % NKB, features 64 (q / NKB) ..; and the lower terms of those features
+  constexpr int NQ = NS2 * NKB;
+  auto k_operand = [&](const char *kl, uint32_t z, int q) {
+    const char *at = kl + (q % NKB) * 32 * D;
+    return two(*reinterpret_cast<const u32x4 *>(at + (offk ^ (64 * (q / NKB) + z))),
+               *reinterpret_cast<const u32x4 *>(at + (offk ^ (64 * (q / NKB) + 16 + z))));
+  };
+  auto low = [&](int s) {
+    if constexpr (QLDS)
+      return two(*reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s),
+                 *reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s + 1024));
+    else
+      return qlo[s];
+  };
+  f32x16 zero;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) zero[v] = 0.f;
   // S^T of the tile in K buffer `kl`, whose tokens' scale bytes are the operands ks (raw scores)
   auto qk = [&](const char *kl, int ks, f32x16 *sc) {
 #pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
-    // (the terms of one score block stand apart: a product waits for the one before it on its accumulators)
-#pragma unroll
-    for (int s = 0; s < NS2; ++s) {
-      i32x8 ka[NKB];
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][0]);
-        const u32x4 y = *reinterpret_cast<const u32x4 *>(kl + kb * 32 * D + offk[s][1]);
-        ka[kb] = i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3],
-                       (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        sc[kb] = mfma8(ka[kb], qhi[s], sc[kb], ks, kb, 0);
-      }
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-        sc[kb] = mfma8(ka[kb], qlo[s], sc[kb], ks, kb, 1);
+    for (int q = 0; q < NQ; ++q) {
+      const int kb = q % NKB, s = q / NKB;
+      const i32x8 ka = k_operand(kl, 0, q);
+      sc[kb] = mfma8(ka, qhi[s], q < NKB ? zero : sc[kb], ks, kb, 0);
+      sc[kb] = mfma8(ka, low(s), sc[kb], ks, kb, 1);
     }
   };
   auto cap = [&](f32x16 *sc) {
@@ -358,67 +373,10 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     }
     return (m_ref == -INFINITY) ? 0.f : -m_ref;
   };
-  // P of 16 keys (half hf of a score block) as a PV operand; adds their sum to l
-  auto softmax_half = [&](const f32x16 &sc, int hf, float nm) -> bf16x8 {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float p0 = fast_exp2(fmaf(sc[8 * hf + 2 * e], c_scale, nm));
-      const float p1 = fast_exp2(fmaf(sc[8 * hf + 2 * e + 1], c_scale, nm));
-      w[e] = pack_bf16x2(p0, p1);
-      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), ones, l, false);
-    }
-    return __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-  };
-  // O^T += V^T P^T over the 16 keys of step ks of the V tile at vl
-  auto pv_step = [&](const char *vl, int ks, const bf16x8 &pb) {
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      const char *p = vl + ks * 16 * VROWB + offv[db];
-      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_read_pair(p, p + 8 * VROWB), pb, o[db], 0, 0, 0);
-    }
-  };
-
   Codes cd{};
   Scales sn{};                               // scales of the tile that loads
   Pages pn{};                                // pages of the tiles to load next
-  if constexpr (D == 256) {
-    // ---- a tile at a time: K by DMA and V codes in registers while the one before is computed
-    if (n_tiles > 0) {
-      if (full(0)) {
-        k_pages(0, pn);
-        v_pages(0, pn);
-      }
-      load_v(0, pn, cd);
-      load_scales(0, sn);
-      dma_k(0, pn);
-    }
-    for (int it = 0; it < n_tiles; ++it) {
-      wait_vm<0>();
-      convert_v(it & 1, cd, sn.v);
-      const int ks = operands(sn);
-      if (it + 1 < n_tiles && full(it + 1)) {
-        k_pages(it + 1, pn);
-        v_pages(it + 1, pn);
-      }
-      tile_barrier();   // K and V of tile `it` are in LDS; the other buffers are free
-      if (it + 1 < n_tiles) {
-        load_v(it + 1, pn, cd);
-        load_scales(it + 1, sn);
-        dma_k(it + 1, pn);
-      }
-      if (!active) continue;
-      f32x16 sc[NKB];
-      qk(kbuf(it & 1), ks, sc);
-      cap(sc);
-      if (needs_mask(it)) mask(sc, it);
-      const float nm = rescale(row_max(sc));
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) pv_step(vbuf(it & 1), 2 * kb + hf, softmax_half(sc[kb], hf, nm));
-    }
-  } else {
+  {
     // ---- the schedule of attn_bf16_dma.hip: per iteration t the wave computes S(t + 1) = K[t + 1] Q^T
     // beside the exponentials of S(t), then O += V[t] P(t) beside the maximum of S(t + 1), while K[t + 2]
     // travels by DMA.  The codes of V[t + 1], in registers since the iteration before, go to LDS as bf16
@@ -482,7 +440,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         const char *kl = kbuf(P ^ 1), *vl = vbuf(P);
         // Both phases are chunks of one MFMA, the operand reads of a later one and a few vector
         // instructions, in the order written here (the sched_barriers hold it).
-        // P(t), two scores of this lane at a time: pair i of 16, keys of 4 pairs per PV step
+        // P(t), two scores of this lane at a time: pair i of 8 NKB, keys of 4 pairs per PV step
         uint32_t pw[8 * NKB];
         auto p_pair = [&](int i) {
           const float p0 = fast_exp2(fmaf(s_cur[i >> 3][2 * (i & 7)], c_scale, nm));
@@ -490,61 +448,57 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
           pw[i] = pack_bf16x2(p0, p1);
           l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[i]), ones, l, false);
         };
-        // ---- S(t + 1), beside the first 12 pairs
-        constexpr int NQ = NS2 * NKB;         // K operands: block q % NKB, features 64 (q / NKB) ..
-        auto k_operand = [&](int q) {
-          const char *at = kl + (q % NKB) * 32 * D;
-          const u32x4 x = *reinterpret_cast<const u32x4 *>(at + offk[q / NKB][0]);
-          const u32x4 y = *reinterpret_cast<const u32x4 *>(at + offk[q / NKB][1]);
-          return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        };
-        i32x8 ka[2];
-        ka[0] = k_operand(0);
+        // ---- S(t + 1), beside the pairs of all PV steps but the last
+        constexpr int NP = 8 * NKB, NPQ = NP - 4;   // pairs, and those here
+        i32x8 ka[2], ql;
+        // a zero that the compiler takes for anything: without it, the XORs of the operand offsets would be kept
+        // in registers across the loop
+        uint32_t z;
+        asm volatile("s_mov_b32 %0, 0" : "=s"(z));
+        ka[0] = k_operand(kl, z, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          const int kb = q % NKB, s = q / NKB;
-          if (q + 1 < NQ) ka[(q + 1) & 1] = k_operand(q + 1);
-          if (q < NKB) {
-            f32x16 zero;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) zero[v] = 0.f;
-            s_nxt[kb] = zero;
+        for (int c = 0; c < 2 * NQ; ++c) {
+          const int q = c >> 1, kb = q % NKB, s = q / NKB;
+          if (c & 1) {
+            s_nxt[kb] = mfma8(ka[q & 1], ql, s_nxt[kb], ks, kb, 1);
+          } else {
+            ql = low(s);
+            if (q + 1 < NQ) ka[(q + 1) & 1] = k_operand(kl, z, q + 1);
+            s_nxt[kb] = mfma8(ka[q & 1], qhi[s], q < NKB ? zero : s_nxt[kb], ks, kb, 0);
           }
-          s_nxt[kb] = mfma8(ka[q & 1], qhi[s], s_nxt[kb], ks, kb, 0);
 #pragma unroll
-          for (int i = 24 * q / (2 * NQ); i < 12 * (2 * q + 1) / (2 * NQ); ++i) p_pair(i);
-          __builtin_amdgcn_sched_barrier(0);
-          s_nxt[kb] = mfma8(ka[q & 1], qlo[s], s_nxt[kb], ks, kb, 1);
-#pragma unroll
-          for (int i = 12 * (2 * q + 1) / (2 * NQ); i < 12 * (2 * q + 2) / (2 * NQ); ++i) p_pair(i);
+          for (int i = NPQ * c / (2 * NQ); i < NPQ * (c + 1) / (2 * NQ); ++i) p_pair(i);
           __builtin_amdgcn_sched_barrier(0);
         }
         // ---- O += V P, beside the last 4 pairs, the conversion of V[t + 1] (past the last tile: to a
         // buffer that nothing reads any more) and the cap and maximum of S(t + 1)
         __builtin_amdgcn_s_setprio(kPrioPV);
-        constexpr int NM = 4 * NDB;           // MFMA m: step m / NDB, features 32 (m % NDB) ..
+        constexpr int NM = 2 * NKB * NDB;     // MFMA m: step m / NDB, features 32 (m % NDB) ..
         auto v_operand = [&](int m) {
-          const char *at = vl + (m / NDB) * 16 * VROWB + offv[m % NDB];
+          const int db = m % NDB;
+          const char *at = vl + (m / NDB) * 16 * VROWB + (db < NOV ? offv[db % NOV] : offv[db % NOV] ^ (256 + 16 + z));
           return tr_read_pair(at, at + 8 * VROWB);
         };
-        bf16x8 va[3];
-        va[0] = v_operand(0);
-        va[1] = v_operand(1);
+        constexpr int VA = D == 256 ? 1 : 2;  // V operands read ahead
+        bf16x8 va[VA + 1];
+#pragma unroll
+        for (int i = 0; i < VA; ++i) va[i] = v_operand(i);
         u32x2 cw[4];
         float mt = -INFINITY;
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
           const int step_m = m / NDB, db = m % NDB;
-          if (m + 2 < NM) va[(m + 2) % 3] = v_operand(m + 2);
+          if (m + VA < NM) va[(m + VA) % (VA + 1)] = v_operand(m + VA);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              va[m % 3],
+              va[m % (VA + 1)],
               __builtin_bit_cast(bf16x8, u32x4{pw[4 * step_m], pw[4 * step_m + 1], pw[4 * step_m + 2],
                                                pw[4 * step_m + 3]}),
               o[db], 0, 0, 0);
-          // the pairs before the step that takes them, a word of codes in two of three chunks
+          // the pairs before the step that takes them, then words of codes and scores
+          constexpr int ML = NM - NDB;
 #pragma unroll
-          for (int i = 4 * m / (3 * NDB); i < 4 * (m + 1) / (3 * NDB) && i < 4; ++i) p_pair(12 + i);
+          for (int i = 4 * m / ML; i < 4 * (m + 1) / ML && i < 4; ++i) p_pair(NPQ + i);
 #pragma unroll
           for (int w = 4 * NVC * m / NM; w < 4 * NVC * (m + 1) / NM; ++w) {
             const int k = w >> 2, i = w & 3;
