@@ -41,9 +41,11 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   constexpr float kSlack = 8.0f;                   // lazy rescale: p <= 2^8 between rescales
   constexpr int kPrioPV = 2;                       // wave priority of the PV phase (attn_bf16_dma.hip)
   static_assert(NI >= 1 && NVC >= 1 && RPI <= kPage, "tile shape");
-  // head_dim 256: O^T takes 128 of a wave's 256 registers and Q's upper terms 32; the lower terms wait in LDS
+  // head_dim 256: O^T takes 128 of a wave's 256 registers and the scores 32, which leaves room for the upper
+  // terms of Q's first 192 features; the others and the lower terms wait in LDS
   constexpr bool QLDS = D == 256;
-  constexpr int QLB = QLDS ? 64 * 32 * NS2 : 0;    // bytes of a wave's lower terms
+  constexpr int NSR = QLDS ? 3 : NS2;              // steps whose upper terms stay in registers
+  constexpr int QLB = QLDS ? 64 * 32 * (NS2 + 1) : 0;   // a wave's terms in LDS: lower, and upper of the last step
   __shared__ __align__(1024) char smem[2 * KTILEB + 2 * VTILEB + W * QLB];
   __shared__ __align__(16) int32_t pg[kMaxSplitKeys / kPage + 8];
 
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   for (int i = tid; i < n_pg; i += NT) pg[i] = a.map[pg0 + i];
 
   // ---- the query as two E4M3 terms: lane (hh, j) holds features 64 s + 32 hh .. + 31 of query q0 + j
-  i32x8 qhi[NS2], qlo[QLDS ? 1 : NS2];
+  i32x8 qhi[NSR], qlo[QLDS ? 1 : NS2];
   char *const ql_lds = smem + 2 * KTILEB + 2 * VTILEB + wave * QLB + 16 * lane;   // 16-byte piece i at + 1024 i
   int qscale;              // scale bytes of hi (byte 0) and lo (byte 1)
   {
@@ -112,8 +114,12 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         }
         uint32_t hi[2], lo[2];
         split_query<8>(x, e, bad, hi, lo);
-        qhi[s][2 * c] = hi[0];
-        qhi[s][2 * c + 1] = hi[1];
+        if (s < NSR) {
+          qhi[s % NSR][2 * c] = hi[0];
+          qhi[s % NSR][2 * c + 1] = hi[1];
+        } else {
+          *reinterpret_cast<u32x2 *>(ql_lds + 1024 * (2 * NS2 + (c >> 1)) + 8 * (c & 1)) = u32x2{hi[0], hi[1]};
+        }
         if constexpr (QLDS) {
           *reinterpret_cast<u32x2 *>(ql_lds + 1024 * (2 * s + (c >> 1)) + 8 * (c & 1)) = u32x2{lo[0], lo[1]};
         } else {
@@ -183,6 +189,12 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
 #pragma unroll
     for (int k = 0; k < NVC; ++k) p.v[k] = page_at(it * (KT / kPage) + (64 * wave + NT * k) / CH / kPage);
   };
+  // (what the rare paths derive from the lane is derived there, not kept in registers for them)
+  auto rare_lane = [&]() {
+    int x = lane;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
   // DMA of K tile `it`: instruction i of the wave fills rows (wave NI + i) RPI ..
   uint32_t kdo[NI];
 #pragma unroll
@@ -196,13 +208,14 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
 #pragma unroll
       for (int i = 0; i < NI; ++i) dma_s<0>(dst + i * 1024, kbytes + p.k[i] * pbytes, kdo[i]);
     } else {
+      const int x = rare_lane();
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int row = (wave * NI + i) * RPI + lane / CH;
+        const int row = (wave * NI + i) * RPI + x / CH;
         const int t = min(k_begin + it * KT + row, k_end - 1);
         const uint64_t pp = (uint32_t)pg[(t >> kPageShift) - pg0];
         dma_v(dst + i * 1024, kbytes + pp * pbytes + (uint32_t)(t & (kPage - 1)) * D +
-                                  16 * ((lane % CH) ^ kswz(row)));
+                                  16 * ((x % CH) ^ kswz(row)));
       }
     }
   };
@@ -219,12 +232,13 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
       // (keeps these loads apart from the others below, whose addresses are the lanes' own)
       asm volatile("" ::: "memory");
     } else {
+      const int x = rare_lane();
 #pragma unroll
       for (int k = 0; k < NVC; ++k) {
-        const int t = min(k_begin + it * KT + (64 * wave + NT * k) / CH + lane / CH, k_end - 1);
+        const int t = min(k_begin + it * KT + (64 * wave + NT * k) / CH + x / CH, k_end - 1);
         const uint64_t pp = (uint32_t)pg[(t >> kPageShift) - pg0];
         cd.v[k] = *reinterpret_cast<const u32x4 *>(vbytes + pp * pbytes +
-                                                   (uint32_t)(t & (kPage - 1)) * D + 16 * (lane % CH));
+                                                   (uint32_t)(t & (kPage - 1)) * D + 16 * (x % CH));
       }
     }
   };
@@ -310,13 +324,17 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     return two(*reinterpret_cast<const u32x4 *>(at + (offk ^ (64 * (q / NKB) + z))),
                *reinterpret_cast<const u32x4 *>(at + (offk ^ (64 * (q / NKB) + 16 + z))));
   };
+  auto q_lds = [&](int s) {
+    return two(*reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s),
+               *reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s + 1024));
+  };
   auto low = [&](int s) {
     if constexpr (QLDS)
-      return two(*reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s),
-                 *reinterpret_cast<const u32x4 *>(ql_lds + 2048 * s + 1024));
+      return q_lds(s);
     else
       return qlo[s];
   };
+  auto high = [&](int s) { return s < NSR ? qhi[s % NSR] : q_lds(NS2); };
   f32x16 zero;
 #pragma unroll
   for (int v = 0; v < 16; ++v) zero[v] = 0.f;
@@ -326,7 +344,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     for (int q = 0; q < NQ; ++q) {
       const int kb = q % NKB, s = q / NKB;
       const i32x8 ka = k_operand(kl, 0, q);
-      sc[kb] = mfma8(ka, qhi[s], q < NKB ? zero : sc[kb], ks, kb, 0);
+      sc[kb] = mfma8(ka, high(s), q < NKB ? zero : sc[kb], ks, kb, 0);
       sc[kb] = mfma8(ka, low(s), sc[kb], ks, kb, 1);
     }
   };
@@ -344,7 +362,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     return (kt + KT > k_end) || (kt + KT - 1 > qpos0);
   };
   auto mask = [&](f32x16 *sc, int t) {
-    const int lim = min(qpos0 + j, k_end - 1) - (k_begin + t * KT) - 4 * hh;   // last visible key
+    const int x = rare_lane();
+    const int lim = min(qpos0 + (x & 31), k_end - 1) - (k_begin + t * KT) - 4 * (x >> 5);   // last visible key
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -465,7 +484,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
           } else {
             ql = low(s);
             if (q + 1 < NQ) ka[(q + 1) & 1] = k_operand(kl, z, q + 1);
-            s_nxt[kb] = mfma8(ka[q & 1], qhi[s], q < NKB ? zero : s_nxt[kb], ks, kb, 0);
+            s_nxt[kb] = mfma8(ka[q & 1], high(s), q < NKB ? zero : s_nxt[kb], ks, kb, 0);
           }
 #pragma unroll
           for (int i = NPQ * c / (2 * NQ); i < NPQ * (c + 1) / (2 * NQ); ++i) p_pair(i);
@@ -549,11 +568,12 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   }
 
   // ---- epilogue
+  const int el = rare_lane(), ej = el & 31, eh = el >> 5;
   const float l_tot = sum_halves(l);
   float part_c = 0.f, part_sc = 0.f;
   if (uw.n_splits > 1) part_sc = part_scale(row_amax(o), l_tot, part_c);
-  if (!active || q0 + j >= sp.len) return;
-  const int row = q0 + j;
+  if (!active || q0 + ej >= sp.len) return;
+  const int row = q0 + ej;
   if (uw.n_splits == 1) {
     const float inv = 1.0f / l_tot;
     uint16_t *orow = a.out + ((int64_t)(sp.q_start + row) * a.n_q_heads + qhead) * D;
@@ -561,14 +581,14 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
-        const int d0 = 32 * db + 8 * gq + 4 * hh;
+        const int d0 = 32 * db + 8 * gq + 4 * eh;
         *reinterpret_cast<u32x2 *>(orow + d0) =
             u32x2{pack_bf16x2(o[db][4 * gq + 0] * inv, o[db][4 * gq + 1] * inv),
                   pack_bf16x2(o[db][4 * gq + 2] * inv, o[db][4 * gq + 3] * inv)};
       }
   } else {
     const int64_t prow = ((int64_t)split * sp.len + row) * a.n_q_heads + qhead;
-    store_partial<NDB, D>(o, part_sc, m_ref, l_tot, part_c, hh, a.ws, sp, prow);
+    store_partial<NDB, D>(o, part_sc, m_ref, l_tot, part_c, eh, a.ws, sp, prow);
   }
 }
 
