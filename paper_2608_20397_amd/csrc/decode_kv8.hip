@@ -2,16 +2,24 @@
 // sequences, each with its own page map and a length on the device; optional tanh soft cap.
 //
 // The work decomposition is that of the bf16 decode (decode_attn.hip): a workgroup takes one (sequence, KV
-// head, group of up to 16 query heads, run of pages); its 4 waves take the run's page pairs in turn, a
+// head, group of up to 16 query heads, run of pages); its waves take the run's page pairs in turn, a
 // pair in registers while the next one loads, and meet through LDS; a second kernel merges the runs.
 //   * S^T = K.Q^T on v_mfma_scale_f32_16x16x128_f8f6f4, the keys' codes straight from global memory into
 //     the A operand (lane l: row l % 16, 32 bytes from 32 (l / 16)); the query as two E4M3 terms
-//     (split_query).  head_dim 64: lane groups 2 and 3 hold the row's codes again, against zeros.
+//     (split_query).  head_dim 64: one instruction.  Its lane group g takes k 16 g .. + 15 in the first
+//     half of the operand and k 64 + 16 g .. + 15 in the second, and the scales of k < 64 from groups 0 and
+//     1; so a lane's 16 bytes of codes stand in both halves, against hi in one and lo in the other.
 //   * a lane holds the scores of keys 4 (l / 16) .. +3, whose 4 scale bytes are one word: the key's scale is
 //     multiplied to the score, the value's to the probability that it is weighed with (a power of two:
 //     exact), and V enters the PV product as its codes in bf16.
 // Keys past a sequence's end re-read its last key and weigh nothing.  HBM-bound: head_dim + 1 bytes of K and of
 // V per key and KV head, half the bf16 cache's.
+//   * All heads of one (sequence, run) go to one XCD, side by side: a page's 16 scale bytes of 8 heads are one
+//     cache line, which every XCD fetched for itself when heads were dealt to them (32 sequences of 17473
+//     tokens: 1.19 GB fetched for 1.12 GB, 1.13 so).
+//   * Launches over more bytes than the caches hold read the codes with non-temporal loads, except where the
+//     next sequence maps the same page and may find it in a cache: 210 -> 192 us for those 32 sequences on pages
+//     of their own; on pages that all of them share 118 us with plain loads, 162 without.
 #include "attn_common.h"
 #include "attn_dma.h"
 #include "decode_common.h"
@@ -19,21 +27,24 @@
 #include "launch_kv8.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace nexus {
 
 namespace {
 
-template <int D, bool CAP>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const DecodeArgs a) {
-  constexpr int NP = 2;               // pages per step of a wave
+// NW: waves of a workgroup.  STREAM: see the header comment.
+template <int D, bool CAP, int NW, bool STREAM>
+__global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs a) {
+  constexpr int NP = D == 256 ? 1 : 2;   // pages per step of a wave
   constexpr int KS = D == 256 ? 2 : 1;   // 128-feature steps of S^T
   constexpr int DT = D / 16;          // O^T tiles
   constexpr int ROWB = 2 * D;         // bytes of a staged V row (bf16)
+  constexpr int KC = D == 64 ? 1 : 2;    // 16-byte loads of K codes per lane, page and step
   constexpr int VL = D / 64;          // 16-byte loads of V codes per lane and page
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer (floats)
-  constexpr int STAGE_BYTES = kDecWaves * NP * 16 * ROWB;
-  constexpr int MERGE_BYTES = 2 * 16 * MO_LD * 4 + 2 * 2 * 16 * 4;
+  constexpr int STAGE_BYTES = NW * NP * 16 * ROWB;
+  constexpr int MERGE_BYTES = NW / 2 * (16 * MO_LD * 4 + 2 * 16 * 4);
   __shared__ __align__(1024) char smem[STAGE_BYTES > MERGE_BYTES ? STAGE_BYTES : MERGE_BYTES];
   __shared__ int32_t pgs[kMaxSplitPages];
 
@@ -41,7 +52,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qn = lane & 15, grp = lane >> 4;
-  const int split = blockIdx.x, hg = blockIdx.y, b = blockIdx.z;
+  // workgroups go to the 8 XCDs in turn
+  const int unit = 8 * (int)(blockIdx.y + gridDim.y * blockIdx.z) + (blockIdx.x & 7), hg = blockIdx.x >> 3;
+  if (unit >= a.n_seqs * a.own_splits) return;
+  const int b = unit / a.own_splits, split = unit - b * a.own_splits;
+  // The run's pages are loaded beside the length (a map row has max_len's pages; those past the sequence's
+  // end are not used).
+  const int32_t *map = a.maps + (size_t)b * a.map_stride;
+  const int p_begin = split * a.split_pages;
+  const int n_map = min(a.split_pages, (a.max_len + 15) / 16 - p_begin);
+  for (int i = tid; i < n_map; i += 64 * NW) pgs[i] = map[p_begin + i];
+  bool shared = false;
+  if constexpr (STREAM) {
+    const int next = b + 1 < a.n_seqs ? b + 1 : 0, mid = p_begin + n_map / 2;
+    shared = next != b && map[mid] == a.maps[(size_t)next * a.map_stride + mid];
+  }
   const int len = seq_len_of(a, b);
   const int qg = hg % a.n_qgroups;
   const int h = hg / a.n_qgroups;
@@ -52,18 +77,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
 
   if (len == 0) {
     if (split == 0)
-      for (int i = tid; i < g_cnt * D; i += 256)
+      for (int i = tid; i < g_cnt * D; i += 64 * NW)
         out[((size_t)b * a.n_q_heads + hq0) * D + i] = 0;
     return;
   }
   const int n_pages = (len + 15) >> 4;
-  const int p_begin = split * a.split_pages;
   if (p_begin >= n_pages) return;
   const int p_end = min(p_begin + a.split_pages, n_pages);
   const int n_splits = (n_pages + a.split_pages - 1) / a.split_pages;
   const int n_sp = p_end - p_begin;
-  const int32_t *map = a.maps + (size_t)b * a.map_stride;
-  for (int i = tid; i < n_sp; i += 256) pgs[i] = map[p_begin + i];
 
   // ---- the queries: column qn = query head hq0 + qn (columns past the group are zero)
   const bool q_ok = qn < g_cnt;
@@ -78,7 +100,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int f = D == 64 ? 32 * (grp & 1) : 128 * s + 32 * grp;
+        const int f = D == 64 ? 16 * grp : 128 * s + 32 * grp;
+        if (D == 64 && c >= 2) {
+          raw[s][c] = u32x4{0u, 0u, 0u, 0u};
+          continue;
+        }
         raw[s][c] = q_ok ? *reinterpret_cast<const u32x4 *>(qrow + f + 8 * c) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -102,12 +128,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
         split_query<8>(x, e, bad, hi, lo);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          qhi[s][2 * c + w] = D == 64 && grp >= 2 ? 0u : hi[w];
-          qlo[s][2 * c + w] = D == 64 && grp >= 2 ? 0u : lo[w];
+          if (D == 64 && c >= 2) continue;
+          qhi[s][2 * c + w] = hi[w];
+          if (D == 64)
+            qhi[s][4 + 2 * c + w] = lo[w];
+          else
+            qlo[s][2 * c + w] = lo[w];
         }
       }
-    qs_hi = e + 127;
     qs_lo = e + 127 - 4;
+    qs_hi = D == 64 && grp >= 2 ? qs_lo : e + 127;
   }
   __syncthreads();   // pgs[]
 
@@ -118,30 +148,36 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
   const uint64_t page_scales = (uint64_t)a.n_kv_heads * 16;
   const char *kbase = reinterpret_cast<const char *>(a.kc) + (size_t)h * 16 * D;
   const char *vbase = reinterpret_cast<const char *>(a.vc) + (size_t)h * 16 * D;
-  const uint8_t *ksb = a.ks + h * 16 + 4 * grp, *vsb = a.vs + h * 16 + 4 * grp;
+  const uint8_t *ksb = a.ks + h * 16, *vsb = a.vs + h * 16;
   char *vstage = smem + wave * NP * 16 * ROWB;
 
   struct Page {
-    u32x4 k[KS][2];
+    u32x4 k[KS][KC];
     u32x4 v[VL];
     uint32_t ks, vs;         // scale bytes of keys 4 grp .. +3
   };
-  auto load_page = [&](int nvalid, uint32_t phys, Page &pg) {
-    const char *kp = kbase + phys * page_bytes + min(qn, nvalid - 1) * D;
+  const uint32_t ko = D == 64 ? 16 * grp : 32 * grp;
+  auto load_page = [&](int nvalid, uint32_t phys, Page &pg, auto stream) {
+    auto ld = [&](const char *p) {
+      const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+      return decltype(stream)::value ? ld_stream(q) : *q;
+    };
+    // uniform page addresses, 32-bit lane offsets
+    const char *kp = kbase + phys * page_bytes, *vp = vbase + phys * page_bytes;
+    const uint32_t krow = (uint32_t)min(qn, nvalid - 1) * D + ko;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-        pg.k[s][c] = *reinterpret_cast<const u32x4 *>(
-            kp + (D == 64 ? 32 * (grp & 1) : 128 * s + 32 * grp) + 16 * c);
-    const char *vp = vbase + phys * page_bytes;
+      for (int c = 0; c < KC; ++c)
+        pg.k[s][c] = ld(kp + (uint32_t)(krow + 128 * s + 16 * c));
 #pragma unroll
     for (int j = 0; j < VL; ++j) {
-      const int byte = 16 * lane + 1024 * j;
-      pg.v[j] = *reinterpret_cast<const u32x4 *>(vp + min(byte / D, nvalid - 1) * D + byte % D);
+      const uint32_t row = min((16 * lane + 1024 * j) / D, nvalid - 1);
+      pg.v[j] = ld(vp + (uint32_t)(row * D + 16 * lane % D));
     }
-    pg.ks = *reinterpret_cast<const uint32_t *>(ksb + phys * page_scales);
-    pg.vs = *reinterpret_cast<const uint32_t *>(vsb + phys * page_scales);
+    const uint8_t *kq = ksb + phys * page_scales, *vq = vsb + phys * page_scales;
+    pg.ks = *reinterpret_cast<const uint32_t *>(kq + (uint32_t)(4 * grp));
+    pg.vs = *reinterpret_cast<const uint32_t *>(vq + (uint32_t)(4 * grp));
   };
 
   f32x4 o[DT];
@@ -160,11 +196,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
       f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 u = pr.pg[pp].k[st][0], w = pr.pg[pp].k[st][1];
+        const u32x4 u = pr.pg[pp].k[st][0], w = pr.pg[pp].k[st][KC - 1];
         const i32x8 ka = {(int)u[0], (int)u[1], (int)u[2], (int)u[3],
                           (int)w[0], (int)w[1], (int)w[2], (int)w[3]};
         s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qhi[st], s, 0, 0, 0, 127, 0, qs_hi);
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qlo[st], s, 0, 0, 0, 127, 0, qs_lo);
+        if constexpr (D != 64)
+          s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qlo[st], s, 0, 0, 0, 127, 0, qs_lo);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -219,55 +256,64 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
     for (int t = 0; t < DT; ++t) {
       const int c = 2 * t + ((qn & 3) >> 1);
       const char *src = vstage + r * ROWB + 16 * (c ^ vswz<D>(r)) + 8 * (qn & 1);
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          tr_read_pair(src, src + 16 * ROWB), __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]}),
-          o[t], 0, 0, 0);
+      if constexpr (NP == 2)
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            tr_read_pair(src, src + 16 * ROWB),
+            __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2 * NP - 2], w[2 * NP - 1]}), o[t], 0, 0, 0);
+      else
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src),
+            __builtin_bit_cast(s16x4, u32x2{w[0], w[1]}), o[t], 0, 0, 0);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
 
-  // ---- this wave's page pairs through two register buffers, as decode_attn.hip
-  {
-    const int n_pairs = (n_sp + NP - 1) / NP;
-    const int n_mine = wave < n_pairs ? (n_pairs - wave + kDecWaves - 1) / kDecWaves : 0;
-    if (n_mine > 0) {
-      auto entry = [&](int k) { return NP * (wave + kDecWaves * k); };
-      auto issue = [&](int k, Pair &pr) {
+  // ---- this wave's steps (NP pages each) of the run, entries NP (wave + NW k), through two register
+  // buffers, as decode_attn.hip: a step loads while the one before is computed
+  auto run = [&](auto stream) {
+    const int n_steps = (n_sp + NP - 1) / NP;
+    const int n_mine = wave < n_steps ? (n_steps - wave + NW - 1) / NW : 0;
+    if (n_mine == 0) return;
+    auto entry = [&](int k) { return NP * (wave + NW * k); };
+    auto issue = [&](int k, Pair &pr) {
 #pragma unroll
-        for (int pp = 0; pp < NP; ++pp) {
-          const int e = min(entry(min(k, n_mine - 1)) + pp, n_sp - 1);
-          load_page(keys_of(e), (uint32_t)__builtin_amdgcn_readfirstlane(pgs[e]), pr.pg[pp]);
-        }
-      };
-      auto compute = [&](int k, const Pair &pr) {
-        const int e = entry(k);
-        int keys[NP];
-#pragma unroll
-        for (int pp = 0; pp < NP; ++pp) keys[pp] = keys_of(min(e + pp, n_sp - 1));
-        compute_pair(keys, e + 1 < n_sp, pr);
-      };
-      Pair b0, b1;
-      issue(0, b0);
-      int k = 0;
-      for (; k + 1 < n_mine; k += 2) {
-        issue(k + 1, b1);
-        __builtin_amdgcn_sched_barrier(0);
-        compute(k, b0);
-        __builtin_amdgcn_sched_barrier(0);
-        issue(k + 2, b0);
-        __builtin_amdgcn_sched_barrier(0);
-        compute(k + 1, b1);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int pp = 0; pp < NP; ++pp) {
+        const int e = min(entry(min(k, n_mine - 1)) + pp, n_sp - 1);
+        load_page(keys_of(e), (uint32_t)__builtin_amdgcn_readfirstlane(pgs[e]), pr.pg[pp], stream);
       }
-      if (k < n_mine) compute(k, b0);
+    };
+    auto compute = [&](int k, const Pair &pr) {
+      const int e = entry(k);
+      int keys[NP];
+#pragma unroll
+      for (int pp = 0; pp < NP; ++pp) keys[pp] = keys_of(min(e + pp, n_sp - 1));
+      compute_pair(keys, e + 1 < n_sp, pr);
+    };
+    Pair b0, b1;
+    issue(0, b0);
+    int k = 0;
+    for (; k + 1 < n_mine; k += 2) {
+      issue(k + 1, b1);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(k, b0);
+      __builtin_amdgcn_sched_barrier(0);
+      issue(k + 2, b0);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(k + 1, b1);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
+    if (k < n_mine) compute(k, b0);
+  };
+  if (STREAM && !shared)
+    run(std::true_type{});
+  else
+    run(std::false_type{});
 
-  // ---- merge the 4 waves' (m, l, O^T): waves 2 and 3 into 0 and 1, then 1 into 0, which writes
+  // ---- merge the waves' (m, l, O^T) pairwise through LDS, the upper half of them into the lower
   lsum = sum_x32(sum_x16(lsum));
-  float *mo = reinterpret_cast<float *>(smem);   // [2 slots][16 columns][MO_LD]
-  float *mml = mo + 2 * 16 * MO_LD;              // [2 slots][16 columns][m, l]
+  float *mo = reinterpret_cast<float *>(smem);   // [NW / 2 slots][16 columns][MO_LD]
+  float *mml = mo + NW / 2 * 16 * MO_LD;         // [NW / 2 slots][16 columns][m, l]
   auto store_state = [&](int slot) {
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -294,14 +340,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void decode_kv8_kernel(const
     m_ref = M;
   };
   __syncthreads();   // the V staging slots are reused
-  if (wave >= 2) store_state(wave - 2);
-  __syncthreads();
-  if (wave < 2) merge_state(wave);
-  __syncthreads();
-  if (wave == 1) store_state(0);
-  __syncthreads();
+#pragma unroll
+  for (int half = NW / 2; half >= 1; half >>= 1) {
+    if (wave >= half && wave < 2 * half) store_state(wave - half);
+    __syncthreads();
+    if (wave < half) merge_state(wave);
+    __syncthreads();
+  }
   if (wave != 0) return;
-  merge_state(0);
   if (!q_ok) return;
   const int row = b * a.n_q_heads + hq0 + qn;
   if (n_splits == 1) {
@@ -362,17 +408,36 @@ hipError_t launch_decode_kv8(const DecodeLaunch &p, hipStream_t stream) {
   a.cap_in = p.softcap > 0.f ? p.scale / p.softcap : 0.f;
   a.cap_out = p.softcap * log2e;
   const bool cap = p.softcap > 0.f;
-  const dim3 grid(ns, p.n_kv_heads * a.n_qgroups, p.n_seqs);
-  auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
+  // 8 units side by side, one per XCD; three grid dimensions, for one does not hold every launch
+  const int64_t units8 = ((int64_t)p.n_seqs * ns + 7) / 8;
+  const uint32_t gy = (uint32_t)std::min<int64_t>(units8, 32768);
+  const int n_hq = p.n_kv_heads * a.n_qgroups;
+  const dim3 grid(8 * n_hq, gy, (uint32_t)((units8 + gy - 1) / gy));
+  // Non-temporal loads where the codes may pass twice the 256 MB last-level cache and a page is read by one
+  // workgroup of a sequence (64 sequences of 2000 tokens, 0.26 GB: 46.9 us, 48.8 so).
+  const bool stream_codes =
+      a.n_qgroups == 1 &&
+      (int64_t)p.n_seqs * p.max_len * p.n_kv_heads * p.head_dim * 2 >= (int64_t)512 << 20;
+  // 8 waves where the launch has a workgroup per CU or fewer and a run gives each wave two steps or more: 48
+  // sequences of up to 700 tokens, 64 heads of 64 over 2, 10.1 -> 8.9 us; with 512 workgroups 20.6 us
+  // becomes 26.7 (8 sequences of 4000), with 7 pages 6.2 becomes 7.2.  (head_dim 256 would spill.)
+  const bool wide = p.head_dim != 256 && (int64_t)n_hq * p.n_seqs * ns <= 256 && a.split_pages >= 32;
+  auto run = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a);
     return hipGetLastError();
   };
-  hipError_t e;
-  switch (p.head_dim) {
-    case 64: e = cap ? run(decode_kv8_kernel<64, true>) : run(decode_kv8_kernel<64, false>); break;
-    case 128: e = cap ? run(decode_kv8_kernel<128, true>) : run(decode_kv8_kernel<128, false>); break;
-    default: e = cap ? run(decode_kv8_kernel<256, true>) : run(decode_kv8_kernel<256, false>); break;
-  }
+  auto with_cap = [&](auto d, auto c) {
+    constexpr int NW8 = d() == 256 ? 4 : 8;
+    if (wide)
+      return stream_codes ? run(decode_kv8_kernel<d(), c(), NW8, true>, NW8)
+                          : run(decode_kv8_kernel<d(), c(), NW8, false>, NW8);
+    return stream_codes ? run(decode_kv8_kernel<d(), c(), 4, true>, 4)
+                        : run(decode_kv8_kernel<d(), c(), 4, false>, 4);
+  };
+  auto with_d = [&](auto d) { return cap ? with_cap(d, std::true_type{}) : with_cap(d, std::false_type{}); };
+  const hipError_t e = p.head_dim == 64    ? with_d(std::integral_constant<int, 64>{})
+                       : p.head_dim == 128 ? with_d(std::integral_constant<int, 128>{})
+                                           : with_d(std::integral_constant<int, 256>{});
   if (e != hipSuccess || ns <= 1) return e;
   return launch_decode_combine(a, p.head_dim, true, stream);
 }
