@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs
   constexpr int VL = D / 64;          // 16-byte loads of V codes per lane and page
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer (floats)
   constexpr int STAGE_BYTES = NW * NP * 16 * ROWB;
-  constexpr int MERGE_BYTES = NW / 2 * (16 * MO_LD * 4 + 2 * 16 * 4);
+  constexpr int MERGE_BYTES = NW * (16 * MO_LD * 4 + 2 * 16 * 4);
   __shared__ __align__(1024) char smem[STAGE_BYTES > MERGE_BYTES ? STAGE_BYTES : MERGE_BYTES];
   __shared__ int32_t pgs[kMaxSplitPages];
 
@@ -310,55 +310,57 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs
   else
     run(std::false_type{});
 
-  // ---- merge the waves' (m, l, O^T) pairwise through LDS, the upper half of them into the lower
+  // ---- merge the waves' (m, l, O^T): every wave leaves its state in LDS, then a thread adds all of them for
+  // NF features of one column (pairwise, with two barriers a level, 48 sequences of up to 700 tokens took 8.7
+  // us instead of 8.0)
   lsum = sum_x32(sum_x16(lsum));
-  float *mo = reinterpret_cast<float *>(smem);   // [NW / 2 slots][16 columns][MO_LD]
-  float *mml = mo + NW / 2 * 16 * MO_LD;         // [NW / 2 slots][16 columns][m, l]
-  auto store_state = [&](int slot) {
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<f32x4 *>(mo + (slot * 16 + qn) * MO_LD + 16 * t + 4 * grp) = o[t];
-    if (grp == 0) {
-      mml[2 * (slot * 16 + qn)] = m_ref;
-      mml[2 * (slot * 16 + qn) + 1] = lsum;
-    }
-  };
-  auto merge_state = [&](int slot) {
-    const float mb = mml[2 * (slot * 16 + qn)];
-    const float lb = mml[2 * (slot * 16 + qn) + 1];
-    const float M = fmaxf(m_ref, mb);
-    // a wave that saw no page has m = -inf and contributes nothing
-    const float wa = m_ref > -INFINITY ? fast_exp2(m_ref - M) : 0.f;
-    const float wb = mb > -INFINITY ? fast_exp2(mb - M) : 0.f;
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      const f32x4 ob =
-          *reinterpret_cast<const f32x4 *>(mo + (slot * 16 + qn) * MO_LD + 16 * t + 4 * grp);
-      o[t] = o[t] * wa + ob * wb;
-    }
-    lsum = lsum * wa + lb * wb;
-    m_ref = M;
-  };
+  float *mo = reinterpret_cast<float *>(smem);   // [NW][16 columns][MO_LD]
+  float *mml = mo + NW * 16 * MO_LD;             // [16 columns][NW][m, l]
   __syncthreads();   // the V staging slots are reused
 #pragma unroll
-  for (int half = NW / 2; half >= 1; half >>= 1) {
-    if (wave >= half && wave < 2 * half) store_state(wave - half);
-    __syncthreads();
-    if (wave < half) merge_state(wave);
-    __syncthreads();
-  }
-  if (wave != 0) return;
-  if (!q_ok) return;
-  const int row = b * a.n_q_heads + hq0 + qn;
-  if (n_splits == 1) {
-    const float inv = 1.0f / lsum;
+  for (int t = 0; t < DT; ++t)
+    *reinterpret_cast<f32x4 *>(mo + (wave * 16 + qn) * MO_LD + 16 * t + 4 * grp) = o[t];
+  if (grp == 0)
+    *reinterpret_cast<f32x2 *>(mml + 2 * (qn * NW + wave)) = f32x2{m_ref, lsum};
+  __syncthreads();
+  constexpr int NF = 16 * D / (64 * NW);         // features of a thread
+  const int col = tid * NF / D, f0 = tid * NF % D;
+  if (col >= g_cnt) return;
+  float mw[NW], M = -INFINITY, l_tot = 0.f, acc[NF];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<u32x2 *>(out + (size_t)row * D + 16 * t + 4 * grp) =
-          u32x2{pack_bf16x2(o[t][0] * inv, o[t][1] * inv),
-                pack_bf16x2(o[t][2] * inv, o[t][3] * inv)};
+  for (int w = 0; w < NW; ++w) {
+    mw[w] = mml[2 * (col * NW + w)];
+    M = fmaxf(M, mw[w]);
+  }
+#pragma unroll
+  for (int i = 0; i < NF; ++i) acc[i] = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    // a wave that saw no page has m = -inf and contributes nothing
+    const float f = mw[w] > -INFINITY ? fast_exp2(mw[w] - M) : 0.f;
+    l_tot += f * mml[2 * (col * NW + w) + 1];
+#pragma unroll
+    for (int i = 0; i < NF; i += 2) {
+      const f32x2 x = *reinterpret_cast<const f32x2 *>(mo + (w * 16 + col) * MO_LD + f0 + i);
+      acc[i] += f * x[0];
+      acc[i + 1] += f * x[1];
+    }
+  }
+  const size_t row = (size_t)b * a.n_q_heads + hq0 + col;
+  if (n_splits == 1) {
+    const float inv = 1.0f / l_tot;
+#pragma unroll
+    for (int i = 0; i < NF; i += 2)
+      *reinterpret_cast<uint32_t *>(out + row * D + f0 + i) = pack_bf16x2(acc[i] * inv, acc[i + 1] * inv);
   } else {
-    store_part<D>(a, row, split, o, m_ref, lsum, grp);
+    const size_t slot = row * a.max_splits + split;
+#pragma unroll
+    for (int i = 0; i < NF; i += 2)
+      *reinterpret_cast<f32x2 *>(a.part + slot * D + f0 + i) = f32x2{acc[i], acc[i + 1]};
+    if (f0 == 0) {
+      a.part_ml[2 * slot] = M;
+      a.part_ml[2 * slot + 1] = l_tot;
+    }
   }
 }
 
