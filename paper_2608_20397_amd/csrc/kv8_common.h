@@ -19,6 +19,8 @@ constexpr uint32_t kBadScale = 255;           // the row had an element that is 
 constexpr uint32_t kBadCodes = 0x7F7F7F7Fu;   // its codes: NaN
 
 typedef __attribute__((ext_vector_type(8))) int32_t i32x8;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
 // Exponent of a row from the bits of its largest magnitude (a finite one): adding 0x1FFFFF carries into
 // the exponent field exactly when the mantissa passes 1.75.
@@ -48,21 +50,56 @@ __device__ __forceinline__ uint32_t pack_e4m3(float y0, float y1, float y2, floa
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y2, y3, lo, true);
 }
 
-// Codes of N values (a multiple of 4) of a row whose largest magnitude has the bits `am`.
+// The same largest magnitude of bf16 pairs as they lie in words: the upper halves and the lower ones together.
+template <int W>
+__device__ __forceinline__ uint32_t amax_bits_bf16(const uint32_t *w) {
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+  return (uint32_t)max(m[0], m[1]) << 16;
+}
+
+// Codes of N values (a multiple of 4) of a row whose largest magnitude has the bits `am`: x / 2^e, which the
+// conversion divides by itself.
 template <int N>
 __device__ __forceinline__ void quantise(const float *x, uint32_t am, uint32_t *codes) {
-  const float inv = exp2i(-row_exp(am));
+  const float scale = exp2i(row_exp(am));
   float y[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) y[e] = x[e] * inv;
+  for (int e = 0; e < N; ++e) y[e] = x[e];
   if (am > 0x7F600000u) {   // past 448 * 2^kMaxExp, or not finite
 #pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = fminf(fmaxf(y[e], -448.f), 448.f);
+    for (int e = 0; e < N; ++e) y[e] = fminf(fmaxf(y[e], -448.f * scale), 448.f * scale);
   }
 #pragma unroll
   for (int e = 0; e < N / 4; ++e) {
-    codes[e] = pack_e4m3(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
-    if (am >= 0x7F800000u) codes[e] = kBadCodes;
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[4 * e], y[4 * e + 1], scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, y[4 * e + 2], y[4 * e + 3], scale, true);
+    codes[e] = am >= 0x7F800000u ? kBadCodes : __builtin_bit_cast(uint32_t, w);
+  }
+}
+// ... of W words of bf16 pairs.
+template <int W>
+__device__ __forceinline__ void quantise_bf16(const uint32_t *x, uint32_t am, uint32_t *codes) {
+  if (am > 0x7F600000u) {   // (the largest exponents take the clamps of the fp32 path)
+    float y[2 * W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      y[2 * i] = __uint_as_float(x[i] << 16);
+      y[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+    }
+    quantise<2 * W>(y, am, codes);
+    return;
+  }
+  const float scale = exp2i(row_exp(am));
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x[2 * i]), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x[2 * i + 1]), scale, true);
+    codes[i] = __builtin_bit_cast(uint32_t, w);
   }
 }
 __device__ __forceinline__ uint32_t scale_byte(uint32_t am) {
