@@ -592,16 +592,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   }
 }
 
-size_t attn_kv8_workspace_bytes(const AttnLaunch &p) {
-  AttnPlan plan;
-  if (!plan_attention(p, plan)) return (size_t)-1;
-  return plan.ws_bytes;
-}
-
-hipError_t launch_attention_kv8(const AttnLaunch &p, hipStream_t stream) {
-  AttnPlan plan;
-  if (!plan_attention(p, plan)) return hipErrorInvalidValue;
-  if (plan.ws_bytes > p.workspace_bytes) return hipErrorInvalidValue;
+hipError_t launch_attention_kv8(const AttnLaunch &p, const AttnPlan &plan, hipStream_t stream) {
   AttnArgs args{};
   const int64_t layer_rows = (int64_t)p.layer * p.n_phys_pages * p.n_kv_heads * kPage;
   args.q = (const uint16_t *)p.q;

@@ -10,9 +10,9 @@
 // neighbours in a wave and find its largest magnitude by lane exchanges.  HBM-bound: a row is read once
 // and written once, at half (bf16) or a quarter (fp32) of its bytes.
 //
-// A workgroup takes a few tokens of some layers, all heads.  Its first loads go out before it forms its
-// angles.  Angles that differ by token cost an fp64 sine and cosine per token and pair, more time than the rows of one layer take: such workgroups go through two
-// layers with one table where there are enough of them.
+// A workgroup takes a few tokens of one or two layers, all heads.  Its first loads go out before it forms its
+// angles.  Angles that differ by token cost an fp64 sine and cosine per token and pair, more time than the
+// rows of one layer take: such workgroups go through two layers with one table where there are enough of them.
 #include "kv8_common.h"
 #include "launch_kv8.h"
 #include "rope_math.h"

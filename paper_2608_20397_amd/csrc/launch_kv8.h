@@ -45,9 +45,9 @@ struct Kv8ReadLaunch {
 };
 hipError_t launch_kv8_read(const Kv8ReadLaunch &p, hipStream_t stream);
 
-// Suffix attention over an 8-bit cache (AttnLaunch::kv8 set).
-size_t attn_kv8_workspace_bytes(const AttnLaunch &p);
-hipError_t launch_attention_kv8(const AttnLaunch &p, hipStream_t stream);
+// Suffix attention over an 8-bit cache (AttnLaunch::kv8 set), with the launch's plan (attn_common.h).
+struct AttnPlan;
+hipError_t launch_attention_kv8(const AttnLaunch &p, const AttnPlan &plan, hipStream_t stream);
 
 // Decode step over an 8-bit cache (DecodeLaunch::k_scale and v_scale set).
 size_t decode_kv8_workspace_bytes(const DecodeLaunch &p);

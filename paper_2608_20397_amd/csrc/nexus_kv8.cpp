@@ -1,6 +1,7 @@
 // C-ABI entry points of the 8-bit cache: host-side validation (fail-closed: nothing is enqueued unless every
 // check passes) and dispatch.  Stateless; allocates no device memory.
 #include "api_checks.h"
+#include "attn_common.h"
 #include "launch_kv8.h"
 
 #include <new>
@@ -228,7 +229,8 @@ size_t nexus_kv8_suffix_attn_varlen_workspace(int32_t n_seqs, const int32_t *q_s
   Suffixes s;
   AttnLaunch L;
   if (plan_launch(n_seqs, q_start, seq_len, seq_n_past, n_q_heads, cache, s, L)) return SIZE_MAX;
-  return attn_kv8_workspace_bytes(L);
+  AttnPlan plan;
+  return plan_attention(L, plan) ? plan.ws_bytes : SIZE_MAX;
 } catch (const std::bad_alloc &) {
   return SIZE_MAX;
 }
@@ -255,9 +257,10 @@ nexus_status nexus_kv8_suffix_attn_varlen(const void *q, int32_t n_seqs, const i
   if ((st = plan_launch(n_seqs, q_start, seq_len, seq_n_past, n_q_heads, cache, s, L))) return st;
   for (int32_t b = 0; b < n_seqs; ++b)
     if (seq_n_past[b] + seq_len[b] > (int64_t)pt->n_logical_pages * kPageSize) return NEXUS_ERANGE;
-  const size_t need = attn_kv8_workspace_bytes(L);
-  if (need == SIZE_MAX) return NEXUS_EINVAL;
-  if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
+  AttnPlan plan;
+  if (!plan_attention(L, plan)) return NEXUS_EINVAL;
+  if (plan.ws_bytes > 0 &&
+      (!workspace || workspace_bytes < plan.ws_bytes || (uintptr_t)workspace % 16 != 0))
     return NEXUS_EWORKSPACE;
   L.q = q;
   L.out = out;
@@ -273,7 +276,7 @@ nexus_status nexus_kv8_suffix_attn_varlen(const void *q, int32_t n_seqs, const i
   L.softcap = softcap;
   L.workspace = workspace;
   L.workspace_bytes = workspace ? workspace_bytes : 0;
-  return from_hip(launch_attention_kv8(L, as_stream(stream)));
+  return from_hip(launch_attention_kv8(L, plan, as_stream(stream)));
 } catch (const std::bad_alloc &) {
   return NEXUS_EHIP;
 }

@@ -172,23 +172,15 @@ def _on_device(*named):
     return dev
 
 
-def _on_current_device(*named):
-    """_on_device, and that device must be the current one: the launch goes to its stream."""
-    dev = _on_device(*named)
-    if dev is not None and dev.index != torch.cuda.current_device():
-        raise NexusError(EINVAL, f"operands are on {dev}, the current device is "
-                                 f"{torch.cuda.current_device()}")
-
-
 def _checked_map(cache, k: torch.Tensor, pm: torch.Tensor) -> CPageTable:
     if pm.dtype != torch.int32 or pm.dim() != 1 or not pm.is_contiguous():
         raise NexusError(EINVAL, "page_map must be a contiguous int32 vector")
     _on_device(("cache k", k), ("page_map", pm))
     npp = k.shape[1]
     key = (pm.data_ptr(), pm._version, pm.numel(), npp)
-    if cache._map_checked != key:
+    if cache._map_checked is None or cache._map_checked[0] != key:
         check_page_table(pm.cpu().numpy(), npp)      # raises NexusError(ERANGE)
-        cache._map_checked = key
+        cache._map_checked = (key, pm)               # pm is kept, so no other map can get its address
     return CPageTable(pm.data_ptr(), pm.numel())
 
 
@@ -481,36 +473,51 @@ class KV8Cache:
                    new(rows, torch.uint8), new(rows, torch.uint8), page_map, rope_base, rope_style)
 
     def c(self) -> CKv8Cache:
-        if self.k.dim() != 5:
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        shape = k.shape
+        if len(shape) != 5 or shape[3] != PAGE:
             raise NexusError(ESHAPE, "cache k must be [L][pages][H][16][D]")
-        L, npp, H, P, D = self.k.shape
-        parts = (("cache k", self.k), ("cache v", self.v), ("k_scale", self.k_scale),
-                 ("v_scale", self.v_scale))
-        _on_current_device(*parts, ("page_map", self.page_map))
-        for name, t in parts:
-            scale = name.endswith("scale")
-            if t.dtype != torch.uint8 and (scale or t.dtype != torch.float8_e4m3fn):
-                raise NexusError(EDTYPE, f"{name}: unsupported dtype {t.dtype}")
-            if tuple(t.shape) != ((L, npp, H, P) if scale else (L, npp, H, P, D)) or P != PAGE \
-                    or not t.is_contiguous():
-                raise NexusError(ESHAPE, f"{name} must be contiguous [L][pages][H][16]"
-                                         f"{'' if scale else '[D]'}, got {tuple(t.shape)}")
-        return CKv8Cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
-                         self.v_scale.data_ptr(), L, npp, P, H, D, self.rope_style, self.rope_base)
+        _here(cache_k=k, cache_v=v, k_scale=ks, v_scale=vs, page_map=self.page_map)
+        for t in (k, v):
+            if t.dtype != torch.float8_e4m3fn and t.dtype != torch.uint8:
+                raise NexusError(EDTYPE, f"cache k/v: unsupported dtype {t.dtype}")
+            if t.shape != shape or not t.is_contiguous():
+                raise NexusError(ESHAPE, f"cache k/v must be contiguous [L][pages][H][16][D], got {tuple(t.shape)}")
+        for t in (ks, vs):
+            if t.dtype != torch.uint8:
+                raise NexusError(EDTYPE, f"k_scale/v_scale: unsupported dtype {t.dtype}")
+            if t.shape != shape[:4] or not t.is_contiguous():
+                raise NexusError(ESHAPE, f"k_scale/v_scale must be contiguous [L][pages][H][16], got {tuple(t.shape)}")
+        L, npp, H, P, D = shape
+        return CKv8Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), L, npp, P, H, D,
+                         self.rope_style, self.rope_base)
 
     def pt(self) -> CPageTable:
         return _checked_map(self, self.k, self.page_map)
 
 
+def _here(**tensors):
+    """The given tensors must be on the current device, to whose stream the launch goes."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if dev is None and t.is_cuda:
+            dev = torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != dev:
+            raise NexusError(EINVAL, f"{name} is on {t.device}, not on the current device")
+
+
 def _kv8_rows(cc: CKv8Cache, k: torch.Tensor, v: torch.Tensor):
     """Checks rows [L][n][H][D] beside an 8-bit cache; returns n and their dtype's code."""
-    if k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (cc.n_layers, cc.n_kv_heads, cc.head_dim) \
-            or v.shape != k.shape or not (k.is_contiguous() and v.is_contiguous()):
+    shape = k.shape
+    if len(shape) != 4 or shape[0] != cc.n_layers or shape[2] != cc.n_kv_heads or shape[3] != cc.head_dim \
+            or v.shape != shape or not (k.is_contiguous() and v.is_contiguous()):
         raise NexusError(ESHAPE, "k/v must be contiguous [L][T][H][D] with the cache's L, H and D")
     if v.dtype != k.dtype:
         raise NexusError(EDTYPE, "k and v dtypes differ")
-    _on_current_device(("k", k), ("v", v))
-    return k.shape[1], _dtype_code(k)
+    _here(k=k, v=v)
+    return shape[1], _dtype_code(k)
 
 
 def kv8_append(cache: KV8Cache, k: torch.Tensor, v: torch.Tensor, offset: int, pos0: int):
@@ -541,7 +548,7 @@ def kv8_splice(cache: KV8Cache, block: Block, offset: int, dst_pos: int):
     cc, pt, cb = cache.c(), cache.pt(), block.c()
     if block.v.dtype != block.k.dtype:
         raise NexusError(EDTYPE, "block k and v dtypes differ")
-    _on_current_device(("block k", block.k))
+    _here(block_k=block.k)
     _check(lib().nexus_kv8_splice(C.byref(cc), C.byref(pt), C.byref(cb), offset, dst_pos, _stream()),
            "nexus_kv8_splice")
 
@@ -564,7 +571,7 @@ def kv8_read(cache: KV8Cache, offset: int, n_tokens: int, dtype: torch.dtype = t
 
 
 def _kv8_maps(maps: torch.Tensor, seq_len: torch.Tensor, n: int):
-    _on_current_device(("maps", maps), ("seq_len", seq_len))
+    _here(maps=maps, seq_len=seq_len)
     if maps.dtype != torch.int32 or maps.dim() != 2 or maps.shape[0] != n or not maps.is_contiguous():
         raise NexusError(EINVAL, "maps must be a contiguous int32 [n_seqs][stride] device tensor")
     if seq_len.dtype != torch.int32 or tuple(seq_len.shape) != (n,) or not seq_len.is_contiguous():
@@ -585,7 +592,7 @@ def _kv8_query(q: torch.Tensor, cc: CKv8Cache, out, workspace):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
-    _on_current_device(("q", q), ("out", out), ("workspace", workspace))
+    _here(q=q, out=out, workspace=workspace)
     return out
 
 
