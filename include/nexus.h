@@ -388,7 +388,11 @@ size_t nexus_kv8_suffix_attn_varlen_workspace(int32_t n_seqs, const int32_t *q_s
 
 /*
  * nexus_decode_attn over an 8-bit cache: q and out are bf16, 16-byte aligned; maps, lengths (0 gives a
- * zero row), softcap and scale as there.  Pages that sequences share are read by each of them.
+ * zero row), softcap and scale as there.  Leading pages that neighbouring sequences of a large launch map alike
+ * (a warm prefix) are read once for several of them; the result of a sequence may then differ in its last
+ * bit from that of a launch without the others.  The workspace is 16-byte aligned; one of fewer bytes than
+ * nexus_kv8_decode_attn_workspace() serves too, down to what the same launch needs without shared pages
+ * (NEXUS_EWORKSPACE below that), which are then cut into fewer ranges or not looked for.
  */
 nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_heads,
                                    const nexus_kv8_cache *cache, const int32_t *maps, int32_t map_stride,

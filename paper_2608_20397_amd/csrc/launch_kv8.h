@@ -50,7 +50,8 @@ struct AttnPlan;
 hipError_t launch_attention_kv8(const AttnLaunch &p, const AttnPlan &plan, hipStream_t stream);
 
 // Decode step over an 8-bit cache (DecodeLaunch::k_scale and v_scale set).
-size_t decode_kv8_workspace_bytes(const DecodeLaunch &p);
+size_t decode_kv8_workspace_bytes(const DecodeLaunch &p);   // all it can use
+size_t decode_kv8_workspace_min(const DecodeLaunch &p);     // without shared pages
 hipError_t launch_decode_kv8(const DecodeLaunch &p, hipStream_t stream);
 
 }  // namespace nexus

@@ -310,9 +310,9 @@ nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_he
   if ((st = decode_launch(n_seqs, n_q_heads, cache, max_seq_len, L))) return st;
   if ((int64_t)map_stride * kPageSize < max_seq_len) return NEXUS_ERANGE;
   if ((int64_t)n_seqs * map_stride >= kMaxElems32) return NEXUS_ESHAPE;
-  const size_t need = decode_kv8_workspace_bytes(L);
-  if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
-    return NEXUS_EWORKSPACE;
+  const size_t need = decode_kv8_workspace_min(L);
+  const bool usable = workspace && (uintptr_t)workspace % 16 == 0;
+  if (need > 0 && (!usable || workspace_bytes < need)) return NEXUS_EWORKSPACE;
   L.q = q;
   L.out = out;
   L.cache_k = cache->k;
@@ -327,7 +327,7 @@ nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_he
   L.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim);
   L.softcap = softcap;
   L.workspace = workspace;
-  L.workspace_bytes = workspace ? workspace_bytes : 0;
+  L.workspace_bytes = usable ? workspace_bytes : 0;
   return from_hip(launch_decode_kv8(L, as_stream(stream)));
 }
 

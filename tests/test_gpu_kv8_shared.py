@@ -1,0 +1,185 @@
+"""Decode over the 8-bit cache where sequences map the same pages, in launches large enough to read those
+together, against 64 bits on the cache's own values.  Slots past a sequence's end hold NaN codes under the NaN
+scale."""
+
+import numpy as np
+import pytest
+import torch
+
+import _kv8 as R
+from paper_2608_20397_amd import nexus as N
+
+pytestmark = pytest.mark.gpu
+
+t = torch.from_numpy
+
+
+def _bound(n, H, D):
+    """A max_seq_len from which on a launch looks for shared pages (half a GiB of codes, if all were as long)."""
+    return -(-2 ** 29 // (n * H * D * 2))
+
+
+def _pool(page_of, lens, H, D, bound, seed):
+    """A one-layer cache and maps [n][pages of bound]: page p of sequence b is the pool's page of the label
+    page_of(b, p); entries past a sequence's pages name its first one."""
+    labels, pages = {}, []
+    for b, m in enumerate(lens):
+        pages.append([labels.setdefault(page_of(b, p), len(labels)) for p in range((m + 15) // 16)])
+    npp = len(labels) + 2
+    cache = R.make_cache(1, npp, H, D, npp, seed=seed)
+    phys = cache.page_map.cpu().numpy()
+    k, v = (R.rows(500 + seed + s, 1, 16 * len(labels), H, D, spread=0.5) for s in (0, 1))
+    N.kv8_splice(cache, N.Block(k, v, 0, 1e4), 0, 0)
+    maps = np.zeros((len(lens), (bound + 15) // 16), np.int32)
+    for b, m in enumerate(lens):
+        own = phys[pages[b]] if m else phys[:1]
+        maps[b] = own[0]
+        maps[b, :len(pages[b])] = own[:len(pages[b])] if m else 0
+        if m % 16:                              # the slots past its end, in a page of its own
+            for x in (cache.k, cache.v):
+                x.view(torch.uint8)[0, int(own[-1]), :, m % 16:] = 0x7F
+            for x in (cache.k_scale, cache.v_scale):
+                x[0, int(own[-1]), :, m % 16:] = 255
+    return cache, maps
+
+
+def _q(n, Hq, D, seed):
+    g = np.random.default_rng([20397, 81, seed])
+    return t(g.standard_normal((n, Hq, D))).to(torch.bfloat16).cuda()
+
+
+def _check(cache, maps, lens, q, cap, got, what):
+    kv = {x: R.values(cache, x)[0] for x in ("k", "v")}
+    D = q.shape[-1]
+    for b, m in enumerate(lens):
+        if m == 0:
+            assert np.all(got[b] == 0), what
+            continue
+        k, v = (R.tokens(kv[x], maps[b], 0, m)[0] for x in ("k", "v"))
+        R.assert_attention(got[b:b + 1], R.attention(R.f64(q)[b:b + 1], k, v, [m], D ** -0.5, cap),
+                           f"{what}: sequence {b} of {m}")
+
+
+def _prefix(n_shared):
+    return lambda b, p: ("all", p) if p < n_shared else (b, p)
+
+
+# sequences, shared pages: less than pay, up to one run's part, more than a run; lengths that end inside the
+# shared pages' last, on it, just past it and far past it
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("D,Hq,H,lens,n_shared", [
+    (128, 10, 2, [4900, 4801, 0, 5300, 4800, 4817, 6001, 4999], 300),
+    (128, 10, 2, [700, 650, 1200, 640, 641], 40),
+    (128, 10, 2, [700, 650, 1200, 640], 20),
+    (128, 16, 1, [900, 1000, 901], 50),
+    (128, 3, 1, [600, 601], 37),
+    (64, 4, 4, [560 + 3 * i for i in range(33)], 35),
+    (64, 16, 2, [5000, 5600, 7000, 5010, 5020], 310),
+    (256, 16, 8, [800, 801, 850, 1000, 803, 804, 0, 2000, 900], 50),
+    (256, 4, 4, [1040] * 17, 65),
+])
+def test_a_shared_prefix(D, Hq, H, lens, n_shared, cap):
+    n = len(lens)
+    bound = max(_bound(n, H, D), max(lens))
+    cache, maps = _pool(_prefix(n_shared), lens, H, D, bound, seed=D + n)
+    q = _q(n, Hq, D, n)
+    got = N.kv8_decode_attn(q, cache, t(maps).cuda(), t(np.array(lens, np.int32)).cuda(), bound, 0, softcap=cap)
+    _check(cache, maps, lens, q, cap, R.f64(got), f"D={D} {n_shared} pages of {n}")
+
+
+def _many(b, p):
+    return ("all", p) if p < 34 else (b, p)
+
+
+def _one_elsewhere(b, p):
+    """Sequence 2 has pages of its own throughout, sequence 4 from page 50 on, sequence 1 page 60 alone."""
+    if p >= 300 or b == 2 or (b == 4 and p >= 50) or (b == 1 and p == 60):
+        return (b, p)
+    return ("all", p)
+
+
+def _two_prefixes(b, p):
+    return (b % 2, p) if p < 280 else ("own", b, p)
+
+
+def _later(b, p):
+    """The first run (256 pages here) is each sequence's own, the pages behind it are shared."""
+    return ("all", p) if 256 <= p < 400 else (b, p)
+
+
+@pytest.mark.parametrize("page_of,n,H,length", [
+    (_many, 64, 8, 600), (_one_elsewhere, 8, 2, 5000), (_two_prefixes, 8, 2, 4600), (_later, 8, 2, 6600),
+])
+def test_what_is_shared_is_found_page_by_page(page_of, n, H, length):
+    """One run a sequence (no merge without shared pages); sequences that share nothing or less than the
+    others; two groups; a run of one's own before a shared one."""
+    D, Hq = 128, H
+    bound = _bound(n, H, D)
+    lens = [length + 7 * b for b in range(n)]
+    cache, maps = _pool(page_of, lens, H, D, bound, seed=n)
+    q = _q(n, Hq, D, n + 1)
+    got = N.kv8_decode_attn(q, cache, t(maps).cuda(), t(np.array(lens, np.int32)).cuda(), bound, 0)
+    _check(cache, maps, lens, q, 0.0, R.f64(got), page_of.__name__)
+
+
+def test_what_is_not_finite_stays_with_its_sequence_and_its_page():
+    """A query with NaN beside finite ones of a group; a value row with inf in a page that two of four share."""
+    D, H, Hq, n = 128, 2, 10, 4
+    lens = [1500, 1480, 1510, 1460]
+    bound = _bound(n, H, D)
+    cache, maps = _pool(lambda b, p: ("all", p) if p < 80 else (b // 2, p) if p < 85 else (b, p), lens, H, D, bound,
+                        seed=3)
+    q = _q(n, Hq, D, 5)
+    run = lambda: R.f64(N.kv8_decode_attn(q, cache, t(maps).cuda(), t(np.array(lens, np.int32)).cuda(), bound, 0))
+    ref = run()
+    _check(cache, maps, lens, q, 0.0, ref, "finite")
+    q[1, 3, 7] = float("nan")
+    got = run()
+    assert np.isnan(got[1, 3]).all()
+    got[1, 3] = ref[1, 3]
+    assert np.array_equal(got, ref)
+    cache.v.view(torch.uint8)[0, int(maps[0, 82]), :, 4] = 0x7F
+    cache.v_scale[0, int(maps[0, 82]), :, 4] = 255
+    got = run()
+    assert np.isnan(got[:2]).all()
+    assert np.array_equal(got[2:], ref[2:])
+
+
+def test_a_smaller_workspace_and_a_replayed_launch():
+    """The least workspace (no shared pages), one byte fewer, all of it; lengths that advance between replays
+    of one launch, from nothing shared to a run of shared pages."""
+    D, H, Hq, n = 128, 2, 10, 8
+    bound = _bound(n, H, D)
+    lens = [4700 + 16 * b for b in range(n)]
+    cache, maps = _pool(_prefix(290), lens, H, D, bound, seed=4)
+    q = _q(n, Hq, D, 6)
+    m, ln = t(maps).cuda(), t(np.array(lens, np.int32)).cuda()
+    full = N.kv8_decode_attn_workspace_bytes(cache, n, Hq, bound)
+    splits = -(-(-(-bound // 16)) // 256)               # runs of 256 pages
+    least = n * Hq * splits * (D + 2) * 4
+    assert full > least
+    ws = lambda nbytes: torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+    for nbytes in (least, least + (full - least) // 2, full):
+        got = N.kv8_decode_attn(q, cache, m, ln, bound, 0, workspace=ws(nbytes))
+        _check(cache, maps, lens, q, 0.0, R.f64(got), f"{nbytes} bytes")
+    with pytest.raises(N.NexusError) as e:
+        N.kv8_decode_attn(q, cache, m, ln, bound, 0, workspace=ws(least - 1))
+    assert e.value.status == N.EWORKSPACE
+    w, out = ws(full), torch.empty_like(q)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        N.kv8_decode_attn(q, cache, m, ln, bound, 0, out=out, workspace=w)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        N.kv8_decode_attn(q, cache, m, ln, bound, 0, out=out, workspace=w)
+    for now in ([400 + b for b in range(n)], lens, [0] + lens[1:], [600] * n, lens):
+        ln.copy_(t(np.array(now, np.int32)))
+        out.fill_(7)
+        g.replay()
+        got = out.clone()
+        eager = N.kv8_decode_attn(q, cache, m, ln, bound, 0)
+        assert torch.equal(got, eager)
+        if now is not lens:
+            continue
+        _check(cache, maps, lens, q, 0.0, R.f64(got), "replayed")
