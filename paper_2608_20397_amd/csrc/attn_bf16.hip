@@ -415,12 +415,21 @@ namespace {
 // workgroups the plan takes to be resident per CU, wave tasks per workgroup, and the plan's time per key
 // of one workgroup (us, measured).  (head_dim 64: three fit a CU.  The plan keeps two, because with three it
 // also cuts short contexts, whose rows then pass through fp16 partials that they had been spared.)
+// One sequence over an 8-bit cache (us_alone > 0): its launches of a workgroup per CU at most are priced by
+// their longest piece, us_alone per key and us_piece for its prologue and epilogue.  (Several sequences
+// priced so got more splits than pay: 16 of 256 queries at depths up to 15233, 32 heads over 8 of 64,
+// 312 -> 321 us.)
 struct KernelShape {
   int qpw, key_tile, wgs_per_cu, waves;
-  double us_per_key;
+  double us_per_key, us_alone = 0, us_piece = 0;
 };
 
 KernelShape kernel_shape(const AttnLaunch &p) {
+  if (p.kv8 && p.n_seqs == 1) {
+    if (p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.043, 0.043, 14.0};
+    if (p.head_dim == 128) return {kQB, 64, 2, kWaves, 0.0285, 0.0169, 4.7};
+    return {kQB, 64, 2, kWaves, 0.0208, 0.0125, 4.7};
+  }
   if (p.kv8 && p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.04};
   if (p.head_dim <= 128) return {kQB, 64, 2, kWaves, 0.03 * p.head_dim / 128.0};   // LDS DMA
   if (p.v_transposed) return {kQB, 32, 1, kWavesWide, 0.04};                       // LDS DMA
@@ -437,7 +446,10 @@ constexpr int kCUs = 256;
 // the latter, causal prefills by the former two) at the kernel's measured time per key of one
 // workgroup (KernelShape), plus, when keys are split, the combine: writing and reading the
 // partials (priced as fp32 rows, split_cost_bytes) at about 4 TB/s and one more launch.  A piece's work is its keys plus a fixed 128 for
-// its prologue and epilogue.
+// its prologue and epilogue.  One sequence over an 8-bit cache: the split term is combine_us_kv8, and
+// launches of a workgroup per CU at most have a rate of their own (KernelShape).  Without both, 40 heads over
+// 8 of 128: 16 queries at depth 2432 23.0 -> 16.8 us, 64 at 4480 28.8 -> 24.3, 192 at 2432 30.3 -> 27.5, 300 at
+// 1500 34.6 -> 29.9, 512 at 4480 65.7 -> 64.5; 32 over 8 of 64: 192 at 4480 31.6 -> 24.6.
 bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
   if (p.n_seqs < 1 || p.n_seqs > kMaxSeqs) return false;
   const int G = p.n_q_heads / p.n_kv_heads;
@@ -510,13 +522,20 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
   auto split_cost_bytes = [&](const AttnSeq &s, int64_t n) {
     return n > 1 ? 8.0 * (double)n * s.len * p.n_q_heads * (p.head_dim + 2) : 0.0;
   };
+  // 8-bit: the combine's launch, a record per split, the fp16 partials' write and read, and a second batch
+  // of its loads beyond 8 splits (measured: 16 to 512 queries at depths of 960 to 4480, 1 to 20 splits)
+  auto combine_us_kv8 = [&](double part_rows, int64_t max_splits) {
+    if (max_splits <= 1) return 0.0;
+    return 3.5 + 0.35 * (double)max_splits + part_rows * (4.0 * p.head_dim + 32.0) / 2.9e6 +
+           (max_splits > 8 ? 4.0 : 0.0);
+  };
   for (int ns = 1; ns <= kMaxRanges; ++ns) {
     int64_t sk = (max_keys + ns - 1) / ns;
     sk = (sk + KT - 1) / KT * KT;
     if (sk > kMaxSplitKeys) continue;
     if (sk < kMinSplitKeysSmall && ns > 1) break;
     int64_t max_splits = 1, n_full = 0, full_len = 0, max_piece = 0, n_pieces = 0;
-    double total = 0.0, combine_bytes = 0.0, ws_need = 0.0;
+    double total = 0.0, combine_bytes = 0.0, part_rows = 0.0, ws_need = 0.0;
     for (int b = 0; b < p.n_seqs; ++b) {
       const AttnSeq &s = p.seqs[b];
       const std::vector<int64_t> &wk = tg_keys[b];
@@ -525,6 +544,7 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
       const int64_t nsb = (keys + skb - 1) / skb;
       max_splits = std::max(max_splits, nsb);
       ws_need += part_bytes(s, nsb);
+      if (nsb > 1) part_rows += (double)nsb * s.len * p.n_q_heads;
       if (nsb > 1)
         combine_bytes += split_cost_bytes(s, nsb) + 2.0 * s.len * p.n_q_heads * p.head_dim;
       // piece j of a task group is non-empty when its keys exceed j * skb, and counts as
@@ -555,7 +575,13 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
     const double rounds_full = (double)((n_full + slots - 1) / slots);
     const double est = std::max({rounds_full * (double)(full_len + kPieceOverhead),
                                  (double)max_piece, total / (double)slots});
-    const double cost = est * ks.us_per_key + (max_splits > 1 ? combine_bytes / 4.0e6 + 8.0 : 0.0);
+    double cost;
+    if (ks.us_alone > 0)
+      cost = (n_pieces <= kCUs ? ks.us_piece + (double)(max_piece - kPieceOverhead) * ks.us_alone
+                               : est * ks.us_per_key) +
+             combine_us_kv8(part_rows, max_splits);
+    else
+      cost = est * ks.us_per_key + (max_splits > 1 ? combine_bytes / 4.0e6 + 8.0 : 0.0);
     if (cost < best_cost - 1e-9) {
       best_cost = cost;
       best_sk = sk;
@@ -599,7 +625,11 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
         const double comb = 8.0 * rows_heads * (p.head_dim + 2) *
                                 (double)(n_a * ns_a + n_b * ns_b) / (double)n_tg +
                             2.0 * rows_heads * p.head_dim;
-        const double cost = est * ks.us_per_key + comb / 4.0e6 + 8.0;
+        const double cost =
+            est * ks.us_per_key +
+            (ks.us_alone > 0 ? combine_us_kv8(rows_heads * (double)(n_a * ns_a + n_b * ns_b) / (double)n_tg,
+                                                std::max(ns_a, ns_b))
+                             : comb / 4.0e6 + 8.0);
         if (cost < best_cost - 1e-9) {
           best_cost = cost;
           two_n_a = n_a;
