@@ -26,10 +26,10 @@
 //     leading pages that those sequences of a group which map the same 32nd page have in common, whole in each,
 //     are read once for all of them: cut into ranges, one for a workgroup of the group, whose partials the
 //     merge adds.  The other pages of each sequence are cut evenly over its workgroups.  Every workgroup finds
-//     this out for itself from the maps (4 to 5 us where pages are shared, 1 to 2 where none are).  32 sequences
-//     of 17473 tokens, 40 heads over 8 of 128: all shared 109 -> 51 us, 14000 tokens 104 -> 85, 8704 tokens 159 ->
-//     131, 4096 tokens 188 -> 172, none 195 -> 196; 64 of them, all shared 198 -> 77; 128 sequences of 4000, none shared
-//     170 -> 172; 48 of 9000 sharing 8000, 16 heads over 8 of 256, capped, 149 -> 88.
+//     this out for itself from the maps (4 to 5 us where pages are shared, 1 to 2 where none are).  Against
+//     every sequence on its own, 32 of 17473 tokens, 40 heads over 8 of 128: all shared 109 -> 48 us, 14000 tokens
+//     104 -> 82, 8704 159 -> 127, 4096 188 -> 166; 64 of them, all shared 198 -> 77; 128 of 4000, none shared 170
+//     -> 171; 48 of 9000 sharing 8000, 16 heads over 8 of 256, capped, 149 -> 88.
 #include "attn_common.h"
 #include "attn_dma.h"
 #include "decode_common.h"
@@ -37,6 +37,7 @@
 #include "launch_kv8.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace nexus {
@@ -528,6 +529,30 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs
   }
 }
 
+// Pages of a run.  A workgroup keeps its CU's memory pipe full by itself, so launches that have a workgroup per
+// (sequence, KV head, query group) for half the CUs or more take whole sequences and need no merge, smaller ones
+// as many runs as make one workgroup per CU (32 sequences of 17473 tokens, 40 heads over 8 of 128: one run 181
+// us, two 186; 24: 154 and 170; 8 of 4000: four runs 17.8, eight 19.3; 2 of 17473: sixteen 19.2, 32 21.5).
+//   * No more than the merge is worth: 8 pages and 0.7 sqrt(pages) a run (one sequence of 17473 tokens over one
+//     head: 23 pages 12.7 us, 12 15.2, 46 14.1; of 70000: 46 19.5, 23 23.6, 92 22.0; of 1000 over 8: 8 pages
+//     8.4, 12 9.1, 32 11.3); one run up to 32 pages, or 96 where there would be two (16 sequences of 1300: 14.0,
+//     two runs 15.0).
+//   * Between 256 and 512, two a CU: runs that fill whole rounds of 512 (36 sequences of 4000 over 8 heads:
+//     three runs 55.6 us, one 66, two 60; 48 of 6000: two 102, one 114, three 111; 56 of 4000: one 82, two 92).
+int kv8_split_pages(const DecodeLaunch &p, int n_qgroups) {
+  const int64_t max_pages = ((int64_t)p.max_len + 15) / 16;
+  const int64_t pairs = (int64_t)p.n_seqs * p.n_kv_heads * n_qgroups;
+  if (max_pages <= 0 || pairs > 512) return decode_split_pages(p.n_seqs, p.n_kv_heads, n_qgroups, p.max_len);
+  int64_t ns;
+  if (pairs > 256)
+    ns = max_pages < 96 || pairs > 416 ? 1 : 3 * pairs > 1024 ? 2 : 3;
+  else
+    ns = max_pages <= (pairs > 85 ? 96 : 32) ? 1 : 256 / pairs;
+  int64_t sp = (max_pages + ns - 1) / ns;
+  if (ns > 1) sp = std::max({sp, (int64_t)8, (int64_t)std::ceil(0.7 * std::sqrt((double)max_pages))});
+  return (int)std::min<int64_t>(sp, kMaxSplitPages);
+}
+
 struct Shape {
   int split_pages, own_splits;         // pages per run, runs of the longest sequence
   int n_groups, group_seqs;            // 0 groups: shared pages are not looked for
@@ -550,7 +575,7 @@ Shape kv8_shape(const DecodeLaunch &p, size_t ws_bytes) {
   Shape s{};
   const int group = p.n_q_heads / p.n_kv_heads;
   const int n_qgroups = (group + 15) / 16;
-  s.split_pages = decode_split_pages(p.n_seqs, p.n_kv_heads, n_qgroups, p.max_len);
+  s.split_pages = kv8_split_pages(p, n_qgroups);
   const int64_t max_pages = ((int64_t)p.max_len + 15) / 16;
   s.own_splits = (int)std::max<int64_t>(1, (max_pages + s.split_pages - 1) / s.split_pages);
   // Non-temporal loads where the codes may pass twice the 256 MB last-level cache and a page is read by one
@@ -619,10 +644,12 @@ hipError_t launch_decode_kv8(const DecodeLaunch &p, hipStream_t stream) {
   const uint32_t gy = (uint32_t)std::min<int64_t>(units8, 32768);
   const int n_hq = p.n_kv_heads * a.n_qgroups;
   const dim3 grid(8 * n_hq, gy, (uint32_t)((units8 + gy - 1) / gy));
-  // 8 waves where the launch has a workgroup per CU or fewer and a run gives each wave two steps or more: 48
-  // sequences of up to 700 tokens, 64 heads of 64 over 2, 10.1 -> 8.9 us; with 512 workgroups 20.6 us
-  // becomes 26.7 (8 sequences of 4000), with 7 pages 6.2 becomes 7.2.  (head_dim 256 would spill.)
-  const bool wide = p.head_dim != 256 && (int64_t)n_hq * p.n_seqs * ns <= 256 && a.split_pages >= 32;
+  // 8 waves where there are fewer workgroups than CUs and their runs give each wave two steps or more (4
+  // sequences of 8000 over 8 heads of 128 in 128 workgroups 24.1 -> 21.2 us, in 256 17.8 -> 19.3; with 7 pages 6.2
+  // becomes 7.2); up to 256 with head_dim 64, whose steps load half as much (32 of 4000: 29.9 -> 24.7), and where
+  // pages may be shared (32 of 17473, all shared: 55 -> 48; none: 181 -> 183).  (head_dim 256 would spill.)
+  const bool wide = p.head_dim != 256 && sh.split_pages >= 32 &&
+                    (int64_t)n_hq * p.n_seqs * ns <= (p.head_dim == 64 || sh.n_groups > 0 ? 256 : 192);
   auto run = [&](auto kernel, int waves) {
     hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a);
     return hipGetLastError();

@@ -103,7 +103,7 @@ def _two_prefixes(b, p):
 
 
 def _later(b, p):
-    """The first run (256 pages here) is each sequence's own, the pages behind it are shared."""
+    """The first pages are each sequence's own, those behind them are shared."""
     return ("all", p) if 256 <= p < 400 else (b, p)
 
 
@@ -112,7 +112,7 @@ def _later(b, p):
 ])
 def test_what_is_shared_is_found_page_by_page(page_of, n, H, length):
     """One run a sequence (no merge without shared pages); sequences that share nothing or less than the
-    others; two groups; a run of one's own before a shared one."""
+    others; two groups; pages of one's own before shared ones."""
     D, Hq = 128, H
     bound = _bound(n, H, D)
     lens = [length + 7 * b for b in range(n)]
@@ -155,10 +155,22 @@ def test_a_smaller_workspace_and_a_replayed_launch():
     q = _q(n, Hq, D, 6)
     m, ln = t(maps).cuda(), t(np.array(lens, np.int32)).cuda()
     full = N.kv8_decode_attn_workspace_bytes(cache, n, Hq, bound)
-    splits = -(-(-(-bound // 16)) // 256)               # runs of 256 pages
-    least = n * Hq * splits * (D + 2) * 4
-    assert full > least
     ws = lambda nbytes: torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+
+    def taken(nbytes):
+        try:
+            N.kv8_decode_attn(q, cache, m, ln, bound, 0, workspace=ws(nbytes))
+        except N.NexusError as e:
+            assert e.status == N.EWORKSPACE
+            return False
+        return True
+
+    low, least = 0, full                                # low is refused, least is taken
+    assert not taken(low) and taken(least)
+    while least - low > 1:
+        mid = (low + least) // 2
+        low, least = (low, mid) if taken(mid) else (mid, least)
+    assert least < full and least % (n * Hq * (D + 2) * 4) == 0
     for nbytes in (least, least + (full - least) // 2, full):
         got = N.kv8_decode_attn(q, cache, m, ln, bound, 0, workspace=ws(nbytes))
         _check(cache, maps, lens, q, 0.0, R.f64(got), f"{nbytes} bytes")
