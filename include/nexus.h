@@ -305,11 +305,11 @@ size_t nexus_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const nexu
  *   k, v              codes [n_layers][n_phys_pages][n_kv_heads][16][head_dim];
  *   k_scale, v_scale  bytes [n_layers][n_phys_pages][n_kv_heads][16].
  * All four pointers are 16-byte aligned (NEXUS_EINVAL); V is row-major; head_dim is 64, 128 or 256
- * (NEXUS_ESHAPE).  A layer may hold any number of bytes (fewer than 2^31 tokens).  Caches of other origin have
- * to keep bytes within [27, 246], or 255 with codes 0x7F.  Slots that no call wrote may hold
- * anything: a call reads only tokens that its lengths name.  The checks of the other calls hold here too
- * (layers, page table entries, page lifetimes); each call is one kernel launch, the attention calls one
- * more where they split the keys.
+ * (NEXUS_ESHAPE).  A layer may hold any number of bytes (fewer than 2^31 tokens and 2^32 rows, NEXUS_ESHAPE).
+ * Caches of other origin have to keep bytes within [27, 246], or 255 with codes 0x7F.  Slots that no call
+ * wrote may hold anything: a call reads only tokens that its lengths name.  The checks of the other calls hold
+ * here too (layers, page table entries, page lifetimes); each call is one kernel launch, the attention calls
+ * one more where they split the keys or look for shared pages.
  */
 typedef struct nexus_kv8_cache {
   void *k;
@@ -388,11 +388,14 @@ size_t nexus_kv8_suffix_attn_varlen_workspace(int32_t n_seqs, const int32_t *q_s
 
 /*
  * nexus_decode_attn over an 8-bit cache: q and out are bf16, 16-byte aligned; maps, lengths (0 gives a
- * zero row), softcap and scale as there.  Leading pages that neighbouring sequences of a large launch map alike
+ * zero row), softcap and scale as there (max_seq_len at most 2^31 - 17, NEXUS_ERANGE; a map row's entries are read,
+ * though not followed, up to max_seq_len's pages).  Leading pages that neighbouring sequences of a large launch map alike
  * (a warm prefix) are read once for several of them; the result of a sequence may then differ in its last
  * bit from that of a launch without the others.  The workspace is 16-byte aligned; one of fewer bytes than
  * nexus_kv8_decode_attn_workspace() serves too, down to what the same launch needs without shared pages
- * (NEXUS_EWORKSPACE below that), which are then cut into fewer ranges or not looked for.
+ * (NEXUS_EWORKSPACE below that), which are then cut into fewer ranges or not looked for.  Fewer sequences
+ * may need more of it, for theirs are cut into more runs: a buffer for batches of several sizes is as
+ * large as the largest of their queries.
  */
 nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_heads,
                                    const nexus_kv8_cache *cache, const int32_t *maps, int32_t map_stride,

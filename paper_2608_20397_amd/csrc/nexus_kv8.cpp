@@ -127,7 +127,7 @@ nexus_status plan_launch(int32_t n_seqs, const int32_t *q_start, const int32_t *
 nexus_status decode_launch(int32_t n_seqs, int32_t n_q_heads, const nexus_kv8_cache *c, int32_t max_seq_len,
                            DecodeLaunch &L) {
   if (n_seqs <= 0) return NEXUS_EINVAL;
-  if (max_seq_len < 0) return NEXUS_ERANGE;
+  if (max_seq_len < 0 || max_seq_len > INT32_MAX - kPageSize) return NEXUS_ERANGE;   // (pages: rounded up)
   if (n_q_heads <= 0 || n_q_heads % c->n_kv_heads) return NEXUS_ESHAPE;
   // grid limits and 32-bit row offsets of q and out
   if (n_seqs > 65535 || n_q_heads > 65535) return NEXUS_ESHAPE;

@@ -161,6 +161,23 @@ def test_decode():
     assert L.nexus_kv8_decode_attn_workspace(1, 4, C.byref(c), -1) == bad
 
 
+def test_decode_length_limit_and_workspaces():
+    """Lengths whose pages cannot be counted in 32 bits are refused; the workspace of large launches, with what
+    shared pages take, stays far below the cache that it serves."""
+    L, bad = N.lib(), (1 << 64) - 1
+    c = _cache(n_phys_pages=1 << 20, n_layers=1, n_kv_heads=8)
+    top = (1 << 31) - 17
+    assert L.nexus_kv8_decode_attn_workspace(1, 8, C.byref(c), top) not in (0, bad)
+    assert L.nexus_kv8_decode_attn_workspace(1, 8, C.byref(c), top + 1) == bad
+    assert decode(c=c, n=1, hq=8, stride=1 << 27, max_len=top + 1) == N.ERANGE
+    for n in (1, 2, 7, 31, 32, 33, 48, 64, 65, 300, 1000):
+        for hq in (8, 40, 128):
+            for length in (1, 513, 17473, 131072):
+                need = L.nexus_kv8_decode_attn_workspace(n, hq, C.byref(c), length)
+                codes = n * length * 8 * 128 * 2
+                assert need != bad and need <= max(codes, 64 << 20), (n, hq, length, need)
+
+
 def test_binding_refuses_host_tensors():
     rows = (1, 4, 2, 16)
     c = N.KV8Cache(torch.empty(*rows, 128, dtype=torch.float8_e4m3fn),
