@@ -13,7 +13,19 @@
 //     and nothing to the others: 255 is its keys' scale operand, which makes its scores NaN; they are masked
 //     like any other, and its values enter the product as zeros.
 //   * Slots past the last key of a workgroup are never read: their rows repeat the last key and are masked.
-// LDS: K row r, 16-byte chunk c at c ^ kswz(r); V (bf16) chunk c at c ^ vswz(r), as the bf16 kernels.
+// LDS: K row r, 16-byte chunk c at c ^ kswz(r); V (bf16) chunk c at vchunk(c, r).
+//
+// What bounds it: the matrix and the vector units, about alike.  1088 queries at depth 16384, 40 heads over 8 of
+// 128: 347 us (1.09 PFLOP/s; the bf16 kernel 347 to 352 on the same boxes, from twice the cache), matrix pipe
+// busy 50% of the cycles, vector instructions issuing in 49% (7.6 of them per MFMA: the softmax and the
+// conversion of V).  Steps that led there from 436 us: the conversion beside the PV products instead of at
+// the end of the iteration; MFMAs and vector work interleaved in the written order; a step without branches
+// for whole, unmasked tiles.  head_dim 64, 16 x 256 queries at depths up to 15233, 32 heads over 8: 305 us, bound
+// by the exponentials (408 before).  head_dim 256, capped, 512 queries at depth 8704, 16 heads over 8: 99 us (149
+// before the lower query terms went to LDS and the kernel took the schedule of the others).
+// 4 waves of 32 queries, two workgroups a CU (head_dim 256: 8 waves, for K and V tiles of twice the width to be
+// read by 8 tasks).  64 queries a wave, which would halve the operand reads, leave one wave a SIMD, and the
+// accumulators then cost a copy per score between the register files.
 #include "attn_common.h"
 #include "attn_dma.h"
 #include "kv8_common.h"
@@ -269,7 +281,7 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   };
   auto row_scales = [&](uint32_t vs, RowScales &rs) {
 #pragma unroll
-    for (int k = 0; k < NVC; ++k) 
+    for (int k = 0; k < NVC; ++k)
       rs.byte[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (vrow + NT / CH * k), (int)vs);
   };
   auto clear_bad = [&](Codes &cd, uint32_t vs, RowScales &rs) {
