@@ -415,20 +415,34 @@ namespace {
 // workgroups the plan takes to be resident per CU, wave tasks per workgroup, and the plan's time per key
 // of one workgroup (us, measured).  (head_dim 64: three fit a CU.  The plan keeps two, because with three it
 // also cuts short contexts, whose rows then pass through fp16 partials that they had been spared.)
-// One sequence over an 8-bit cache (us_alone > 0): its launches of a workgroup per CU at most are priced by
-// their longest piece, us_alone per key and us_piece for its prologue and epilogue.  (Several sequences
-// priced so got more splits than pay: 16 of 256 queries at depths up to 15233, 32 heads over 8 of 64,
-// 312 -> 321 us.)
+// One sequence over an 8-bit cache has prices of its own (KernelShape::alone): launches of a workgroup per CU at
+// most by their longest piece, others by their rounds and their total work.  (Several sequences priced
+// so got more splits than pay: 16 of 256 queries at depths up to 15233, 32 heads over 8 of 64, 312 -> 321 us.)
+struct SplitPrice {
+  double launch, key;            // us of a launch, and per key of a piece
+  double split, per_split;       // the merge, and each partial of a row
+  double per_mb, over8;          // per 10^6 of rows x splits x (4 D + 32), and beyond 8 splits
+};
+
 struct KernelShape {
   int qpw, key_tile, wgs_per_cu, waves;
-  double us_per_key, us_alone = 0, us_piece = 0;
+  double us_per_key;
+  const SplitPrice *alone = nullptr, *beside = nullptr;   // up to a workgroup per CU, and more
 };
 
 KernelShape kernel_shape(const AttnLaunch &p) {
   if (p.kv8 && p.n_seqs == 1) {
-    if (p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.043, 0.043, 14.0};
-    if (p.head_dim == 128) return {kQB, 64, 2, kWaves, 0.0285, 0.0169, 4.7};
-    return {kQB, 64, 2, kWaves, 0.0208, 0.0125, 4.7};
+    // fitted to 3445 launches (1 to 1024 queries at depths of 200 to 40000, 1 to 32 KV heads, 1 to 40 splits): 5% off
+    // in the mean, the splits that they choose 1% slower than the best of all measured
+    static const SplitPrice k64[2] = {{9.8, 0.741 / 64, 0.34, 0.30, 0.469, 2.6},
+                                      {13.2, 0.882 / 64, 0.0, 0.40, 0.384, 0.0}};
+    static const SplitPrice k128[2] = {{9.6, 1.023 / 64, 0.63, 0.28, 0.438, 2.2},
+                                       {8.6, 1.392 / 64, 4.55, 0.34, 0.299, 0.0}};
+    static const SplitPrice k256[2] = {{16.2, 1.371 / 32, 1.28, 0.24, 0.379, 1.3},
+                                       {0.0, 1.392 / 32, 21.9, 0.20, 0.337, 0.0}};
+    if (p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.04, &k256[0], &k256[1]};
+    if (p.head_dim == 128) return {kQB, 64, 2, kWaves, 0.03, &k128[0], &k128[1]};
+    return {kQB, 64, 2, kWaves, 0.015, &k64[0], &k64[1]};
   }
   if (p.kv8 && p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.04};
   if (p.head_dim <= 128) return {kQB, 64, 2, kWaves, 0.03 * p.head_dim / 128.0};   // LDS DMA
@@ -446,10 +460,11 @@ constexpr int kCUs = 256;
 // the latter, causal prefills by the former two) at the kernel's measured time per key of one
 // workgroup (KernelShape), plus, when keys are split, the combine: writing and reading the
 // partials (priced as fp32 rows, split_cost_bytes) at about 4 TB/s and one more launch.  A piece's work is its keys plus a fixed 128 for
-// its prologue and epilogue.  One sequence over an 8-bit cache: the split term is combine_us_kv8, and
-// launches of a workgroup per CU at most have a rate of their own (KernelShape).  Without both, 40 heads over
-// 8 of 128: 16 queries at depth 2432 23.0 -> 16.8 us, 64 at 4480 28.8 -> 24.3, 192 at 2432 30.3 -> 27.5, 300 at
-// 1500 34.6 -> 29.9, 512 at 4480 65.7 -> 64.5; 32 over 8 of 64: 192 at 4480 31.6 -> 24.6.
+// its prologue and epilogue.  One sequence over an 8-bit cache is priced by SplitPrice instead, which took 3.4%
+// off in the mean of 270 shapes (at worst 10% slower: 100 queries at 500, 32 heads over 32 of 128, 17.7 ->
+// 19.6 us).  40 heads over 8 of 128: 192 queries at 2432 30.3 -> 27.5 us, 64 at 4480 28.8 -> 24.3, 16 at 2432 23.0 ->
+// 16.8; 8 over 1: 64 at 16000 49.9 -> 34.4; 32 over 8 of 64: 16 at 16000 46.7 -> 29.9; 16 over 8 of 256: 1024 at
+// 0 65.6 -> 49.6.
 bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
   if (p.n_seqs < 1 || p.n_seqs > kMaxSeqs) return false;
   const int G = p.n_q_heads / p.n_kv_heads;
@@ -522,12 +537,10 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
   auto split_cost_bytes = [&](const AttnSeq &s, int64_t n) {
     return n > 1 ? 8.0 * (double)n * s.len * p.n_q_heads * (p.head_dim + 2) : 0.0;
   };
-  // 8-bit: the combine's launch, a record per split, the fp16 partials' write and read, and a second batch
-  // of its loads beyond 8 splits (measured: 16 to 512 queries at depths of 960 to 4480, 1 to 20 splits)
-  auto combine_us_kv8 = [&](double part_rows, int64_t max_splits) {
-    if (max_splits <= 1) return 0.0;
-    return 3.5 + 0.35 * (double)max_splits + part_rows * (4.0 * p.head_dim + 32.0) / 2.9e6 +
-           (max_splits > 8 ? 4.0 : 0.0);
+  auto split_us = [&](const SplitPrice &s, double keys, double part_rows, int64_t max_splits) {
+    if (max_splits <= 1) return s.launch + s.key * keys;
+    return s.launch + s.key * keys + s.split + s.per_split * (double)max_splits +
+           s.per_mb * part_rows * (4.0 * p.head_dim + 32.0) * 1e-6 + (max_splits > 8 ? s.over8 : 0.0);
   };
   for (int ns = 1; ns <= kMaxRanges; ++ns) {
     int64_t sk = (max_keys + ns - 1) / ns;
@@ -576,12 +589,21 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
     const double est = std::max({rounds_full * (double)(full_len + kPieceOverhead),
                                  (double)max_piece, total / (double)slots});
     double cost;
-    if (ks.us_alone > 0)
-      cost = (n_pieces <= kCUs ? ks.us_piece + (double)(max_piece - kPieceOverhead) * ks.us_alone
-                               : est * ks.us_per_key) +
-             combine_us_kv8(part_rows, max_splits);
-    else
+    if (ks.alone) {
+      const double longest = (double)(max_piece - kPieceOverhead);
+      // (uniform pieces: a short last round takes its time too)
+      const bool uniform = tg_keys[0].front() * 10 >= tg_keys[0].back() * 9;
+      if (n_pieces <= kCUs)
+        cost = split_us(*ks.alone, longest, part_rows, max_splits);
+      else
+        cost = split_us(*ks.beside,
+                        std::max(uniform ? (double)((n_pieces + slots - 1) / slots) * longest
+                                         : std::max(1.0, rounds_full) * longest,
+                                 (total - (double)(n_pieces * kPieceOverhead)) / (double)slots),
+                        part_rows, max_splits);
+    } else {
       cost = est * ks.us_per_key + (max_splits > 1 ? combine_bytes / 4.0e6 + 8.0 : 0.0);
+    }
     if (cost < best_cost - 1e-9) {
       best_cost = cost;
       best_sk = sk;
@@ -626,10 +648,10 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
                                 (double)(n_a * ns_a + n_b * ns_b) / (double)n_tg +
                             2.0 * rows_heads * p.head_dim;
         const double cost =
-            est * ks.us_per_key +
-            (ks.us_alone > 0 ? combine_us_kv8(rows_heads * (double)(n_a * ns_a + n_b * ns_b) / (double)n_tg,
-                                                std::max(ns_a, ns_b))
-                             : comb / 4.0e6 + 8.0);
+            ks.alone ? split_us(*ks.beside, est - (double)kPieceOverhead,
+                                rows_heads * (double)(n_a * ns_a + n_b * ns_b) / (double)n_tg,
+                                std::max(ns_a, ns_b))
+                     : est * ks.us_per_key + comb / 4.0e6 + 8.0;
         if (cost < best_cost - 1e-9) {
           best_cost = cost;
           two_n_a = n_a;
