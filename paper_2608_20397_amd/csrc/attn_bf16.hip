@@ -411,10 +411,6 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(const AttnArgs a, con
 
 namespace {
 
-// Geometry of the kernel that serves a launch: queries per wave task, key tile, how many of its
-// workgroups the plan takes to be resident per CU, wave tasks per workgroup, and the plan's time per key
-// of one workgroup (us, measured).  (head_dim 64: three fit a CU.  The plan keeps two, because with three it
-// also cuts short contexts, whose rows then pass through fp16 partials that they had been spared.)
 // One sequence over an 8-bit cache has prices of its own (KernelShape::alone): launches of a workgroup per CU at
 // most by their longest piece, others by their rounds and their total work.  (Several sequences priced
 // so got more splits than pay: 16 of 256 queries at depths up to 15233, 32 heads over 8 of 64, 312 -> 321 us.)
@@ -424,6 +420,10 @@ struct SplitPrice {
   double per_mb, over8;          // per 10^6 of rows x splits x (4 D + 32), and beyond 8 splits
 };
 
+// Geometry of the kernel that serves a launch: queries per wave task, key tile, how many of its
+// workgroups the plan takes to be resident per CU, wave tasks per workgroup, and the plan's time per key
+// of one workgroup (us, measured).  (head_dim 64: three fit a CU.  The plan keeps two, because with three it
+// also cuts short contexts, whose rows then pass through fp16 partials that they had been spared.)
 struct KernelShape {
   int qpw, key_tile, wgs_per_cu, waves;
   double us_per_key;
@@ -432,8 +432,8 @@ struct KernelShape {
 
 KernelShape kernel_shape(const AttnLaunch &p) {
   if (p.kv8 && p.n_seqs == 1) {
-    // fitted to 3445 launches (1 to 1024 queries at depths of 200 to 40000, 1 to 32 KV heads, 1 to 40 splits): 5% off
-    // in the mean, the splits that they choose 1% slower than the best of all measured
+    // fitted to 3445 launches (1 to 1024 queries at depths of 200 to 40000, 1 to 32 KV heads, 1 to 40 splits): off
+    // by 5% (rms; head_dim 256 10%), the splits that they choose 1% slower than the best of all measured
     static const SplitPrice k64[2] = {{9.8, 0.741 / 64, 0.34, 0.30, 0.469, 2.6},
                                       {13.2, 0.882 / 64, 0.0, 0.40, 0.384, 0.0}};
     static const SplitPrice k128[2] = {{9.6, 1.023 / 64, 0.63, 0.28, 0.438, 2.2},
@@ -459,8 +459,8 @@ constexpr int kCUs = 256;
 // and the rounds that the near-full-length pieces need: uniform suffix shapes are decided by the
 // the latter, causal prefills by the former two) at the kernel's measured time per key of one
 // workgroup (KernelShape), plus, when keys are split, the combine: writing and reading the
-// partials (priced as fp32 rows, split_cost_bytes) at about 4 TB/s and one more launch.  A piece's work is its keys plus a fixed 128 for
-// its prologue and epilogue.  One sequence over an 8-bit cache is priced by SplitPrice instead, which took 3.4%
+// partials (priced as fp32 rows, split_cost_bytes) at about 4 TB/s and one more launch.  A piece's work is its
+// keys plus a fixed 128 for its prologue and epilogue.  One sequence over an 8-bit cache is priced by SplitPrice instead, which took 3.4%
 // off in the mean of 270 shapes (at worst 10% slower: 100 queries at 500, 32 heads over 32 of 128, 17.7 ->
 // 19.6 us).  40 heads over 8 of 128: 192 queries at 2432 30.3 -> 27.5 us, 64 at 4480 28.8 -> 24.3, 16 at 2432 23.0 ->
 // 16.8; 8 over 1: 64 at 16000 49.9 -> 34.4; 32 over 8 of 64: 16 at 16000 46.7 -> 29.9; 16 over 8 of 256: 1024 at

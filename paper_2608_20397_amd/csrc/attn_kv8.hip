@@ -508,7 +508,8 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
         constexpr int NM = 2 * NKB * NDB;     // MFMA m: step m / NDB, features 32 (m % NDB) ..
         auto v_operand = [&](int m) {
           const int db = m % NDB;
-          const char *at = vl + (m / NDB) * 16 * VROWB + (db < NOV ? offv[db % NOV] : offv[db % NOV] ^ (256 + 16 + z));
+          const char *at =
+              vl + (m / NDB) * 16 * VROWB + (db < NOV ? offv[db % NOV] : offv[db % NOV] ^ (256 + 16 + z));
           return tr_read_pair(at, at + 8 * VROWB);
         };
         constexpr int VA = D == 256 ? 1 : 2;  // V operands read ahead

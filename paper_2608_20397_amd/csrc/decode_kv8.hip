@@ -364,8 +364,9 @@ __device__ __forceinline__ void put_part(const DecodeArgs &a, int row, int slot_
   if (f0 == 0) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * slot) = f32x2{m, l};
 }
 
-// The sequences of a group g0 .. g1 - 1 (bits: index in the group) that map one physical page as page p of theirs, whole
-// in each; the largest such set, empty if no two do.  min_whole: the least count of whole pages among them.
+// The sequences of a group g0 .. g1 - 1 (bits: index in the group) that map one physical page as page p of
+// theirs, whole in each; the largest such set, empty if no two do.  min_whole: the least count of whole pages
+// among them.
 __device__ __forceinline__ uint32_t sharers(const DecodeArgs &a, int g0, int g1, int p, int &min_whole) {
   const int lane = threadIdx.x & 63;
   const int s = g0 + lane;
