@@ -71,3 +71,66 @@ def test_decode_of_few_sequences(D, Hq, H, lens):
         kk, vv = (R.tokens(kv[x], maps[b], 0, m)[0] for x in ("k", "v"))
         R.assert_attention(got[b:b + 1], R.attention(R.f64(q)[b:b + 1], kk, vv, [m], D ** -0.5, 0.0),
                            f"D={D} length {m}")
+
+
+@pytest.mark.parametrize("bound", [0, 300, 1 << 21])
+def test_decode_reads_no_page_that_a_length_does_not_name(bound):
+    """Map entries past a sequence's pages are anything at all; a bound of no tokens gives zeros; a bound far above
+    the lengths takes the launches that look for shared pages."""
+    D, H, Hq, n = 128, 2, 8, 4
+    lens = [min(m, bound) for m in (290, 0, 17, 288)]
+    stride = max(1, (bound + 15) // 16)
+    cache = R.make_cache(1, 60, H, D, 60, seed=3)
+    k, v = (R.rows(s, 1, 960, H, D, spread=0.5) for s in (67, 68))
+    N.kv8_splice(cache, N.Block(k, v, 0, 1e4), 0, 0)
+    own = np.random.default_rng(9).permutation(60).astype(np.int32)
+    maps = np.full((n, stride), -2 ** 31, np.int32)
+    maps[:, 1::2] = 2 ** 31 - 1
+    for b, m in enumerate(lens):
+        pages = (m + 15) // 16
+        maps[b, :pages] = own[:pages] if b in (0, 3) else own[30 + b:30 + b + pages]
+    q = torch.from_numpy(np.random.default_rng(10).standard_normal((n, Hq, D))).to(torch.bfloat16).cuda()
+    got = R.f64(N.kv8_decode_attn(q, cache, torch.from_numpy(maps).cuda(),
+                                  torch.from_numpy(np.array(lens, np.int32)).cuda(), bound, 0))
+    kv = {x: R.values(cache, x)[0] for x in ("k", "v")}
+    for b, m in enumerate(lens):
+        if m == 0:
+            assert np.all(got[b] == 0)
+            continue
+        kk, vv = (R.tokens(kv[x], maps[b], 0, m)[0] for x in ("k", "v"))
+        R.assert_attention(got[b:b + 1], R.attention(R.f64(q)[b:b + 1], kk, vv, [m], D ** -0.5, 0.0), f"length {m}")
+
+
+def test_calls_on_two_streams_at_once():
+    """Suffix attention and decode of two caches, side by side with workspaces of their own, against one after
+    the other; codes held as bytes."""
+    D, H, Hq = 128, 8, 40
+    jobs = []
+    for seed in (70, 71):
+        cache = R.make_cache(1, 300, H, D, 300, seed=seed)
+        k, v = (R.rows(seed + s, 1, 4500, H, D, spread=0.5) for s in (0, 100))
+        N.kv8_splice(cache, N.Block(k, v, 0, 1e4), 0, 0)
+        cache = N.KV8Cache(cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale,
+                           cache.page_map, 1e4)
+        q = torch.from_numpy(np.random.default_rng(seed).standard_normal((150, Hq, D))).to(torch.bfloat16).cuda()
+        maps = cache.page_map[:282].view(1, -1).repeat(3, 1).contiguous()
+        lens = torch.tensor([4500, 4001, 77], dtype=torch.int32, device="cuda")
+        cache.pt()                                    # (checks the map: a copy to the host)
+        jobs.append((cache, q, maps, lens))
+
+    def run(job):
+        cache, q, maps, lens = job
+        return [(N.kv8_suffix_attn(q, cache, 0, 4350), N.kv8_decode_attn(q[:3].contiguous(), cache, maps, lens, 4500, 0))
+                for _ in range(4)]
+
+    alone = [run(j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    both = []
+    for s, j in zip(streams, jobs):
+        with torch.cuda.stream(s):
+            both.append(run(j))
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        for (s1, d1), (s2, d2) in zip(a, b):
+            assert torch.equal(s1, s2) and torch.equal(d1, d2)
