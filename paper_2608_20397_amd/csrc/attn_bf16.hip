@@ -411,9 +411,10 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(const AttnArgs a, con
 
 namespace {
 
-// One sequence over an 8-bit cache has prices of its own (KernelShape::alone): launches of a workgroup per CU at
-// most by their longest piece, others by their rounds and their total work.  (Several sequences priced
-// so got more splits than pay: 16 of 256 queries at depths up to 15233, 32 heads over 8 of 64, 312 -> 321 us.)
+// One sequence over an 8-bit cache, and several of head_dim 256, have prices of their own (KernelShape::alone):
+// launches of a workgroup per CU at most by their longest piece, others by their rounds and their total work.
+// (Several sequences of fewer dimensions priced so got more splits than pay: 8 of 192 queries at depths up to
+// 8177, 40 heads over 8 of 128, 180 -> 193 us; 4 of 192 at 2000 and more, 16 over 8 of 256, 95 -> 73.)
 struct SplitPrice {
   double launch, key;            // us of a launch, and per key of a piece
   double split, per_split;       // the merge, and each partial of a row
@@ -431,7 +432,7 @@ struct KernelShape {
 };
 
 KernelShape kernel_shape(const AttnLaunch &p) {
-  if (p.kv8 && p.n_seqs == 1) {
+  if (p.kv8 && (p.n_seqs == 1 || p.head_dim == 256)) {
     // fitted to 3445 launches (1 to 1024 queries at depths of 200 to 40000, 1 to 32 KV heads, 1 to 40 splits): off
     // by 5% (rms; head_dim 256 10%), the splits that they choose 1% slower than the best of all measured
     static const SplitPrice k64[2] = {{9.8, 0.741 / 64, 0.34, 0.30, 0.469, 2.6},
@@ -444,7 +445,6 @@ KernelShape kernel_shape(const AttnLaunch &p) {
     if (p.head_dim == 128) return {kQB, 64, 2, kWaves, 0.03, &k128[0], &k128[1]};
     return {kQB, 64, 2, kWaves, 0.015, &k64[0], &k64[1]};
   }
-  if (p.kv8 && p.head_dim == 256) return {kQB, 32, 1, kWavesWide, 0.04};
   if (p.head_dim <= 128) return {kQB, 64, 2, kWaves, 0.03 * p.head_dim / 128.0};   // LDS DMA
   if (p.v_transposed) return {kQB, 32, 1, kWavesWide, 0.04};                       // LDS DMA
   return {kQB, 32, 1, kWaves, 0.06};
@@ -460,11 +460,12 @@ constexpr int kCUs = 256;
 // the latter, causal prefills by the former two) at the kernel's measured time per key of one
 // workgroup (KernelShape), plus, when keys are split, the combine: writing and reading the
 // partials (priced as fp32 rows, split_cost_bytes) at about 4 TB/s and one more launch.  A piece's work is its
-// keys plus a fixed 128 for its prologue and epilogue.  One sequence over an 8-bit cache is priced by SplitPrice instead, which took 3.4%
-// off in the mean of 270 shapes (at worst 10% slower: 100 queries at 500, 32 heads over 32 of 128, 17.7 ->
-// 19.6 us).  40 heads over 8 of 128: 192 queries at 2432 30.3 -> 27.5 us, 64 at 4480 28.8 -> 24.3, 16 at 2432 23.0 ->
-// 16.8; 8 over 1: 64 at 16000 49.9 -> 34.4; 32 over 8 of 64: 16 at 16000 46.7 -> 29.9; 16 over 8 of 256: 1024 at
-// 0 65.6 -> 49.6.
+// keys plus a fixed 128 for its prologue and epilogue.
+// One sequence over an 8-bit cache (and several of head_dim 256) is priced by SplitPrice instead, which took
+// 3.4% off in the mean of 270 shapes (at worst 10% slower: 100 queries at depth 500, 32 heads over 32 of 128,
+// 17.7 -> 19.6 us).  40 heads over 8 of 128: 192 queries at 2432 30.3 -> 27.5 us, 64 at 4480 28.8 -> 24.3, 16 at
+// 2432 23.0 -> 16.8; 8 over 1: 64 at 16000 49.9 -> 34.4; 32 over 8 of 64: 16 at 16000 46.7 -> 29.9; 16 over 8 of
+// 256: 1024 at 0 65.6 -> 49.6, 20 sequences of one query at up to 9530 195 -> 173.
 bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
   if (p.n_seqs < 1 || p.n_seqs > kMaxSeqs) return false;
   const int G = p.n_q_heads / p.n_kv_heads;
@@ -592,7 +593,7 @@ bool make_plan(const AttnLaunch &p, AttnPlan &plan) {
     if (ks.alone) {
       const double longest = (double)(max_piece - kPieceOverhead);
       // (uniform pieces: a short last round takes its time too)
-      const bool uniform = tg_keys[0].front() * 10 >= tg_keys[0].back() * 9;
+      const bool uniform = range_major || tg_keys[0].front() * 10 >= tg_keys[0].back() * 9;
       if (n_pieces <= kCUs)
         cost = split_us(*ks.alone, longest, part_rows, max_splits);
       else
