@@ -103,35 +103,28 @@ __global__ __launch_bounds__(D == 256 ? 512 : 256, D == 64 ? 3 : 2) void attn_kv
   {
     const int qi = min(q0 + j, sp.len - 1);
     const uint16_t *qrow = a.q + ((int64_t)(sp.q_start + qi) * a.n_q_heads + qhead) * D;
-    u32x4 raw[NS2][4];
-    uint32_t am = 0;
+    uint32_t raw[16 * NS2];
 #pragma unroll
     for (int s = 0; s < NS2; ++s)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        raw[s][c] = active ? *reinterpret_cast<const u32x4 *>(qrow + 64 * s + 32 * hh + 8 * c)
-                           : u32x4{0u, 0u, 0u, 0u};
+        const u32x4 x = active ? *reinterpret_cast<const u32x4 *>(qrow + 64 * s + 32 * hh + 8 * c)
+                               : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          am = max(am, max((raw[s][c][e] << 16) & 0x7FFF0000u, raw[s][c][e] & 0x7FFF0000u));
+        for (int w = 0; w < 4; ++w) raw[16 * s + 4 * c + w] = x[w];
       }
+    uint32_t am = amax_bits_bf16<16 * NS2>(raw);
     const auto r = __builtin_amdgcn_permlane32_swap(am, am, false, false);
     am = max((uint32_t)r[0], (uint32_t)r[1]);
-    const bool bad = am >= 0x7F800000u;
     const int e = row_exp(am);
-    qscale = (e + 127) | (e + 127 - 4) << 8;
+    qscale = am >= 0x7F800000u ? (int)(kBadScale | kBadScale << 8) : (e + 127) | (e + 127 - 4) << 8;
+    clamp_query<16 * NS2>(raw, am);
 #pragma unroll
     for (int s = 0; s < NS2; ++s)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float x[8];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          x[2 * w] = __uint_as_float(raw[s][c][w] << 16);
-          x[2 * w + 1] = __uint_as_float(raw[s][c][w] & 0xFFFF0000u);
-        }
         uint32_t hi[2], lo[2];
-        split_query<8>(x, e, bad, hi, lo);
+        split_query<4>(raw + 16 * s + 4 * c, e, hi, lo);
         if (s < NSR) {
           qhi[s % NSR][2 * c] = hi[0];
           qhi[s % NSR][2 * c + 1] = hi[1];

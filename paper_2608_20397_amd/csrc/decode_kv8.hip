@@ -83,41 +83,29 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, int h, char *smem, c
     const int row = row_of(16 * cb + qn);
     const bool q_ok = row >= 0;
     const uint16_t *qrow = reinterpret_cast<const uint16_t *>(a.q) + (size_t)max(row, 0) * D;
-    u32x4 raw[KS][4];
-    uint32_t am = 0;
+    constexpr int QW = D == 64 ? 8 : 16 * KS;      // words of a lane
+    uint32_t raw[QW];
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+    for (int i = 0; i < QW / 4; ++i) {
+      const int f = D == 64 ? 16 * grp + 8 * i : 128 * (i >> 2) + 32 * grp + 8 * (i & 3);
+      const u32x4 x = q_ok ? *reinterpret_cast<const u32x4 *>(qrow + f) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int f = D == 64 ? 16 * grp : 128 * s + 32 * grp;
-        if (D == 64 && c >= 2) {
-          raw[s][c] = u32x4{0u, 0u, 0u, 0u};
-          continue;
-        }
-        raw[s][c] = q_ok ? *reinterpret_cast<const u32x4 *>(qrow + f + 8 * c) : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          am = max(am, max((raw[s][c][e] << 16) & 0x7FFF0000u, raw[s][c][e] & 0x7FFF0000u));
-      }
+      for (int w = 0; w < 4; ++w) raw[4 * i + w] = x[w];
+    }
+    uint32_t am = amax_bits_bf16<QW>(raw);
     am = max(am, (uint32_t)__shfl_xor((int)am, 16));
     am = max(am, (uint32_t)__shfl_xor((int)am, 32));
     const bool bad = am >= 0x7F800000u;
     const int e = row_exp(am);
+    clamp_query<QW>(raw, am);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float x[8];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          x[2 * w] = __uint_as_float(raw[s][c][w] << 16);
-          x[2 * w + 1] = __uint_as_float(raw[s][c][w] & 0xFFFF0000u);
-        }
+      for (int c = 0; c < (D == 64 ? 2 : 4); ++c) {
         uint32_t hi[2], lo[2];
-        split_query<8>(x, e, bad, hi, lo);
+        split_query<4>(raw + 16 * s + 4 * c, e, hi, lo);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          if (D == 64 && c >= 2) continue;
           qhi[cb][s][2 * c + w] = hi[w];
           if (D == 64)
             qhi[cb][s][4 + 2 * c + w] = lo[w];
@@ -125,8 +113,8 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, int h, char *smem, c
             qlo[cb][s][2 * c + w] = lo[w];
         }
       }
-    qs_lo[cb] = e + 127 - 4;
-    qs_hi[cb] = D == 64 && grp >= 2 ? qs_lo[cb] : e + 127;
+    qs_lo[cb] = bad ? (int)kBadScale : e + 127 - 4;
+    qs_hi[cb] = bad || (D == 64 && grp >= 2) ? qs_lo[cb] : e + 127;
   }
   __syncthreads();   // pgs[]
 
