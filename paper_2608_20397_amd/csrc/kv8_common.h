@@ -112,9 +112,9 @@ __device__ __forceinline__ u32x2 codes_to_bf16(uint32_t w, float scale) {
 // takes the upper 4 and the remainder needs no more than 4.  Two fp8 products with keys as they are
 // stored then give the bf16 product at the matrix cores' same cost, with no conversion of the keys and
 // half the bytes read from LDS.  x: W words of bf16 pairs (a multiple of 2); e: of the whole row (row_exp), whose
-// magnitudes stay below 448 * 2^e (clamp_query).  In a row that is not finite, what is becomes NaN through the
-// scale byte kBadScale, not here.  (The conversions scale by themselves, 7 instructions for 2 elements; scaled, clamped
-// and converted apart, 16, one query over 16 keys took 10.7 us at head_dim 256 instead of 9.1, at 128 7.7 for 7.0.)
+// magnitudes stay below 448 * 2^e (clamp_query).  A row that is not finite becomes NaN through the scale byte
+// kBadScale, not here.  (The conversions scale by themselves, 7 instructions for 2 elements; scaled, clamped and
+// converted apart, 16, one query over 16 keys took 10.7 us at head_dim 256 instead of 9.1, at 128 7.7 for 7.0.)
 template <int W>
 __device__ __forceinline__ void split_query(const uint32_t *x, int e, uint32_t *hi, uint32_t *lo) {
   const float s = exp2i(e), sl = exp2i(e - 4);
