@@ -16,8 +16,8 @@
 // LDS: K row r, 16-byte chunk c at c ^ kswz(r); V (bf16) chunk c at vchunk(c, r).
 //
 // What bounds it: the matrix and the vector units, about alike.  1088 queries at depth 16384, 40 heads over 8 of
-// 128: 347 us (1.09 PFLOP/s; the bf16 kernel 347 to 352 on the same cards, from twice the cache), matrix pipe
-// busy 50% of the cycles, vector instructions issuing in 49% (7.6 of them per MFMA: the softmax and the
+// 128: 347 to 359 us (1.05 to 1.09 PFLOP/s; the bf16 kernel 343 to 357 on the same cards, from twice the cache), matrix pipe
+// busy 50% of the cycles, vector instructions issuing in 48% (7.5 of them per MFMA: the softmax and the
 // conversion of V).  Steps that led there from 436 us: the conversion beside the PV products instead of at
 // the end of the iteration; MFMAs and vector work interleaved in the written order; a step without branches
 // for whole, unmasked tiles.  head_dim 64, 16 x 256 queries at depths up to 15233, 32 heads over 8: 305 us, bound
