@@ -16,9 +16,9 @@
 // LDS: K row r, 16-byte chunk c at c ^ kswz(r); V (bf16) chunk c at vchunk(c, r).
 //
 // What bounds it: the matrix and the vector units, about alike.  1088 queries at depth 16384, 40 heads over 8 of
-// 128: 347 to 359 us (1.05 to 1.09 PFLOP/s; the bf16 kernel 343 to 357 on the same cards, from twice the cache), matrix pipe
-// busy 50% of the cycles, vector instructions issuing in 48% (7.5 of them per MFMA: the softmax and the
-// conversion of V).  Steps that led there from 436 us: the conversion beside the PV products instead of at
+// 128: 347 to 359 us (1.05 to 1.09 PFLOP/s; the bf16 kernel 343 to 357 on the same cards, from twice the
+// cache), matrix pipe busy 50% of the cycles, vector instructions issuing in 48% (7.5 of them per MFMA: the
+// softmax and the conversion of V).  Steps that led there from 436 us: the conversion beside the PV products instead of at
 // the end of the iteration; MFMAs and vector work interleaved in the written order; a step without branches
 // for whole, unmasked tiles.  head_dim 64, 16 x 256 queries at depths up to 15233, 32 heads over 8: 305 us, bound
 // by the exponentials (408 before).  head_dim 256, capped, 512 queries at depth 8704, 16 heads over 8: 99 us (149

@@ -477,23 +477,35 @@ class KV8Cache:
         shape = k.shape
         if len(shape) != 5 or shape[3] != PAGE:
             raise NexusError(ESHAPE, "cache k must be [L][pages][H][16][D]")
-        _here(cache_k=k, cache_v=v, k_scale=ks, v_scale=vs, page_map=self.page_map)
-        for t in (k, v):
-            if t.dtype != torch.float8_e4m3fn and t.dtype != torch.uint8:
-                raise NexusError(EDTYPE, f"cache k/v: unsupported dtype {t.dtype}")
-            if t.shape != shape or not t.is_contiguous():
-                raise NexusError(ESHAPE, f"cache k/v must be contiguous [L][pages][H][16][D], got {tuple(t.shape)}")
-        for t in (ks, vs):
-            if t.dtype != torch.uint8:
-                raise NexusError(EDTYPE, f"k_scale/v_scale: unsupported dtype {t.dtype}")
-            if t.shape != shape[:4] or not t.is_contiguous():
-                raise NexusError(ESHAPE, f"k_scale/v_scale must be contiguous [L][pages][H][16], got {tuple(t.shape)}")
+        if not _all_here(k, v, ks, vs, self.page_map):
+            _here(cache_k=k, cache_v=v, k_scale=ks, v_scale=vs, page_map=self.page_map)
+        kd, vd = k.dtype, v.dtype
+        if (kd != torch.float8_e4m3fn and kd != torch.uint8) or (vd != torch.float8_e4m3fn and vd != torch.uint8):
+            raise NexusError(EDTYPE, f"cache k/v: unsupported dtype {kd}, {vd}")
+        if ks.dtype != torch.uint8 or vs.dtype != torch.uint8:
+            raise NexusError(EDTYPE, f"k_scale/v_scale: unsupported dtype {ks.dtype}, {vs.dtype}")
+        if v.shape != shape or not (k.is_contiguous() and v.is_contiguous()):
+            raise NexusError(ESHAPE, f"cache k/v must be contiguous [L][pages][H][16][D], got {tuple(shape)}, "
+                                     f"{tuple(v.shape)}")
+        rows = shape[:4]
+        if ks.shape != rows or vs.shape != rows or not (ks.is_contiguous() and vs.is_contiguous()):
+            raise NexusError(ESHAPE, f"k_scale/v_scale must be contiguous [L][pages][H][16], got "
+                                     f"{tuple(ks.shape)}, {tuple(vs.shape)}")
         L, npp, H, P, D = shape
         return CKv8Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), L, npp, P, H, D,
                          self.rope_style, self.rope_base)
 
     def pt(self) -> CPageTable:
         return _checked_map(self, self.k, self.page_map)
+
+
+def _all_here(*tensors) -> bool:
+    """Whether the given tensors (None among them) are all on the current device."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            return False
+    return dev >= 0 and dev == torch.cuda.current_device()
 
 
 def _here(**tensors):
@@ -516,7 +528,8 @@ def _kv8_rows(cc: CKv8Cache, k: torch.Tensor, v: torch.Tensor):
         raise NexusError(ESHAPE, "k/v must be contiguous [L][T][H][D] with the cache's L, H and D")
     if v.dtype != k.dtype:
         raise NexusError(EDTYPE, "k and v dtypes differ")
-    _here(k=k, v=v)
+    if not _all_here(k, v):
+        _here(k=k, v=v)
     return shape[1], _dtype_code(k)
 
 
@@ -571,16 +584,18 @@ def kv8_read(cache: KV8Cache, offset: int, n_tokens: int, dtype: torch.dtype = t
 
 
 def _kv8_maps(maps: torch.Tensor, seq_len: torch.Tensor, n: int):
-    _here(maps=maps, seq_len=seq_len)
+    if not _all_here(maps, seq_len):
+        _here(maps=maps, seq_len=seq_len)
     if maps.dtype != torch.int32 or maps.dim() != 2 or maps.shape[0] != n or not maps.is_contiguous():
         raise NexusError(EINVAL, "maps must be a contiguous int32 [n_seqs][stride] device tensor")
-    if seq_len.dtype != torch.int32 or tuple(seq_len.shape) != (n,) or not seq_len.is_contiguous():
+    if seq_len.dtype != torch.int32 or seq_len.dim() != 1 or seq_len.shape[0] != n or not seq_len.is_contiguous():
         raise NexusError(EINVAL, "seq_len must be a contiguous int32 [n_seqs] device tensor")
 
 
 def _kv8_query(q: torch.Tensor, cc: CKv8Cache, out, workspace):
     """Checks q [rows][n_q_heads][D] (bf16), out and workspace; returns out."""
-    if q.dim() != 3 or q.shape[2] != cc.head_dim:
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != cc.head_dim:
         raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
     if not q.is_contiguous():
         raise NexusError(EINVAL, "q must be contiguous")
@@ -592,7 +607,8 @@ def _kv8_query(q: torch.Tensor, cc: CKv8Cache, out, workspace):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
-    _here(q=q, out=out, workspace=workspace)
+    if not _all_here(q, out, workspace):
+        _here(q=q, out=out, workspace=workspace)
     return out
 
 
