@@ -357,8 +357,9 @@ nexus_status nexus_kv8_splice(const nexus_kv8_cache *cache, const nexus_page_tab
 /*
  * Read logical tokens [offset, offset + n_tokens) back as values: k and v receive
  * [n_layers][n_tokens][n_kv_heads][head_dim] of `dtype`, the layout of a block, keys as they are rotated in
- * the cache.  Splicing what was read gives the same codes and scales when nothing rotates it.  Checks as
- * nexus_kv8_append.
+ * the cache.  Splicing what was read gives the same values when nothing rotates it, and the same codes and
+ * scales but for rows whose largest code is 224, half the largest there is: their codes come out doubled
+ * under a scale byte one less (which stays so from then on).  Checks as nexus_kv8_append.
  */
 nexus_status nexus_kv8_read(const nexus_kv8_cache *cache, const nexus_page_table *pt, int64_t offset,
                             int32_t n_tokens, int32_t dtype, void *k, void *v, void *stream);
