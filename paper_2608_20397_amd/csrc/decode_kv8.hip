@@ -78,6 +78,7 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, int h, char *smem, c
   // ---- the queries (columns without a row are zero)
   i32x8 qhi[NCB][KS], qlo[NCB][KS];
   int qs_hi[NCB], qs_lo[NCB];
+  float qmul[NCB];         // from a product with a key's value to log2 units (CAP: to the cap's argument)
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
     const int row = row_of(16 * cb + qn);
@@ -113,8 +114,14 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, int h, char *smem, c
             qlo[cb][s][2 * c + w] = lo[w];
         }
       }
-    qs_lo[cb] = bad ? (int)kBadScale : e + 127 - 4;
-    qs_hi[cb] = bad || (D == 64 && grp >= 2) ? qs_lo[cb] : e + 127;
+    // The keys' scales come after the sum over features, which is at most 256 * 448 * 448 * 2^e = 2^(e + 25.6): of
+    // queries past 2^96 * 448 a part of the scale, 2^32, waits for them
+    const bool large = e > 96;
+    const int eq = e + 127 - (large ? 32 : 0);
+    qs_lo[cb] = bad ? (int)kBadScale : eq - 4;
+    qs_hi[cb] = bad || (D == 64 && grp >= 2) ? qs_lo[cb] : eq;
+    qmul[cb] = CAP ? a.cap_in : a.scale_log2;
+    if (large) qmul[cb] = fminf(qmul[cb] * 0x1p32f, 3e38f);
   }
   __syncthreads();   // pgs[]
 
@@ -191,7 +198,8 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, int h, char *smem, c
         for (int i = 0; i < 4; ++i) {
           const bool seen = 4 * grp + i < keys[pp] && (pp == 0 || two);
           const float kf = scale_value(pr.pg[pp].ks >> (8 * i) & 255);
-          const float v = CAP ? a.cap_out * tanh_fast(s[i] * kf * a.cap_in) : s[i] * kf * a.scale_log2;
+          const float u = s[i] * kf * qmul[cb];
+          const float v = CAP ? a.cap_out * tanh_fast(u) : u;
           x[4 * pp + i] = seen ? v : -INFINITY;
           vf[4 * pp + i] = seen ? scale_value(pr.pg[pp].vs >> (8 * i) & 255) : 0.f;
         }
