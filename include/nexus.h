@@ -298,10 +298,11 @@ size_t nexus_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const nexu
  *   code    x / 2^e rounded to the nearest E4M3 value, ties to even, at most 448 in magnitude;
  *   value   code * 2^e: exact in bf16 and in f32;
  *   byte    e + 127.
- * An element is at most 2^-4 of its magnitude from its value where it is at least 2^-14 of amax, and at most
- * 2^-18 of amax below that.  Rows below 2^-109 become zeros.  A row with an element that is not finite
- * becomes NaN as a whole (byte 255, codes 0x7F): a query that sees its key or value gets NaN, the
- * other queries nothing of it.
+ * An element is off by at most 2^-4 of its magnitude or half the smallest code's step, 2^(e - 10), whichever is
+ * more.  With amax from 2^-92 to 448 * 2^119 that is 2^-4 of its magnitude down to 2^-13.8 of amax, and 2^-17.8 of
+ * amax below.  Rows smaller than that have the step of e = -100 (magnitudes up to 2^-110 become zeros);
+ * magnitudes past 448 * 2^119 become that.  A row with an element that is not finite becomes NaN as a whole
+ * (byte 255, codes 0x7F): a query that sees its key or value gets NaN, the other queries nothing of it.
  *   k, v              codes [n_layers][n_phys_pages][n_kv_heads][16][head_dim];
  *   k_scale, v_scale  bytes [n_layers][n_phys_pages][n_kv_heads][16].
  * All four pointers are 16-byte aligned (NEXUS_EINVAL); V is row-major; head_dim is 64, 128 or 256
@@ -367,8 +368,8 @@ nexus_status nexus_kv8_read(const nexus_kv8_cache *cache, const nexus_page_table
 /*
  * nexus_suffix_attn and nexus_suffix_attn_varlen over an 8-bit cache: q and out are bf16, 16-byte
  * aligned; layouts, positions, masks, softcap, scale, plan and workspace rules (16-byte aligned) as there.
- * Scores are exact products of q with the keys' values (to 2^-22 of the largest |q| of a row),
- * accumulated in fp32; probabilities are rounded to bf16 for their product with the values.
+ * Scores are exact products of q with the keys' values, accumulated in fp32 (an element of q below 2^-13.8 of its
+ * row's largest is held to 2^-21.8 of that, one past 448 * 2^119 counts as that); probabilities are rounded to bf16 for their product with the values.
  * The rows of the sequences of one launch must not overlap (NEXUS_EINVAL).
  */
 nexus_status nexus_kv8_suffix_attn(const void *q, int32_t n_s, int32_t n_q_heads,

@@ -5,8 +5,9 @@
 // amax <= 448 * 2^e, held within [kMinExp, kMaxExp].  The scale is a power of two because a code times it
 // is then exact in bf16: what the attention multiplies is what a read returns, and the scale costs no
 // instruction (the conversion to bf16 and the scaled MFMA both take it).  Against a scale amax / 448
-// this loses nothing in the codes' normal range, 2^-14 of the row's largest element and up, where a
-// code's relative error is that of its three mantissa bits whatever the scale.
+// this loses nothing in the codes' normal range, from 2^-6 2^e up, where a code's relative error is that of its
+// three mantissa bits whatever the scale.  (amax > 224 * 2^e, so that range begins below 2^-13.8 of amax, and
+// what lies under it is off by at most 2^-10 2^e < 2^-17.8 of amax.)
 #pragma once
 
 #include "device_common.h"
@@ -108,8 +109,8 @@ __device__ __forceinline__ u32x2 codes_to_bf16(uint32_t w, float scale) {
 }
 
 // A row's part of a bf16 query as two E4M3 terms, q = (hi + lo / 16) 2^e exactly where |q| is at least
-// 2^-14 of the row's largest magnitude and to 2^-22 of that below: a bf16 has 8 significant bits, hi
-// takes the upper 4 and the remainder needs no more than 4.  Two fp8 products with keys as they are
+// 2^-6 2^e, which is below 2^-13.8 of the row's largest magnitude, and to 2^-14 2^e, 2^-21.8 of that, below: a bf16
+// has 8 significant bits, hi takes the upper 4 and the remainder needs no more than 4.  Two fp8 products with keys as they are
 // stored then give the bf16 product at the matrix cores' same cost, with no conversion of the keys and
 // half the bytes read from LDS.  x: W words of bf16 pairs (a multiple of 2); e: of the whole row (row_exp), whose
 // magnitudes stay below 448 * 2^e (clamp_query).  A row that is not finite becomes NaN through the scale byte
