@@ -69,3 +69,21 @@ def test_plans_of_long_contexts(harness):
         assert plan is not None, launch
         _check(launch, plan)
     assert [p["range_major"] for p in plans[-3:]] == [0, 1, 0]
+
+
+def test_the_plan_of_several_sequences_does_not_depend_on_their_order(harness):
+    """A sequence keeps its cut wherever it stands, a prefill beside suffixes among them."""
+    r = np.random.default_rng([20397, 94])
+    launches = []
+    for _ in range(150):
+        seqs = [(int(r.integers(64, 2048)), 0)]
+        seqs += [(int(2 ** r.uniform(0, 9)), int(2 ** r.uniform(9, 14))) for _ in range(int(r.integers(1, 6)))]
+        hkv = int(r.choice([1, 2, 8]))
+        for d in (64, 128, 256):
+            launches += [_launch(hkv * 2, hkv, d, *seqs), _launch(hkv * 2, hkv, d, *seqs[::-1])]
+    plans = _plans(harness, launches)
+    for i in range(0, len(launches), 2):
+        cuts = [sorted((s["len"], s["n_past"], u[5], u[6]) for s in p["seqs"] for u in p["unit"] if u[1] == s["b"])
+                for p in plans[i:i + 2]]
+        assert cuts[0] == cuts[1], launches[i]
+        assert plans[i]["ws"] == plans[i + 1]["ws"]
