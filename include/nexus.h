@@ -397,7 +397,8 @@ size_t nexus_kv8_suffix_attn_varlen_workspace(int32_t n_seqs, const int32_t *q_s
  * nexus_kv8_decode_attn_workspace() serves too, down to what the same launch needs without shared pages
  * (NEXUS_EWORKSPACE below that), which are then cut into fewer ranges or not looked for.  Fewer sequences
  * may need more of it, for theirs are cut into more runs: a buffer for batches of several sizes is as
- * large as the largest of their queries.
+ * large as the largest of their queries.  A launch is cut for sequences of about max_seq_len tokens each, so
+ * the longest one decides its time, and the shortest of those that share pages how many are read together.
  */
 nexus_status nexus_kv8_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_heads,
                                    const nexus_kv8_cache *cache, const int32_t *maps, int32_t map_stride,

@@ -8,7 +8,9 @@
 //     two E4M3 terms hi + lo / 16 (split_query), whose products cost what one bf16 product does; the token's
 //     scale byte is the instruction's own operand.  K tiles travel global -> LDS by DMA, 1 byte an element.
 //   * V is converted to bf16 on its way to LDS, its scale applied by the conversion: exact.  P is rounded to
-//     bf16 as in the bf16 kernels and the PV product is theirs (transposed LDS reads, 32x32x16 MFMA).
+//     bf16, which the matrix instruction takes beside such a V, and the PV product is the bf16 kernels' (transposed
+//     LDS reads, 32x32x16 MFMA).  The row sum adds the rounded values, so that the weights sum to one.  Against 64
+//     bits the outputs are off by 1.8e-3 (relative, rms), 1.7e-3 of it the rounding of the results themselves.
 //   * A token whose key or value row is not finite (scale byte 255) gives NaN to the queries that see it
 //     and nothing to the others: 255 is its keys' scale operand, which makes its scores NaN; they are masked
 //     like any other, and its values enter the product as zeros.
@@ -20,9 +22,12 @@
 // cache), matrix pipe busy 50% of the cycles, vector instructions issuing in 48% (7.5 of them per MFMA: the
 // softmax and the conversion of V).  Steps that led there from 436 us: the conversion beside the PV products instead of at
 // the end of the iteration; MFMAs and vector work interleaved in the written order; a step without branches
-// for whole, unmasked tiles.  head_dim 64, 16 x 256 queries at depths up to 15233, 32 heads over 8: 305 us, bound
-// by the exponentials (408 before).  head_dim 256, capped, 512 queries at depth 8704, 16 heads over 8: 99 us (149
-// before the lower query terms went to LDS and the kernel took the schedule of the others).
+// for whole, unmasked tiles.  head_dim 64, 16 x 256 queries at depths up to 15233, 32 heads over 8: 305 us
+// (408 before), vector instructions in 66% and MFMA in 40% of the cycles: a score has half the products of
+// head_dim 128 and the same exponential, and of 2560 workgroups, 10 a CU, three fit, so that the last round is a third
+// full.  head_dim 256, capped, 512 queries at depth 8704, 16 heads over 8: 99 us (149
+// before the lower query terms went to LDS and the kernel took the schedule of the others): one round of 256
+// workgroups, matrix pipe busy 32% and vector instructions issuing in 43% of the cycles; without the cap 28%, 97 us.
 // 4 waves of 32 queries, two workgroups a CU (head_dim 256: 8 waves, for K and V tiles of twice the width to be
 // read by 8 tasks).  64 queries a wave, which would halve the operand reads, leave one wave a SIMD, and the
 // accumulators then cost a copy per score between the register files.

@@ -29,7 +29,10 @@
 //     this out for itself from the maps (4 to 5 us where pages are shared, 1 to 2 where none are).  Against
 //     every sequence on its own, 32 of 17473 tokens, 40 heads over 8 of 128: all shared 109 -> 48 us, 14000 tokens
 //     104 -> 82, 8704 159 -> 127, 4096 188 -> 166; 64 of them, all shared 198 -> 77; 128 of 4000, none shared 170
-//     -> 171; 48 of 9000 sharing 8000, 16 heads over 8 of 256, capped, 149 -> 88.
+//     -> 171; 48 of 9000 sharing 8000, 16 heads over 8 of 256, capped, 149 -> 88.  The shortest sharer bounds what a
+//     group reads together: one of 520 tokens among 31 that share 17008 makes of 55 us 141.
+// Probabilities are rounded to bf16 as in the suffix kernel, for the matrix instruction and, so that the weights sum to
+// one, for the row sum; partials stay fp32.
 #include "attn_common.h"
 #include "attn_dma.h"
 #include "decode_common.h"
@@ -526,7 +529,10 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs
   }
 }
 
-// Pages of a run.  A workgroup keeps its CU's memory pipe full by itself, so launches that have a workgroup per
+// Pages of a run, of lengths up to max_len that are taken to be alike (all figures are of equal lengths; the device's
+// are not known here): the longest sequence decides a launch's time.  32 of 17473 tokens take 181 us, 32 evenly up to
+// 17473 152 for half the bytes, one of 17473 and 31 of 500 135, over 8 heads of 128.
+// A workgroup keeps its CU's memory pipe full by itself, so launches that have a workgroup per
 // (sequence, KV head, query group) for half the CUs or more take whole sequences and need no merge, smaller ones
 // as many runs as make one workgroup per CU (32 sequences of 17473 tokens, 40 heads over 8 of 128: one run 181
 // us, two 186; 24: 154 and 170; 8 of 4000: four runs 17.8, eight 19.3; 2 of 17473: sixteen 19.2, 32 21.5).
@@ -535,7 +541,9 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_kv8_kernel(const DecodeArgs
 //     8.4, 12 9.1, 32 11.3); one run up to 32 pages, or 96 where there would be two (16 sequences of 1300: 14.0,
 //     two runs 15.0).
 //   * Between 256 and 512, two a CU: runs that fill whole rounds of 512 (36 sequences of 4000 over 8 heads:
-//     three runs 55.6 us, one 66, two 60; 48 of 6000: two 102, one 114, three 111; 56 of 4000: one 82, two 92).
+//     three runs 55.6 us, one 66, two 60; 48 of 6000: two 102, one 114, three 111; 56 of 4000: one 82, two 92): three
+//     while they fit two rounds (341 pairs), then two up to the middle of the two counts measured (384 and 448), then
+//     one; the 96 pages below which there is one, and the 85 pairs from which 256 / pairs is two, are those above.
 int kv8_split_pages(const DecodeLaunch &p, int n_qgroups) {
   const int64_t max_pages = ((int64_t)p.max_len + 15) / 16;
   const int64_t pairs = (int64_t)p.n_seqs * p.n_kv_heads * n_qgroups;
