@@ -370,7 +370,8 @@ nexus_status nexus_kv8_read(const nexus_kv8_cache *cache, const nexus_page_table
  * aligned; layouts, positions, masks, softcap, scale, plan and workspace rules (16-byte aligned) as there.
  * Scores are exact products of q with the keys' values, accumulated in fp32 (an element of q below 2^-13.8 of its
  * row's largest is held to 2^-21.8 of that, one past 448 * 2^119 counts as that); probabilities are rounded to bf16 for their product with the values.
- * The rows of the sequences of one launch must not overlap (NEXUS_EINVAL).
+ * The rows of the sequences of one launch must not overlap (NEXUS_EINVAL); a sequence sees at most 2^31 - 65536 keys
+ * (NEXUS_ERANGE).
  */
 nexus_status nexus_kv8_suffix_attn(const void *q, int32_t n_s, int32_t n_q_heads,
                                    const nexus_kv8_cache *cache, const nexus_page_table *pt, int32_t layer,

@@ -92,6 +92,9 @@ nexus_status check_attention(const void *q, const void *out, int32_t n_q_heads, 
 }
 
 constexpr int32_t kMaxSuffixes = 32;
+// Keys of a sequence: the kernel's positions are 32-bit, and those of a split's end (32768 keys at most), a key tile
+// and a query block reach past the last one.
+constexpr int64_t kMaxKeys = kMaxElems32 - 65536;
 
 struct Suffixes {
   AttnSeq seq[kMaxSuffixes];
@@ -105,7 +108,7 @@ nexus_status plan_launch(int32_t n_seqs, const int32_t *q_start, const int32_t *
   for (int32_t b = 0; b < n_seqs; ++b) {
     s.seq[b] = AttnSeq{q_start[b], seq_len[b], seq_n_past[b]};
     if (seq_len[b] <= 0 || q_start[b] < 0) return NEXUS_EINVAL;
-    if (seq_n_past[b] < 0 || seq_n_past[b] > kMaxElems32 - seq_len[b]) return NEXUS_ERANGE;
+    if (seq_n_past[b] < 0 || seq_n_past[b] > kMaxKeys - seq_len[b]) return NEXUS_ERANGE;
     if ((int64_t)q_start[b] + seq_len[b] > kMaxElems32 / 1024) return NEXUS_ERANGE;
     rows += seq_len[b];
     for (int32_t o = 0; o < b; ++o)
