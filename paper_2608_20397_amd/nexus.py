@@ -177,6 +177,9 @@ def _checked_map(cache, k: torch.Tensor, pm: torch.Tensor) -> CPageTable:
         raise NexusError(EINVAL, "page_map must be a contiguous int32 vector")
     _on_device(("cache k", k), ("page_map", pm))
     npp = k.shape[1]
+    if pm.is_inference():                            # has no version counter: its changes cannot be noticed
+        check_page_table(pm.cpu().numpy(), npp)
+        return CPageTable(pm.data_ptr(), pm.numel())
     key = (pm.data_ptr(), pm._version, pm.numel(), npp)
     if cache._map_checked is None or cache._map_checked[0] != key:
         check_page_table(pm.cpu().numpy(), npp)      # raises NexusError(ERANGE)
@@ -210,7 +213,8 @@ class PagedKVCache:
     The kernels read the page map's entries on the device without a host check, so the map is
     validated here (``nexus_check_page_table`` on a host copy: every entry a distinct physical
     page) the first time a call uses it and again whenever it has changed since (another tensor,
-    or an in-place write that bumped its version counter)."""
+    or an in-place write that bumped its version counter).  A map made under torch.inference_mode keeps
+    no such counter and is copied to the host and validated by every call."""
     k: torch.Tensor
     v: torch.Tensor
     page_map: torch.Tensor
