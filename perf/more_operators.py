@@ -279,7 +279,7 @@ def _lay_out(s):
     n_free, stride = s["n_free"].long(), s["maps"].shape[1]
     end = torch.cumsum(fresh.clamp(0, n), 0)
     first, last = (cached + PAGE - 1) // PAGE, (cached + fresh + PAGE - 1) // PAGE
-    valid = (cached >= 0) & (fresh >= 0) & (cached + fresh <= PAGE * stride) & (end <= n)
+    valid = (cached >= 0) & (fresh >= 0) & (cached + fresh <= PAGE * stride) & ((end <= n) | (fresh == 0))
     need = torch.where(valid, last - first, 0)
     upto = torch.cumsum(need, 0)
     ok = valid & ((need == 0) | (upto <= n_free))
