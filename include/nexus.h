@@ -410,6 +410,105 @@ size_t nexus_kv8_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const 
                                        int32_t max_seq_len);
 
 /*
+ * ---- Ragged batches: a round takes some fresh tokens of each of n_seqs sequences (one of a sequence that generates,
+ * a chunk of a prompt, none), laid out sequence by sequence as rows.  nexus_batch_pages lays the batch out on the
+ * device; in every layer nexus_norm_rope_append writes the rows' keys and values and nexus_window_attn attends with
+ * their queries (nexus_window_decode_attn where every sequence has one).  Lengths, starts, positions and slots live on
+ * the device, so one captured launch serves rounds of any lengths within its host bounds.
+ */
+
+/*
+ * The layout of a round, in one kernel launch.
+ *   cached, fresh  DEVICE int32 [n_seqs]: tokens that sequence b has in the cache, and its new ones.
+ *   free_pages     DEVICE int32 [free_capacity]: physical pages; the first n_free[0] (DEVICE, clamped to
+ *                  [0, free_capacity]) are free.  Pages are taken from the end: the batch's i-th one, in the order of
+ *                  sequences and positions, is entry n_free[0] - 1 - i.
+ *   maps           DEVICE int32 [n_seqs][map_stride]: row b's first ceil(cached[b] / 16) entries are its pages; the
+ *                  entries up to ceil((cached[b] + fresh[b]) / 16) are written, no others.
+ * Written:
+ *   q_start  [n_seqs + 1]  rows before sequence b: fresh[0] + .. + fresh[b - 1] (a negative fresh counts 0), at most
+ *                          max_tokens
+ *   seq_len  [n_seqs]      cached[b] + fresh[b], or 0 for a sequence that is refused
+ *   pos, slot [max_tokens] position of each row in its sequence and its place in the cache, page * 16 + token of the
+ *                          page; -1 for the rows of refused sequences and for those behind the last sequence
+ *   n_left   [1]           free pages left: the first n_left[0] entries of free_pages
+ * A sequence is refused, and its map row left as it is, where a length is negative, cached + fresh is more than
+ * 16 * map_stride, it has rows and they pass max_tokens, or the pages that it and the sequences before it need
+ * (refused for want of pages or not) are more than there are; one that needs no page is not refused for their want.
+ * Checks: non-NULL arrays (free_pages too), n_seqs, map_stride, max_tokens > 0, free_capacity >= 0, written arrays
+ * that overlap neither each other nor the ones read (NEXUS_EINVAL); n_seqs <= 16384, n_seqs * map_stride < 2^31
+ * (NEXUS_ESHAPE); map_stride <= 2^25 (NEXUS_ERANGE).
+ */
+nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int32_t n_seqs,
+                               const int32_t *free_pages, const int32_t *n_free, int32_t free_capacity,
+                               int32_t *maps, int32_t map_stride, int32_t max_tokens, int32_t *q_start,
+                               int32_t *seq_len, int32_t *pos, int32_t *slot, int32_t *n_left, void *stream);
+
+/*
+ * The rows of one layer into the cache: queries and keys normalised per head and rotated, in one pass.
+ *   q, k, v   DEVICE rows of the cache dtype, n_tokens of them: row t starts q_stride (k_stride, v_stride) elements
+ *             after row t - 1 and holds n_q_heads (cache->n_kv_heads) heads of head_dim, so that the three may be
+ *             parts of one projection's rows.
+ *   eps       > 0: every head of q and k becomes x / sqrt(mean(x^2) + eps) * weight, weights fp32 [head_dim] on the
+ *             device (NULL: ones); 0: no norm, and no weights.
+ *   pos, slot DEVICE int32 [n_tokens], as nexus_batch_pages writes them: the rotation's position (the cache's base and
+ *             pairing, arithmetic of nexus_rephase_k) and the place of the key and value.  A row whose slot is outside
+ *             the cache (-1 among them) writes nothing, its q_out row included.  Other slots must differ.
+ *   q_out     [n_tokens][n_q_heads][head_dim]; may be q itself where q_stride is n_q_heads * head_dim.
+ * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.
+ * Checks: non-NULL q, k, v, pos, slot, q_out, n_tokens > 0, pointers (cache, rows) 16-byte aligned and strides in
+ * multiples of 16 bytes that cover a row, eps finite and >= 0, no weights without a norm, q_out apart from the rows
+ * read (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens *
+ * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
+ */
+nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride,
+                                    const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                    int32_t n_tokens, int32_t n_q_heads, const float *q_weight,
+                                    const float *k_weight, float eps, const int32_t *pos, const int32_t *slot,
+                                    void *q_out, void *stream);
+
+/*
+ * Grouped-query attention in a sliding window with sinks, over per-sequence page maps: the query at position p sees
+ * key k when k <= p and (k > p - window or k < n_sink).
+ *   q, out    [n_rows][n_q_heads][head_dim] of the cache dtype, 16-byte aligned; queries are rotated.  Rows
+ *             q_start[b] .. q_start[b + 1] - 1 belong to sequence b and sit at its last positions, seq_len[b] - 1 for
+ *             the last of them; rows of no sequence are left as they are in out.  out may be q.
+ *   q_start   DEVICE int32 [n_seqs + 1], not decreasing, within [0, n_rows] (clamped to it).
+ *   maps, map_stride, seq_len, max_seq_len: as nexus_decode_attn (lengths clamped to [0, max_seq_len]; a row that would
+ *             sit before position 0 gets zeros).  Only entries of pages that hold a key some row sees are read, so
+ *             pages that the window has left may be gone.
+ *   window    >= 1; n_sink >= 0.  A window of max_seq_len or more is plain causal attention.
+ *   layer, softcap, v_layout, scale: as nexus_suffix_attn.
+ *   workspace nexus_window_attn_workspace() bytes (NULL allowed when that is 0), 16-byte aligned; contents on entry do
+ *             not matter.
+ * A key or value that is not finite reaches the queries that see it and no others; slots that no query sees may hold
+ * anything.  bf16 caches: MFMA, probabilities rounded to bf16 as in nexus_suffix_attn, head_dim 64, 128 or 256.  f32
+ * caches: fp32 MFMA, head_dim 16 .. 256.  Checks: the sizes and pointers above, positive n_rows and n_seqs
+ * (NEXUS_EINVAL); layouts as nexus_decode_attn, 16-byte aligned caches (NEXUS_EINVAL), max_seq_len <= 2^29
+ * (NEXUS_ERANGE), launches of fewer than 2^24 workgroups (NEXUS_ESHAPE).
+ */
+nexus_status nexus_window_attn(const void *q, int32_t n_rows, int32_t n_q_heads, const nexus_kv_cache *cache,
+                               const int32_t *maps, int32_t map_stride, const int32_t *q_start,
+                               const int32_t *seq_len, int32_t n_seqs, int32_t max_seq_len, int32_t window,
+                               int32_t n_sink, int32_t layer, float softcap, int32_t v_layout, float scale, void *out,
+                               void *workspace, size_t workspace_bytes, void *stream);
+/* Workspace bytes nexus_window_attn needs (0 if none, SIZE_MAX if the arguments are invalid). */
+size_t nexus_window_attn_workspace(int32_t n_rows, int32_t n_q_heads, const nexus_kv_cache *cache, int32_t n_seqs,
+                                   int32_t max_seq_len, int32_t window, int32_t n_sink);
+
+/*
+ * nexus_window_attn for a decode step: row b is the one query of sequence b, at position seq_len[b] - 1
+ * (nexus_decode_attn with a window).  A sequence of length 0 gets zeros.
+ */
+nexus_status nexus_window_decode_attn(const void *q, int32_t n_seqs, int32_t n_q_heads, const nexus_kv_cache *cache,
+                                      const int32_t *maps, int32_t map_stride, const int32_t *seq_len,
+                                      int32_t max_seq_len, int32_t window, int32_t n_sink, int32_t layer,
+                                      float softcap, int32_t v_layout, float scale, void *out, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+size_t nexus_window_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const nexus_kv_cache *cache,
+                                          int32_t max_seq_len, int32_t window, int32_t n_sink);
+
+/*
  * Warm-prefix reuse on the paged cache (the exact-token prefix arena of Sec. VI-D, whose copy
  * within a pre-reserved arena becomes page-table work here).  Both calls take two DEVICE int32
  * page maps of one cache (n_map_pages entries each, logical page -> physical page) and move

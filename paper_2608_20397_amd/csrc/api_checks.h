@@ -44,6 +44,23 @@ inline nexus_status check_block(const nexus_block *b) {
   return NEXUS_OK;
 }
 
+inline nexus_status check_cache(const nexus_kv_cache *c) {
+  if (!c || !c->k || !c->v) return NEXUS_EINVAL;
+  if (c->n_layers <= 0 || c->n_phys_pages <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+    return NEXUS_EINVAL;
+  if (c->page_size != kPageSize) return NEXUS_ESHAPE;
+  const int es = dtype_bytes(c->dtype);
+  if (!es) return NEXUS_EDTYPE;
+  if (!valid_layout(c->v_layout) || !valid_style(c->rope_style)) return NEXUS_EINVAL;
+  if (!head_dim_ok(c->head_dim, es)) return NEXUS_ESHAPE;
+  if (c->n_layers > 65535) return NEXUS_ESHAPE;
+  // kernels address one layer of K or V with 32-bit element offsets
+  if ((int64_t)c->n_phys_pages * kPageSize * c->n_kv_heads * c->head_dim >= kMaxElems32)
+    return NEXUS_ESHAPE;
+  if (!(c->rope_base > 1.0) || !isfinite(c->rope_base)) return NEXUS_EROPE;
+  return NEXUS_OK;
+}
+
 inline nexus_status from_hip(hipError_t e) { return e == hipSuccess ? NEXUS_OK : NEXUS_EHIP; }
 
 inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }

@@ -24,23 +24,6 @@ bool transposed_row_ok(const nexus_kv_cache *c) {
   return c->v_layout != NEXUS_V_TRANSPOSED || c->head_dim * dtype_bytes(c->dtype) <= 512;
 }
 
-nexus_status check_cache(const nexus_kv_cache *c) {
-  if (!c || !c->k || !c->v) return NEXUS_EINVAL;
-  if (c->n_layers <= 0 || c->n_phys_pages <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
-    return NEXUS_EINVAL;
-  if (c->page_size != kPageSize) return NEXUS_ESHAPE;
-  const int es = dtype_bytes(c->dtype);
-  if (!es) return NEXUS_EDTYPE;
-  if (!valid_layout(c->v_layout) || !valid_style(c->rope_style)) return NEXUS_EINVAL;
-  if (!head_dim_ok(c->head_dim, es)) return NEXUS_ESHAPE;
-  if (c->n_layers > 65535) return NEXUS_ESHAPE;
-  // kernels address one layer of K or V with 32-bit element offsets
-  if ((int64_t)c->n_phys_pages * kPageSize * c->n_kv_heads * c->head_dim >= kMaxElems32)
-    return NEXUS_ESHAPE;
-  if (!(c->rope_base > 1.0) || !isfinite(c->rope_base)) return NEXUS_EROPE;
-  return NEXUS_OK;
-}
-
 nexus_status check_pt(const nexus_page_table *pt, const nexus_kv_cache *c) {
   if (!pt || !pt->map || pt->n_logical_pages <= 0) return NEXUS_EINVAL;
   if (pt->n_logical_pages > c->n_phys_pages) return NEXUS_ERANGE;

@@ -105,6 +105,15 @@ def lib():
         "nexus_kv8_decode_attn": (i32, [vp, i32, i32, p8, vp, i32, vp, i32, i32, f32, f32, vp, vp,
                                         sz, vp]),
         "nexus_kv8_decode_attn_workspace": (sz, [i32, i32, p8, i32]),
+        "nexus_batch_pages": (i32, [vp, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
+        "nexus_norm_rope_append": (i32, [pC, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, f32, vp, vp,
+                                         vp, vp]),
+        "nexus_window_attn": (i32, [vp, i32, i32, pC, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, i32, f32,
+                                    vp, vp, sz, vp]),
+        "nexus_window_attn_workspace": (sz, [i32, i32, pC, i32, i32, i32, i32]),
+        "nexus_window_decode_attn": (i32, [vp, i32, i32, pC, vp, i32, vp, i32, i32, i32, i32, f32, i32, f32, vp,
+                                           vp, sz, vp]),
+        "nexus_window_decode_attn_workspace": (sz, [i32, i32, pC, i32, i32, i32]),
         "nexus_kv_copy_tokens": (i32, [pC, vp, vp, i32, i64, i32, vp]),
         "nexus_kv_share_prefix": (i32, [pC, vp, vp, i32, i32, vp]),
         "nexus_l0_longest_prefix": (i32, [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int32),
@@ -710,6 +719,174 @@ def _map_arg(m: torch.Tensor, what: str):
     if m.dtype != torch.int32 or m.dim() != 1 or not m.is_contiguous() or not m.is_cuda:
         raise NexusError(EINVAL, f"{what} must be a contiguous int32 device vector")
     return _ptr(m)
+
+
+@dataclass
+class BatchRows:
+    """The layout of a round, device int32 tensors: q_start [n_seqs + 1], seq_len [n_seqs], pos and slot
+    [max_tokens], n_left [1] (see nexus_batch_pages)."""
+    q_start: torch.Tensor
+    seq_len: torch.Tensor
+    pos: torch.Tensor
+    slot: torch.Tensor
+    n_left: torch.Tensor
+
+    @classmethod
+    def empty(cls, n_seqs: int, max_tokens: int, device):
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        return cls(new(n_seqs + 1), new(n_seqs), new(max_tokens), new(max_tokens), new(1))
+
+
+def _int32s(n, **tensors):
+    """The given tensors must be contiguous int32 vectors of n entries (n None: of any) on the current device."""
+    if not _all_here(*tensors.values()):
+        _here(**tensors)
+    for name, t in tensors.items():
+        if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+            raise NexusError(EINVAL, f"{name} must be a contiguous int32 vector" + ("" if n is None else f" of {n}"))
+
+
+def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Tensor,
+                n_free: torch.Tensor, max_tokens: int, out: BatchRows | None = None) -> BatchRows:
+    """Lays a round out: ``fresh`` tokens of sequences that hold ``cached`` ones (device int32 [n_seqs]) get rows,
+    pages from the end of ``free_pages``' first ``n_free`` entries into their rows of ``maps`` [n_seqs][stride],
+    positions and slots.  ``out`` may hold the tensors to write (a captured round)."""
+    n = cached.shape[0] if cached.dim() == 1 else -1
+    _int32s(n, cached=cached, fresh=fresh)
+    _int32s(None, free_pages=free_pages)
+    _int32s(1, n_free=n_free)
+    _kv8_maps(maps, cached, n)
+    if out is None:
+        out = BatchRows.empty(n, max(0, max_tokens), maps.device)
+    else:
+        _int32s(n + 1, q_start=out.q_start)
+        _int32s(n, seq_len=out.seq_len)
+        _int32s(max_tokens, pos=out.pos, slot=out.slot)
+        _int32s(1, n_left=out.n_left)
+    _check(lib().nexus_batch_pages(_ptr(cached), _ptr(fresh), n, _ptr(free_pages), _ptr(n_free),
+                                   free_pages.shape[0], _ptr(maps), maps.shape[1], max_tokens, _ptr(out.q_start),
+                                   _ptr(out.seq_len), _ptr(out.pos), _ptr(out.slot), _ptr(out.n_left), _stream()),
+           "nexus_batch_pages")
+    return out
+
+
+def _row_stride(name: str, x: torch.Tensor, rows: int, heads, dim: int, dtype) -> int:
+    """Elements between the rows of x [rows][heads][dim], whose heads follow one another."""
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != rows or (heads is not None and shape[1] != heads) or shape[2] != dim:
+        raise NexusError(ESHAPE, f"{name} must be [rows][heads][D] with the cache's heads and D, got {tuple(shape)}")
+    if x.dtype != dtype:
+        raise NexusError(EDTYPE, f"{name}'s dtype differs from the cache's")
+    st = x.stride()
+    if st[2] != 1 or (st[1] != dim and shape[1] > 1):
+        raise NexusError(EINVAL, f"the heads of a row of {name} must be contiguous")
+    return st[0] if rows > 1 else shape[1] * dim
+
+
+def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     pos: torch.Tensor, slot: torch.Tensor, q_weight: torch.Tensor | None = None,
+                     k_weight: torch.Tensor | None = None, eps: float = 0.0,
+                     out: torch.Tensor | None = None) -> torch.Tensor:
+    """The rows of one layer: q [rows][n_q_heads][D], k and v [rows][n_kv_heads][D], which may be parts of one
+    projection's rows, with ``pos`` and ``slot`` [rows] of batch_pages.  Heads of q and k are normalised where eps > 0
+    (weights fp32 [D]) and rotated to their positions; keys and values go to their slots, queries to the tensor that
+    is returned (rows without a slot are not written; ``out`` may be q)."""
+    cc = cache.c()
+    dt, dim = cache.k.dtype, cc.head_dim
+    rows = q.shape[0]
+    strides = (_row_stride("q", q, rows, None, dim, dt), _row_stride("k", k, rows, cc.n_kv_heads, dim, dt),
+               _row_stride("v", v, rows, cc.n_kv_heads, dim, dt))
+    if out is None:
+        out = torch.empty(q.shape, dtype=dt, device=q.device)
+    elif out.shape != q.shape or out.dtype != dt or not out.is_contiguous():
+        raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (dim,) or not w.is_contiguous()):
+            raise NexusError(EINVAL, f"{name} must be a contiguous fp32 vector of head_dim")
+    _int32s(rows, pos=pos, slot=slot)
+    if not _all_here(cache.k, q, k, v, out, q_weight, k_weight):
+        _here(cache_k=cache.k, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight)
+    _check(lib().nexus_norm_rope_append(C.byref(cc), layer, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
+                                        strides[2], rows, q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, _ptr(pos),
+                                        _ptr(slot), _ptr(out), _stream()), "nexus_norm_rope_append")
+    return out
+
+
+def _window_query(q: torch.Tensor, cache: PagedKVCache, cc: CKvCache, out, workspace):
+    """Checks q [rows][n_q_heads][D], out and workspace; returns out."""
+    if q.dim() != 3 or q.shape[2] != cc.head_dim:
+        raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
+    if not q.is_contiguous():
+        raise NexusError(EINVAL, "q must be contiguous")
+    if q.dtype != cache.k.dtype:
+        raise NexusError(EDTYPE, "q dtype differs from the cache")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
+    if workspace is not None and not workspace.is_contiguous():
+        raise NexusError(EINVAL, "workspace must be contiguous")
+    if not _all_here(cache.k, q, out, workspace):
+        _here(cache_k=cache.k, q=q, out=out, workspace=workspace)
+    return out
+
+
+def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_start: torch.Tensor,
+                seq_len: torch.Tensor, max_seq_len: int, window: int, n_sink: int, layer: int, softcap: float = 0.0,
+                v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
+                workspace: torch.Tensor | None = None):
+    """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
+    q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
+    ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
+    cc = cache.c()
+    out = _window_query(q, cache, cc, out, workspace)
+    rows, hq, _ = q.shape
+    n = seq_len.shape[0] if seq_len.dim() == 1 else -1
+    _kv8_maps(maps, seq_len, n)
+    _int32s(n + 1, q_start=q_start)
+    need = lib().nexus_window_attn_workspace(rows, hq, C.byref(cc), n, max_seq_len, window, n_sink)
+    ws, nbytes = _kv8_workspace(need, q, workspace)
+    _check(lib().nexus_window_attn(_ptr(q), rows, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(q_start),
+                                   _ptr(seq_len), n, max_seq_len, window, n_sink, layer, softcap,
+                                   cache.v_layout if v_layout is None else v_layout, scale, _ptr(out), _ptr(ws),
+                                   nbytes, _stream()), "nexus_window_attn")
+    return out
+
+
+def window_attn_workspace_bytes(cache: PagedKVCache, n_rows: int, n_q_heads: int, n_seqs: int, max_seq_len: int,
+                                window: int, n_sink: int) -> int:
+    cc = cache.c()
+    n = lib().nexus_window_attn_workspace(n_rows, n_q_heads, C.byref(cc), n_seqs, max_seq_len, window, n_sink)
+    if n == (1 << 64) - 1:
+        raise NexusError(EINVAL, "nexus_window_attn_workspace")
+    return n
+
+
+def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, seq_len: torch.Tensor,
+                       max_seq_len: int, window: int, n_sink: int, layer: int, softcap: float = 0.0,
+                       v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None):
+    """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
+    cc = cache.c()
+    out = _window_query(q, cache, cc, out, workspace)
+    n, hq, _ = q.shape
+    _kv8_maps(maps, seq_len, n)
+    need = lib().nexus_window_decode_attn_workspace(n, hq, C.byref(cc), max_seq_len, window, n_sink)
+    ws, nbytes = _kv8_workspace(need, q, workspace)
+    _check(lib().nexus_window_decode_attn(_ptr(q), n, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(seq_len),
+                                          max_seq_len, window, n_sink, layer, softcap,
+                                          cache.v_layout if v_layout is None else v_layout, scale, _ptr(out),
+                                          _ptr(ws), nbytes, _stream()), "nexus_window_decode_attn")
+    return out
+
+
+def window_decode_attn_workspace_bytes(cache: PagedKVCache, n_seqs: int, n_q_heads: int, max_seq_len: int,
+                                       window: int, n_sink: int) -> int:
+    cc = cache.c()
+    n = lib().nexus_window_decode_attn_workspace(n_seqs, n_q_heads, C.byref(cc), max_seq_len, window, n_sink)
+    if n == (1 << 64) - 1:
+        raise NexusError(EINVAL, "nexus_window_decode_attn_workspace")
+    return n
 
 
 def kv_copy_tokens(cache: PagedKVCache, src_map: torch.Tensor, dst_map: torch.Tensor, t0: int,
