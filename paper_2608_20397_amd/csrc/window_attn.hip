@@ -1,4 +1,4 @@
-// Windowed attention of many rows, bf16 (MFMA): every row of a ragged batch sees the last `window` keys of its own
+// Windowed attention of many rows, bf16, head_dim 64 and 128 (MFMA): every row of a ragged batch sees the last `window` keys of its own
 // sequence and the first `sinks` ones (Sec. III-A's attention, restricted as models with local layers do).
 //
 // softmax(s) V with s = scale q.k (soft-capped or not) over the keys that the row sees, in one pass with a running
@@ -27,7 +27,8 @@ constexpr int kRing = 2048;        // entries of the page ring in LDS
 }  // namespace
 
 template <int D, bool VT, bool CAP>
-__global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_rows_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const WindowArgs a) {
+  static_assert(D == 64 || D == 128, "head_dim");
   constexpr int KT = 64;
   constexpr int NKB = KT / 32, NDB = D / 32, NS = D / 16;
   constexpr int ROWB = D * 2;                 // bytes per K or V row
@@ -158,12 +159,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_ro
     const char *src = sel ? vbytes : kbytes;
     const uint32_t dst = smem_base + (uint32_t)(dstp - smem) + wave * QTRB;
     auto go = [&](int i, const char *s, uint32_t voff) {
-      const uint32_t d = dst + (i >> 2) * 4096;
-      s += (i >> 2) * 4096;
-      if ((i & 3) == 0) dma_s<0>(d, s, voff);
-      else if ((i & 3) == 1) dma_s<1024>(d, s, voff);
-      else if ((i & 3) == 2) dma_s<2048>(d, s, voff);
-      else dma_s<3072>(d, s, voff);
+      if (i == 0) dma_s<0>(dst, s, voff);
+      else if (i == 1) dma_s<1024>(dst, s, voff);
+      else if (i == 2) dma_s<2048>(dst, s, voff);
+      else dma_s<3072>(dst, s, voff);
     };
     if (VT && sel) {
 #pragma unroll
@@ -347,7 +346,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_ro
       softmax_half(s_cur[0], 0, nm, pb[0]);
       softmax_half(s_cur[0], 1, nm, pb[1]);
       softmax_half(s_cur[1], 0, nm, pb[2]);
-      constexpr int VQ = D == 64 ? 10 : D == 128 ? 5 : 3, VP = D == 64 ? 4 : 2, VM = D == 64 ? 12 : 6;
+      constexpr int VQ = D == 64 ? 10 : 5, VP = D == 64 ? 4 : 2, VM = D == 64 ? 12 : 6;
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
       for (int i = 0; i < NKB * NS; ++i) {
@@ -395,54 +394,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_ro
     if (t + 1 < n_tiles) step(t + 1, std::integral_constant<int, 1>{}, sb, sa);
   }
 
-  // ---- epilogue: lane pair (j, j + 32) holds pair j's row, feature 32 db + 8 gq + 4 hh + i in o[db][4 gq + i]
   if (!active) return;
-  const float l_tot = sum_halves(l);
-  const bool empty = pos < 0 || n_tiles == 0;
-  const float inv = direct ? (empty ? 0.f : 1.0f / l_tot) : l_tot > 0.f ? 1.0f / l_tot : 0.f;
-  float check = 0.f;                             // NaN where an output is not finite
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      o[db][v] = empty ? 0.f : o[db][v] * inv;     // (0 x NaN is NaN)
-      check = fmaf(o[db][v], 0.f, check);
-    }
-  check = sum_halves(check);
-  const bool bad = row_ok && !empty && (!(check == 0.f) || l_tot != l_tot);
-  if (row_ok && !bad) {
-    if (direct) {
-      uint16_t *orow = reinterpret_cast<uint16_t *>(a.out) + row * D;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int gq = 0; gq < 4; ++gq)
-          *reinterpret_cast<u32x2 *>(orow + 32 * db + 8 * gq + 4 * hh) =
-              u32x2{pack_bf16x2(o[db][4 * gq + 0], o[db][4 * gq + 1]),
-                    pack_bf16x2(o[db][4 * gq + 2], o[db][4 * gq + 3])};
-    } else {
-      const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
-      float *po = a.part + slot * D;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int gq = 0; gq < 4; ++gq)
-          *reinterpret_cast<f32x4 *>(po + 32 * db + 8 * gq + 4 * hh) =
-              f32x4{o[db][4 * gq + 0], o[db][4 * gq + 1], o[db][4 * gq + 2], o[db][4 * gq + 3]};
-      if (hh == 0) a.part_ml[slot] = float2{part_max(m_ref, pos >= 0, split), empty ? 0.f : l_tot};
-    }
-  }
-  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && hh == 0);
-  while (left) {
-    const int r = __builtin_ctz(left);
-    left &= left - 1;
-    const int rp = __builtin_amdgcn_readlane(pair, r), rtok = rp / G, rhead = kvh * G + rp - rtok * G;
-    const size_t rrow = (size_t)(rt.row0 + rtok) * a.n_q_heads + rhead;
-    float res[(D + 63) / 64], m, lr_;
-    row_again<uint16_t, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const uint16_t *>(a.q) + rrow * D,
-                                    rt.past + rtok, e0, e0 + n_le, res, m, lr_);
-    store_again<uint16_t, D>(a, rrow, split, direct, res, m, lr_);
-  }
+  store_rows<D, VT, CAP>(a, kl, rt, kvh, split, direct, e0, n_le, pair, row, pos, row_ok, hh, m_ref, l, o);
 }
 
 hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream) {
@@ -457,8 +410,7 @@ hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool c
     return cap ? run(window_rows_kernel<d(), false, true>) : run(window_rows_kernel<d(), false, false>);
   };
   if (head_dim == 64) return with_d(std::integral_constant<int, 64>{});
-  if (head_dim == 128) return with_d(std::integral_constant<int, 128>{});
-  return with_d(std::integral_constant<int, 256>{});
+  return with_d(std::integral_constant<int, 128>{});
 }
 
 }  // namespace nexus

@@ -29,6 +29,7 @@ struct WindowArgs {
   float scale_log2;       // scale * log2(e)
   float cap_in;           // scale / softcap
   float cap_out;          // softcap * log2(e)
+  float cap_k;            // 2 * scale * log2(e) / softcap
 };
 
 // Rows of the launch's sequence b, clamped to the arrays: nothing the device holds leads out of them.
@@ -120,6 +121,11 @@ __host__ __device__ __forceinline__ KeyList key_list(int window, int sinks, int 
   l.wp = apart ? w_page : 0;
   l.n = l.sp + ((l.hi + kPage - 1) >> kPageShift) - l.wp;
   return l;
+}
+
+__device__ __forceinline__ float window_sum_halves(float x) {     // over lanes i and i ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // tanh x = 1 - 2 / (e^{2x} + 1); exp2 overflow to +inf gives 1, underflow to 0 gives -1.
@@ -224,8 +230,65 @@ __device__ __forceinline__ void store_again(const WindowArgs &a, size_t row, int
     a.part_ml[(size_t)split * a.n_rows * a.n_q_heads + row] = float2{part_max(m, true, split), l};
 }
 
+// The end of the 32x32 MFMA kernels, for a wave with rows: lane pair (j, j + 32) holds a pair's row, feature
+// 32 db + 8 gq + 4 hh + i in o[db][4 gq + i].  Rows that are not finite are taken again.
+template <int D, bool VT, bool CAP>
+__device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &kl, const RowTile &rt, int kvh,
+                                           int split, bool direct, int e0, int n_le, int pair, size_t row, int pos,
+                                           bool row_ok, int hh, float m_ref, float l, f32x16 (&o)[D / 32]) {
+  constexpr int NDB = D / 32;
+  const int G = a.group;
+  const float l_tot = window_sum_halves(l);
+  const bool empty = pos < 0 || n_le == 0;
+  const float inv = direct ? (empty ? 0.f : 1.0f / l_tot) : l_tot > 0.f ? 1.0f / l_tot : 0.f;
+  float check = 0.f;                             // NaN where an output is not finite
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      o[db][v] = empty ? 0.f : o[db][v] * inv;     // (0 x NaN is NaN)
+      check = fmaf(o[db][v], 0.f, check);
+    }
+  check = window_sum_halves(check);
+  const bool bad = row_ok && !empty && (!(check == 0.f) || l_tot != l_tot);
+  if (row_ok && !bad) {
+    if (direct) {
+      uint16_t *orow = reinterpret_cast<uint16_t *>(a.out) + row * D;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq)
+          *reinterpret_cast<u32x2 *>(orow + 32 * db + 8 * gq + 4 * hh) =
+              u32x2{pack_bf16x2(o[db][4 * gq + 0], o[db][4 * gq + 1]),
+                    pack_bf16x2(o[db][4 * gq + 2], o[db][4 * gq + 3])};
+    } else {
+      const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
+      float *po = a.part + slot * D;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq)
+          *reinterpret_cast<f32x4 *>(po + 32 * db + 8 * gq + 4 * hh) =
+              f32x4{o[db][4 * gq + 0], o[db][4 * gq + 1], o[db][4 * gq + 2], o[db][4 * gq + 3]};
+      if (hh == 0) a.part_ml[slot] = float2{part_max(m_ref, pos >= 0, split), empty ? 0.f : l_tot};
+    }
+  }
+  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && hh == 0);
+  while (left) {
+    const int r = __builtin_ctz(left);
+    left &= left - 1;
+    const int rp = __builtin_amdgcn_readlane(pair, r), rtok = rp / G, rhead = kvh * G + rp - rtok * G;
+    const size_t rrow = (size_t)(rt.row0 + rtok) * a.n_q_heads + rhead;
+    float res[(D + 63) / 64], m, lr_;
+    row_again<uint16_t, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const uint16_t *>(a.q) + rrow * D,
+                                    rt.past + rtok, e0, e0 + n_le, res, m, lr_);
+    store_again<uint16_t, D>(a, rrow, split, direct, res, m, lr_);
+  }
+}
+
 // Kernel launches by type (window_attn.hip, window_decode.hip, window_f32.hip); the merge of the splits.
 hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
+hipError_t launch_window_d256(const WindowArgs &a, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_decode(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
 

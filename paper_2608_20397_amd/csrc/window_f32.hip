@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kF32Rows = 16;       // (token, head) pairs of an fp32 workgroup
 constexpr int kMfmaRows = 128;     // of a bf16 one (window_attn.hip)
+constexpr int kWideRows = 256;     // of one of head_dim 256 (window_d256.hip)
 constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in each lane
 
 }  // namespace
@@ -238,6 +239,10 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a,
     *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + (size_t)row * D + d) = o * inv;
 }
 
+int64_t tile_rows(const WindowLaunch &p) {
+  return !p.is_bf16 ? kF32Rows : p.head_dim == 256 ? kWideRows : kMfmaRows;
+}
+
 // (row tile, KV head) pairs of a launch; sequences of a decode step take theirs by query group in bf16.
 int64_t window_units(const WindowLaunch &p) {
   const int64_t group = p.n_q_heads / p.n_kv_heads;
@@ -245,15 +250,16 @@ int64_t window_units(const WindowLaunch &p) {
     const int64_t per = (group + 15) / 16;
     return p.n_seqs * p.n_kv_heads * per;
   }
-  const int64_t r = p.is_bf16 ? kMfmaRows : kF32Rows;
+  const int64_t r = tile_rows(p);
   return (p.n_rows * group / r + p.n_seqs) * p.n_kv_heads;
 }
 
 // Splits of the keys: as many as fill the chip once, of at least 4 tiles (256 keys) each.
 int window_splits(const WindowLaunch &p) {
   const int64_t group = p.n_q_heads / p.n_kv_heads, units = window_units(p);
-  const int64_t slots = 512;
-  const int64_t rows = p.q_start == nullptr ? 1 : (p.is_bf16 ? kMfmaRows : kF32Rows) / group + 1;
+  // workgroups the chip holds at once
+  const int64_t slots = p.q_start != nullptr && p.is_bf16 && p.head_dim == 256 ? 256 : 512;
+  const int64_t rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;
   const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 32, p.max_len);
   int64_t s = std::min<int64_t>((slots + units - 1) / units, (keys + 255) / 256);
   return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
@@ -298,10 +304,12 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   a.scale_log2 = p.scale * log2e;
   a.cap_in = p.softcap > 0.f ? p.scale / p.softcap : 0.f;
   a.cap_out = p.softcap * log2e;
+  a.cap_k = p.softcap > 0.f ? 2.0f * p.scale * log2e / p.softcap : 0.f;
   const bool cap = p.softcap > 0.f;
   hipError_t e;
   if (!p.is_bf16) e = launch_window_f32(a, p.head_dim, p.v_transposed, cap, stream);
   else if (p.q_start == nullptr) e = launch_window_decode(a, p.head_dim, p.v_transposed, cap, stream);
+  else if (p.head_dim == 256) e = launch_window_d256(a, p.v_transposed, cap, stream);
   else e = launch_window_rows(a, p.head_dim, p.v_transposed, cap, stream);
   if (e != hipSuccess || a.n_splits == 1) return e;
   const dim3 grid(((uint32_t)p.n_rows * p.n_q_heads + 3) / 4);

@@ -233,17 +233,19 @@ class PagedKVCache:
     _map_checked: tuple | None = field(default=None, init=False, repr=False, compare=False)
 
     def c(self) -> CKvCache:
-        L, npp, H, P, D = self.k.shape
-        if P != PAGE or not (self.k.is_contiguous() and self.v.is_contiguous()):
+        k, v = self.k, self.v
+        shape = L, npp, H, P, D = k.shape
+        if P != PAGE or not (k.is_contiguous() and v.is_contiguous()):
             raise NexusError(ESHAPE, "cache k must be contiguous [L][pages][H][16][D]")
-        _on_device(("cache k", self.k), ("cache v", self.v), ("page_map", self.page_map))
-        want_v = (L, H, D, npp * P) if self.v_layout == V_TRANSPOSED else (L, npp, H, P, D)
-        if tuple(self.v.shape) != want_v:
-            raise NexusError(ESHAPE, f"cache v must be {want_v}, got {tuple(self.v.shape)}")
-        if self.v.dtype != self.k.dtype:
+        if not _all_here(k, v, self.page_map):
+            _on_device(("cache k", k), ("cache v", v), ("page_map", self.page_map))
+        want_v = (L, H, D, npp * P) if self.v_layout == V_TRANSPOSED else shape
+        if v.shape != want_v:
+            raise NexusError(ESHAPE, f"cache v must be {want_v}, got {tuple(v.shape)}")
+        if v.dtype != k.dtype:
             raise NexusError(EDTYPE, "cache k and v dtypes differ")
-        return CKvCache(self.k.data_ptr(), self.v.data_ptr(), L, npp, P, H, D,
-                        _dtype_code(self.k), self.v_layout, self.rope_style, self.rope_base)
+        return CKvCache(k.data_ptr(), v.data_ptr(), L, npp, P, H, D, _dtype_code(k), self.v_layout,
+                        self.rope_style, self.rope_base)
 
     def pt(self) -> CPageTable:
         return _checked_map(self, self.k, self.page_map)
@@ -733,17 +735,20 @@ class BatchRows:
 
     @classmethod
     def empty(cls, n_seqs: int, max_tokens: int, device):
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=device)
-        return cls(new(n_seqs + 1), new(n_seqs), new(max_tokens), new(max_tokens), new(1))
+        """Unwritten, in one allocation."""
+        parts = (n_seqs + 1, n_seqs, max_tokens, max_tokens, 1)
+        return cls(*torch.empty(sum(parts), dtype=torch.int32, device=device).split_with_sizes(parts))
 
 
-def _int32s(n, **tensors):
-    """The given tensors must be contiguous int32 vectors of n entries (n None: of any) on the current device."""
-    if not _all_here(*tensors.values()):
-        _here(**tensors)
-    for name, t in tensors.items():
-        if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
-            raise NexusError(EINVAL, f"{name} must be a contiguous int32 vector" + ("" if n is None else f" of {n}"))
+def _vector(name: str, t: torch.Tensor, n):
+    """t must be a contiguous int32 vector of n entries (n None: of any)."""
+    if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        raise NexusError(EINVAL, f"{name} must be a contiguous int32 vector" + ("" if n is None else f" of {n}"))
+
+
+def _page_rows(maps: torch.Tensor, n: int):
+    if maps.dtype != torch.int32 or maps.dim() != 2 or maps.shape[0] != n or not maps.is_contiguous():
+        raise NexusError(EINVAL, "maps must be a contiguous int32 [n_seqs][stride] device tensor")
 
 
 def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Tensor,
@@ -752,17 +757,20 @@ def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, f
     pages from the end of ``free_pages``' first ``n_free`` entries into their rows of ``maps`` [n_seqs][stride],
     positions and slots.  ``out`` may hold the tensors to write (a captured round)."""
     n = cached.shape[0] if cached.dim() == 1 else -1
-    _int32s(n, cached=cached, fresh=fresh)
-    _int32s(None, free_pages=free_pages)
-    _int32s(1, n_free=n_free)
-    _kv8_maps(maps, cached, n)
+    _vector("cached", cached, n)
+    _vector("fresh", fresh, n)
+    _vector("free_pages", free_pages, None)
+    _vector("n_free", n_free, 1)
+    _page_rows(maps, n)
+    if not _all_here(maps, cached, fresh, free_pages, n_free):
+        _here(maps=maps, cached=cached, fresh=fresh, free_pages=free_pages, n_free=n_free)
     if out is None:
         out = BatchRows.empty(n, max(0, max_tokens), maps.device)
     else:
-        _int32s(n + 1, q_start=out.q_start)
-        _int32s(n, seq_len=out.seq_len)
-        _int32s(max_tokens, pos=out.pos, slot=out.slot)
-        _int32s(1, n_left=out.n_left)
+        for name, size in (("q_start", n + 1), ("seq_len", n), ("pos", max_tokens), ("slot", max_tokens), ("n_left", 1)):
+            _vector(name, getattr(out, name), size)
+        if not _all_here(out.q_start, out.seq_len, out.pos, out.slot, out.n_left):
+            _here(q_start=out.q_start, seq_len=out.seq_len, pos=out.pos, slot=out.slot, n_left=out.n_left)
     _check(lib().nexus_batch_pages(_ptr(cached), _ptr(fresh), n, _ptr(free_pages), _ptr(n_free),
                                    free_pages.shape[0], _ptr(maps), maps.shape[1], max_tokens, _ptr(out.q_start),
                                    _ptr(out.seq_len), _ptr(out.pos), _ptr(out.slot), _ptr(out.n_left), _stream()),
@@ -803,32 +811,39 @@ def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (dim,) or not w.is_contiguous()):
             raise NexusError(EINVAL, f"{name} must be a contiguous fp32 vector of head_dim")
-    _int32s(rows, pos=pos, slot=slot)
-    if not _all_here(cache.k, q, k, v, out, q_weight, k_weight):
-        _here(cache_k=cache.k, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight)
+    _vector("pos", pos, rows)
+    _vector("slot", slot, rows)
+    if not _all_here(cache.k, q, k, v, out, q_weight, k_weight, pos, slot):
+        _here(cache_k=cache.k, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight, pos=pos, slot=slot)
     _check(lib().nexus_norm_rope_append(C.byref(cc), layer, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
                                         strides[2], rows, q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, _ptr(pos),
                                         _ptr(slot), _ptr(out), _stream()), "nexus_norm_rope_append")
     return out
 
 
-def _window_query(q: torch.Tensor, cache: PagedKVCache, cc: CKvCache, out, workspace):
-    """Checks q [rows][n_q_heads][D], out and workspace; returns out."""
-    if q.dim() != 3 or q.shape[2] != cc.head_dim:
+def _window_operands(q, cache, cc, maps, q_start, seq_len, out, workspace):
+    """Checks the operands of a windowed launch (q_start None: a row a sequence); returns out and n_seqs."""
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != cc.head_dim:
         raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
     if not q.is_contiguous():
         raise NexusError(EINVAL, "q must be contiguous")
     if q.dtype != cache.k.dtype:
         raise NexusError(EDTYPE, "q dtype differs from the cache")
-    if out is None:
-        out = torch.empty_like(q)
-    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+    if q_start is None:
+        n = shape[0]
+    else:
+        n = seq_len.shape[0] if seq_len.dim() == 1 else -1
+        _vector("q_start", q_start, n + 1)
+    _vector("seq_len", seq_len, n)
+    _page_rows(maps, n)
+    if out is not None and (out.shape != shape or out.dtype != q.dtype or not out.is_contiguous()):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
-    if not _all_here(cache.k, q, out, workspace):
-        _here(cache_k=cache.k, q=q, out=out, workspace=workspace)
-    return out
+    if not _all_here(cache.k, q, maps, seq_len, q_start, out, workspace):
+        _here(cache_k=cache.k, q=q, maps=maps, seq_len=seq_len, q_start=q_start, out=out, workspace=workspace)
+    return torch.empty_like(q) if out is None else out, n
 
 
 def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_start: torch.Tensor,
@@ -839,11 +854,8 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
     cc = cache.c()
-    out = _window_query(q, cache, cc, out, workspace)
+    out, n = _window_operands(q, cache, cc, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
-    n = seq_len.shape[0] if seq_len.dim() == 1 else -1
-    _kv8_maps(maps, seq_len, n)
-    _int32s(n + 1, q_start=q_start)
     need = lib().nexus_window_attn_workspace(rows, hq, C.byref(cc), n, max_seq_len, window, n_sink)
     ws, nbytes = _kv8_workspace(need, q, workspace)
     _check(lib().nexus_window_attn(_ptr(q), rows, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(q_start),
@@ -868,9 +880,8 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
     cc = cache.c()
-    out = _window_query(q, cache, cc, out, workspace)
-    n, hq, _ = q.shape
-    _kv8_maps(maps, seq_len, n)
+    out, n = _window_operands(q, cache, cc, maps, None, seq_len, out, workspace)
+    hq = q.shape[1]
     need = lib().nexus_window_decode_attn_workspace(n, hq, C.byref(cc), max_seq_len, window, n_sink)
     ws, nbytes = _kv8_workspace(need, q, workspace)
     _check(lib().nexus_window_decode_attn(_ptr(q), n, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(seq_len),

@@ -70,7 +70,7 @@ int main() {
         }
   std::mt19937 rng(7);
   for (int i = 0; i < 20000; ++i, ++tiles)
-    if (!check_tiles<128>(rng) || !check_tiles<16>(rng)) {
+    if (!check_tiles<128>(rng) || !check_tiles<256>(rng) || !check_tiles<16>(rng)) {
       printf("tiles %d\n", i);
       return 0;
     }
