@@ -436,7 +436,7 @@ size_t nexus_kv8_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const 
  * 16 * map_stride, it has rows and they pass max_tokens, or the pages that it and the sequences before it need
  * (refused for want of pages or not) are more than there are; one that needs no page is not refused for their want.
  * Checks: non-NULL arrays (free_pages too), n_seqs, map_stride, max_tokens > 0, free_capacity >= 0, written arrays
- * that overlap neither each other nor the ones read (NEXUS_EINVAL); n_seqs <= 16384, n_seqs * map_stride < 2^31
+ * that overlap neither each other nor the ones read (NEXUS_EINVAL); n_seqs <= 8192, n_seqs * map_stride < 2^31
  * (NEXUS_ESHAPE); map_stride <= 2^25 (NEXUS_ERANGE).
  */
 nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int32_t n_seqs,

@@ -8,7 +8,7 @@
 
 namespace nexus {
 
-constexpr int kMaxBatchSeqs = 16384;   // sequences of a batch_pages launch (their sums sit in LDS)
+constexpr int kMaxBatchSeqs = 8192;    // sequences of a batch_pages launch (12 bytes of LDS each)
 
 struct BatchPagesLaunch {
   const int32_t *cached, *fresh;      // [n_seqs]

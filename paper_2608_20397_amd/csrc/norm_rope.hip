@@ -15,7 +15,7 @@ namespace nexus {
 
 namespace {
 
-// theta_i = a[i / 8] b[i % 8]: 24 powers a launch instead of one for every pair, off by one more rounding
+// theta_i = a[i / 8] b[i % 8], off by three roundings of 2^-53
 struct RopeFreq {
   double a[kTabPairs / 8], b[8];
 };
@@ -37,7 +37,12 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
   __shared__ __align__(16) float w_tab[2][2 * kTabPairs];
   const NormRopeLaunch &p = a.p;
   const int D = p.head_dim, n_pairs = D / 2;
-  const int t0 = blockIdx.x * TOK;
+  // transposed V: neighbouring tokens are neighbours in a feature row, so runs of tokens go to one XCD (ids 8 apart),
+  // whose L2 joins the elements to whole lines
+  const int per = VT ? (gridDim.x + 7) / 8 : 0;
+  const int tile = VT ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
+  const int t0 = tile * TOK;
+  if (VT && t0 >= p.n_tokens) return;         // padding of the grid
   const int n_tok = min(TOK, p.n_tokens - t0);
   const uint32_t items = (uint32_t)(n_tok * a.n_rows) << a.lane_shift;
   const int c = threadIdx.x & ((1u << a.lane_shift) - 1);     // (the lanes of a row divide 256)
@@ -169,14 +174,20 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
 hipError_t launch_norm_rope(const NormRopeLaunch &p, hipStream_t stream) {
   NormRopeArgs a{};
   a.p = p;
-  for (int i = 0; i < 8; ++i) a.f.b[i] = std::pow(p.rope_base, -2.0 * i / p.head_dim);
-  for (int i = 0; i < (p.head_dim / 2 + 7) / 8; ++i) a.f.a[i] = std::pow(p.rope_base, -16.0 * i / p.head_dim);
+  // (powers by products of 64-bit mantissas: a call of pow for each took 1 us of host time)
+  const long double r = powl((long double)p.rope_base, -2.0L / p.head_dim);
+  long double x = 1.0L;
+  for (int i = 0; i < 8; ++i, x *= r) a.f.b[i] = (double)x;
+  const long double r8 = x;
+  x = 1.0L;
+  for (int i = 0; i < (p.head_dim / 2 + 7) / 8; ++i, x *= r8) a.f.a[i] = (double)x;
   const uint32_t lanes = (uint32_t)p.head_dim * p.dtype_bytes / 32;
   while ((1u << a.lane_shift) < lanes) ++a.lane_shift;
   a.n_rows = p.n_q_heads + 2 * p.n_kv_heads;
   a.div_rows = make_fastdiv((uint32_t)a.n_rows);
   constexpr int TOK = 4;
-  const dim3 grid((p.n_tokens + TOK - 1) / TOK);
+  const uint32_t tiles = (p.n_tokens + TOK - 1) / TOK;
+  const dim3 grid(p.v_transposed ? (tiles + 7) / 8 * 8 : tiles);
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
     return hipGetLastError();

@@ -72,22 +72,27 @@ __device__ __forceinline__ RowTile find_tile(const WindowArgs &a, uint32_t u) {
     return t;
   }
   const int lane = threadIdx.x & 63;
-  auto first = [&](int b) { return first_tile<R>(row_start(a, b), a.group, b); };
+  auto first = [&](int start, int b) { return first_tile<R>(start, a.group, b); };
   int lo = 0, n = a.n_seqs;
-  while (n > 1) {
+  while (n > 64) {
     const int step = (n + 63) >> 6;
     const int b = lo + lane * step;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(lane * step < n && first(b) <= u);
+    const uint64_t m = __builtin_amdgcn_ballot_w64(lane * step < n && first(row_start(a, b), b) <= u);
     const int k = max(__popcll(m) - 1, 0);
     lo += k * step;
     n = min(step, n - k * step);
   }
-  lo = __builtin_amdgcn_readfirstlane(min(lo, a.n_seqs - 1));
-  t.row0 = row_start(a, lo);
-  const int rows = max(row_start(a, lo + 1) - t.row0, 0);
+  // what the tile needs of its sequence comes with the last look, in one round trip
+  const int b = min(lo + lane, a.n_seqs - 1);
+  const int start = row_start(a, b), end = row_start(a, b + 1), len = window_len(a, b);
+  const uint64_t m = __builtin_amdgcn_ballot_w64(lane < n && first(start, b) <= u);
+  const int k = max(__popcll(m) - 1, 0);
+  lo += k;
+  t.row0 = __builtin_amdgcn_readlane(start, k);
+  const int rows = max(__builtin_amdgcn_readlane(end, k) - t.row0, 0);
   t.n = rows * a.group;
-  t.past = window_len(a, lo) - rows;
-  const uint32_t f = first(lo);
+  t.past = __builtin_amdgcn_readlane(len, k) - rows;
+  const uint32_t f = first(t.row0, lo);
   const uint64_t i0 = u >= f ? (uint64_t)(u - f) * R : (uint64_t)INT32_MAX;
   t.b = i0 < (uint64_t)t.n ? lo : -1;
   t.i0 = (int)min(i0, (uint64_t)INT32_MAX);

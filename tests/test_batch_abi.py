@@ -62,9 +62,9 @@ def test_pages_refuses_missing_arrays(field):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(n=0), N.EINVAL), (dict(n=-1), N.EINVAL), (dict(n=16385), N.ESHAPE), (dict(capacity=-1), N.EINVAL),
+    (dict(n=0), N.EINVAL), (dict(n=-1), N.EINVAL), (dict(n=8193), N.ESHAPE), (dict(capacity=-1), N.EINVAL),
     (dict(stride=0), N.EINVAL), (dict(max_tokens=0), N.EINVAL), (dict(stride=(1 << 25) + 1), N.ERANGE),
-    (dict(n=16384, stride=1 << 17), N.ESHAPE),
+    (dict(n=8192, stride=1 << 18), N.ESHAPE),
     # written arrays that meet what is read or each other: lengths in place, a count in place, one array twice
     (dict(seq_len=STEP), N.EINVAL), (dict(seq_len=2 * STEP + 8), N.EINVAL), (dict(n_left=4 * STEP), N.EINVAL),
     (dict(pos=9 * STEP), N.EINVAL), (dict(slot=8 * STEP + 28), N.EINVAL), (dict(q_start=7 * STEP - 12), N.EINVAL),

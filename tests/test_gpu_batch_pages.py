@@ -52,7 +52,7 @@ def test_free_count_above_the_list_is_clamped():
 
 
 @pytest.mark.parametrize("n,top,n_free,seed", [(63, 5, 500, 1), (64, 40, 60, 2), (1024, 3, 5000, 3), (1025, 9, 300, 4),
-                                               (4097, 2, 5000, 5), (16384, 2, 9000, 6), (300, 700, 20000, 7)])
+                                               (4097, 2, 5000, 5), (8192, 2, 9000, 6), (300, 700, 20000, 7)])
 def test_many(n, top, n_free, seed):
     rng = np.random.default_rng(seed)
     cached = rng.integers(0, 60, n).tolist()
