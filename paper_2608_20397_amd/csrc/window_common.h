@@ -19,8 +19,11 @@ struct WindowArgs {
   const int32_t *maps;    // [n_seqs][map_stride]
   const int32_t *q_start; // [n_seqs + 1], or null: row b is the one query of sequence b
   const int32_t *lens;    // [n_seqs]
-  float *part;            // [n_splits][n_rows * Hq][D]: O / l of each split
-  float2 *part_ml;        // [n_splits][n_rows * Hq]: (m, l)
+  // partial results of a split, [n_splits][n_rows * Hq]: O / l, fp32 or, of window_rows and window_d256, fp16 scaled by
+  // 2^-e so that the row's largest magnitude lies in [2^14, 2^15) (11 bits, three more than P and the output have; a
+  // power of two costs no rounding and keeps any finite value in range); and (m, l, l 2^e, -), e = 0 in fp32
+  void *part;
+  f32x4 *part_ml;
   int32_t map_stride, max_len, n_seqs, n_rows;
   int32_t n_q_heads, n_kv_heads, group, n_qgroups;
   int32_t window, sinks, n_splits;
@@ -214,25 +217,38 @@ __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl
   l_out = (float)l;
 }
 
-// Writes what row_again gave: to the output, or to the split's partial.
-template <typename T, int D>
+// e of a row's fp16 partial, from its largest finite magnitude.
+__device__ __forceinline__ int part_exponent(float amax) {
+  return amax > 0.f ? min(max((int)(__float_as_uint(amax) >> 23) - 127 - 14, -100), 100) : 0;
+}
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// Writes what row_again gave: to the output, or to the split's partial (HALF: in fp16).
+template <typename T, int D, bool HALF>
 __device__ __forceinline__ void store_again(const WindowArgs &a, size_t row, int split, bool direct,
                                             const float (&res)[(D + 63) / 64], float m, float l) {
   const int lane = threadIdx.x & 63;
+  const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
+  int e = 0;
+  if (!direct && HALF) {
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < (D + 63) / 64; ++i)
+      if (lane + 64 * i < D && fabsf(res[i]) <= 3.4e38f) amax = fmaxf(amax, fabsf(res[i]));
+    for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off));
+    e = part_exponent(amax);
+  }
 #pragma unroll
   for (int i = 0; i < (D + 63) / 64; ++i) {
     const int d = lane + 64 * i;
     if (d >= D) continue;
-    if (!direct) {
-      a.part[((size_t)split * a.n_rows * a.n_q_heads + row) * D + d] = l == 0.f ? 0.f : res[i];
-    } else if constexpr (sizeof(T) == 2) {
-      reinterpret_cast<uint16_t *>(a.out)[row * D + d] = (uint16_t)pack_bf16x2(res[i], 0.f);
-    } else {
-      reinterpret_cast<float *>(a.out)[row * D + d] = res[i];
-    }
+    const float x = !direct && l == 0.f ? 0.f : res[i];
+    if (direct && sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[row * D + d] = (uint16_t)pack_bf16x2(x, 0.f);
+    else if (direct) reinterpret_cast<float *>(a.out)[row * D + d] = x;
+    else if (HALF) reinterpret_cast<uint16_t *>(a.part)[slot * D + d] = (uint16_t)pack_f16x2(x * two_to(-e), 0.f);
+    else reinterpret_cast<float *>(a.part)[slot * D + d] = x;
   }
-  if (!direct && lane == 0)
-    a.part_ml[(size_t)split * a.n_rows * a.n_q_heads + row] = float2{part_max(m, true, split), l};
+  if (!direct && lane == 0) a.part_ml[slot] = f32x4{part_max(m, true, split), l, l * two_to(e), 0.f};
 }
 
 // The end of the 32x32 MFMA kernels, for a wave with rows: lane pair (j, j + 32) holds a pair's row, feature
@@ -256,6 +272,16 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
     }
   check = window_sum_halves(check);
   const bool bad = row_ok && !empty && (!(check == 0.f) || l_tot != l_tot);
+  int e = 0;
+  if (!direct) {
+    float amax = 0.f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) amax = fmaxf(amax, fabsf(o[db][v]));
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(amax), __float_as_uint(amax), false, false);
+    e = part_exponent(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  }
   if (row_ok && !bad) {
     if (direct) {
       uint16_t *orow = reinterpret_cast<uint16_t *>(a.out) + row * D;
@@ -268,14 +294,17 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
                     pack_bf16x2(o[db][4 * gq + 2], o[db][4 * gq + 3])};
     } else {
       const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
-      float *po = a.part + slot * D;
+      const float sc = two_to(-e);
+      uint16_t *po = reinterpret_cast<uint16_t *>(a.part) + slot * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq)
-          *reinterpret_cast<f32x4 *>(po + 32 * db + 8 * gq + 4 * hh) =
-              f32x4{o[db][4 * gq + 0], o[db][4 * gq + 1], o[db][4 * gq + 2], o[db][4 * gq + 3]};
-      if (hh == 0) a.part_ml[slot] = float2{part_max(m_ref, pos >= 0, split), empty ? 0.f : l_tot};
+          *reinterpret_cast<u32x2 *>(po + 32 * db + 8 * gq + 4 * hh) =
+              u32x2{pack_f16x2(o[db][4 * gq + 0] * sc, o[db][4 * gq + 1] * sc),
+                    pack_f16x2(o[db][4 * gq + 2] * sc, o[db][4 * gq + 3] * sc)};
+      const float lw = empty ? 0.f : l_tot;
+      if (hh == 0) a.part_ml[slot] = f32x4{part_max(m_ref, pos >= 0, split), lw, lw * two_to(e), 0.f};
     }
   }
   uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && hh == 0);
@@ -287,7 +316,7 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
     float res[(D + 63) / 64], m, lr_;
     row_again<uint16_t, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const uint16_t *>(a.q) + rrow * D,
                                     rt.past + rtok, e0, e0 + n_le, res, m, lr_);
-    store_again<uint16_t, D>(a, rrow, split, direct, res, m, lr_);
+    store_again<uint16_t, D, true>(a, rrow, split, direct, res, m, lr_);
   }
 }
 

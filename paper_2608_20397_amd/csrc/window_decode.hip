@@ -3,7 +3,8 @@
 //
 // HBM-bound: window + sinks key and value rows a (sequence, KV head), read once for up to 16 query heads.  A workgroup
 // is one (sequence, KV head, query group, split) and takes a run of the list of seen pages (sinks', then window's);
-// its 4 waves take pairs of them in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x32 MFMA straight from global memory
+// its 4 waves take pairs of them in turn (8 waves: as fast over
+// 17473 tokens of one sequence or 32, slower with two workgroups' worth of pairs on a CU), S^T = K.Q^T and O^T += V^T.P^T on 16x16x32 MFMA straight from global memory
 // as decode_bf16 does (layouts there), and merge their (m, l, O) through LDS.  Slots of a listed page that the query
 // does not see are read as one that it sees (transposed V: zeroed) and masked, so that nothing in them matters.
 #include "attn_dma.h"
@@ -17,20 +18,21 @@ namespace nexus {
 namespace {
 
 constexpr int kList = 2048;        // pages listed in LDS at a time
-constexpr int kMinRun = 16;        // pages of a split at least: two pairs a wave
+constexpr int kMinRun = 8;         // pages of a split at least
 
 }  // namespace
 
 template <int D, bool VT, bool CAP>
 __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_decode_kernel(const WindowArgs a) {
+  constexpr int NW = kDecWaves;
   constexpr int NP = D == 256 ? 1 : 2;   // pages per step of a wave
   constexpr int KS = D / 32;          // S^T MFMA steps
   constexpr int DT = D / 16;          // O^T tiles
   constexpr int ROWB = 2 * D;         // bytes per key row
   constexpr int VL = VT ? 1 : D / 32; // 16-byte V loads per lane per row-major page
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer (floats)
-  constexpr int STAGE_BYTES = VT ? 0 : kDecWaves * NP * 16 * ROWB;
-  constexpr int MERGE_BYTES = 2 * 16 * MO_LD * 4 + 2 * 2 * 16 * 4;
+  constexpr int STAGE_BYTES = VT ? 0 : NW * NP * 16 * ROWB;
+  constexpr int MERGE_BYTES = NW / 2 * 16 * (MO_LD * 4 + 2 * 4);
   constexpr int SMEM = STAGE_BYTES > MERGE_BYTES ? STAGE_BYTES : MERGE_BYTES;
   __shared__ __align__(1024) char smem[SMEM];
   __shared__ int32_t pgs[kList];
@@ -63,9 +65,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
   const int e_begin = split * per, e_end = min(e_begin + per, kl.n);
   if (e_begin >= e_end) {
     if (direct) {
-      for (int i = tid; i < g_cnt * D; i += 256) out[((size_t)b * a.n_q_heads + hq0) * D + i] = 0;
+      for (int i = tid; i < g_cnt * D; i += 64 * NW) out[((size_t)b * a.n_q_heads + hq0) * D + i] = 0;
     } else if (tid < g_cnt) {
-      a.part_ml[slot] = float2{-INFINITY, 0.f};
+      a.part_ml[slot] = f32x4{-INFINITY, 0.f, 0.f, 0.f};
     }
     return;
   }
@@ -221,18 +223,18 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
   for (int c0 = e_begin; c0 < e_end; c0 += kList) {
     const int n_sp = min(kList, e_end - c0);
     if (c0 > e_begin) __syncthreads();
-    for (int i = tid; i < n_sp; i += 256) {
+    for (int i = tid; i < n_sp; i += 64 * NW) {
       const int p = kl.page(c0 + i);
       pgs[i] = map[p];
       first[i] = p * kPage;
     }
     __syncthreads();
-    // this wave's pairs of list entries wave + 4 k through two register buffers: a pair is loading while the other
+    // this wave's pairs of list entries wave + NW k through two register buffers: a pair is loading while the other
     // is computed (entries past the list's end re-read its last page, masked or unused)
     const int n_pairs = (n_sp + NP - 1) / NP;
-    const int n_mine = wave < n_pairs ? (n_pairs - wave + kDecWaves - 1) / kDecWaves : 0;
+    const int n_mine = wave < n_pairs ? (n_pairs - wave + NW - 1) / NW : 0;
     if (n_mine > 0) {
-      auto entry = [&](int k) { return NP * (wave + kDecWaves * k); };
+      auto entry = [&](int k) { return NP * (wave + NW * k); };
       auto issue = [&](int k, Pair &pr) {
 #pragma unroll
         for (int pp = 0; pp < NP; ++pp) {
@@ -266,11 +268,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
     }
   }
 
-  // ---- merge the 4 waves' (m, l, O^T), pairwise through LDS: waves 2 and 3 into waves 0 and 1, then wave 1 into wave
-  // 0, which writes the result
+  // ---- merge the waves' (m, l, O^T) pairwise through LDS, the upper half into the lower, down to wave 0, which writes
+  // the result
   lsum = sum_x32(sum_x16(lsum));
-  float *mo = reinterpret_cast<float *>(smem);   // [2 slots][16 columns][MO_LD]
-  float *mml = mo + 2 * 16 * MO_LD;              // [2 slots][16 columns][m, l]
+  float *mo = reinterpret_cast<float *>(smem);   // [NW / 2 slots][16 columns][MO_LD]
+  float *mml = mo + NW / 2 * 16 * MO_LD;         // [NW / 2 slots][16 columns][m, l]
   auto store_state = [&](int s) {
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -295,15 +297,14 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
     lsum = lsum * wa + lb * wb;
     m_ref = M;
   };
-  __syncthreads();   // the V staging slots are reused
-  if (wave >= 2) store_state(wave - 2);
-  __syncthreads();
-  if (wave < 2) merge_state(wave);
-  __syncthreads();
-  if (wave == 1) store_state(0);
-  __syncthreads();
+#pragma unroll
+  for (int half = NW / 2; half > 0; half /= 2) {
+    __syncthreads();   // the V staging slots, or the slots of the step before, are reused
+    if (wave >= half && wave < 2 * half) store_state(wave - half);
+    __syncthreads();
+    if (wave < half) merge_state(wave);
+  }
   if (wave != 0) return;
-  merge_state(0);
   if (!q_ok) return;
   if (direct) {
     const float inv = 1.0f / lsum;
@@ -314,8 +315,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
   } else {
     const float inv = lsum > 0.f ? 1.0f / lsum : 0.f;
 #pragma unroll
-    for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(a.part + slot * D + 16 * t + 4 * grp) = o[t] * inv;
-    if (grp == 0) a.part_ml[slot] = float2{part_max(m_ref, true, split), lsum};
+    for (int t = 0; t < DT; ++t)
+      *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.part) + slot * D + 16 * t + 4 * grp) = o[t] * inv;
+    if (grp == 0) a.part_ml[slot] = f32x4{part_max(m_ref, true, split), lsum, lsum, 0.f};
   }
 }
 

@@ -1,13 +1,15 @@
 // Windowed attention over fp32 caches (many rows or one a sequence), the merge of split results and the launch of all
 // windowed attention.
 //
-// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its 4 waves take the pages of
-// the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory, and merge their
-// (m, l, O) through LDS.  Scores, probabilities and sums are fp32 throughout.
+// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its 8 waves (4 at head_dim 256)
+// take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory
+// (a page's values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O)
+// through LDS.  Scores, probabilities and sums are fp32 throughout.
 #include "decode_common.h"
 #include "window_common.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace nexus {
@@ -21,12 +23,15 @@ constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in ea
 
 }  // namespace
 
+constexpr int f32_waves(int head_dim) { return head_dim == 256 ? 4 : 8; }
+
 template <int D, bool VT, bool CAP>
-__global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(64 * f32_waves(D)) void window_f32_kernel(const WindowArgs a) {
+  constexpr int NW = f32_waves(D);
   constexpr int DT = D / 16;          // O^T tiles, and 16-feature steps of S^T
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer
-  __shared__ float mo[2 * 16 * MO_LD];
-  __shared__ float mml[2 * 2 * 16];
+  __shared__ float mo[NW / 2 * 16 * MO_LD];
+  __shared__ float mml[NW / 2 * 2 * 16];
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -64,20 +69,49 @@ __global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
   const float *kc = reinterpret_cast<const float *>(a.kc), *vc = reinterpret_cast<const float *>(a.vc);
   const int32_t *map = a.maps + (size_t)rt.b * a.map_stride;
   const float c_scale = CAP ? 1.0f : a.scale_log2;
-  for (int e = e0 + wave; e < e1; e += 4) {
-    const int page = kl.page(e), key0 = page * kPage;
-    const uint32_t phys = (uint32_t)map[page];
-    auto from = [&](int s) { return kl.stand_in(key0 + s) & (kPage - 1); };
-    const size_t base = ((size_t)phys * a.n_kv_heads + kvh) * kPage * D;
-    // lane qn feeds key row qn, features 16 s + 4 grp + i as the k index grp of step (s, i); Q alike
-    const float *kr = kc + base + from(qn) * D + 4 * grp;
-    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto from = [&](int k) { return kl.stand_in(k) & (kPage - 1); };
+  auto page_base = [&](uint32_t phys) { return ((size_t)phys * a.n_kv_heads + kvh) * kPage * D; };
+  // lane qn feeds key row qn, features 16 s + 4 grp + i as the k index grp of step (s, i); Q alike
+  f32x4 k[DT];
+  auto load_k = [&](int key0, uint32_t phys) {
+    const float *kr = kc + page_base(phys) + from(key0 + qn) * D + 4 * grp;
 #pragma unroll
-    for (int st = 0; st < DT; ++st) {
-      const f32x4 k = *reinterpret_cast<const f32x4 *>(kr + 16 * st);
+    for (int st = 0; st < DT; ++st) k[st] = *reinterpret_cast<const f32x4 *>(kr + 16 * st);
+  };
+  int e = e0 + wave, page = 0;
+  uint32_t phys = 0, phys_next = 0;
+  if (e < e1) {
+    page = kl.page(e);
+    phys = (uint32_t)map[page];
+    phys_next = (uint32_t)map[kl.page(min(e + NW, e1 - 1))];
+    load_k(page * kPage, phys);
+  }
+  for (; e < e1; e += NW) {
+    const int key0 = page * kPage;
+    f32x4 v[DT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], qreg[st][i], s, 0, 0, 0);
+    for (int t = 0; t < DT; ++t) {
+      if constexpr (VT) {
+        v[t] = *reinterpret_cast<const f32x4 *>(vc + ((size_t)kvh * D + 16 * t + qn) * a.n_cols +
+                                                (size_t)phys * kPage + 4 * grp);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[t][i] = vc[page_base(phys) + from(key0 + 4 * grp + i) * D + 16 * t + qn];
+      }
     }
+    // two chains of MFMAs, added at the end
+    f32x4 s2[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int st = 0; st < DT; ++st)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s2[i & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[st][i], qreg[st][i], s2[i & 1], 0, 0, 0);
+    const f32x4 s = s2[0] + s2[1];
+    // the next page's keys (past the list's end the last page's again, unused)
+    page = kl.page(min(e + NW, e1 - 1));
+    phys = phys_next;
+    load_k(page * kPage, phys);
+    phys_next = (uint32_t)map[kl.page(min(e + 2 * NW, e1 - 1))];
     // the lane's scores: keys 4 grp + i of query column qn
     float x[4], mx = -INFINITY;
 #pragma unroll
@@ -95,25 +129,23 @@ __global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(x[i], c_scale, -ref));
     lsum = fmaf(lsum, alpha, (p[0] + p[1]) + (p[2] + p[3]));
+    if constexpr (VT) {
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      f32x4 v;
-      if constexpr (VT) {
-        v = *reinterpret_cast<const f32x4 *>(vc + ((size_t)kvh * D + 16 * t + qn) * a.n_cols +
-                                             (size_t)phys * kPage + 4 * grp);
+      for (int i = 0; i < 4; ++i) {
+        const bool in = kl.seen(key0 + 4 * grp + i);    // other slots may hold anything
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = kl.seen(key0 + 4 * grp + i) ? v[i] : 0.f;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = vc[base + from(4 * grp + i) * D + 16 * t + qn];
+        for (int t = 0; t < DT; ++t) v[t][i] = in ? v[t][i] : 0.f;
       }
-      o[t] *= alpha;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i], p[i], o[t], 0, 0, 0);
     }
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] *= alpha;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], p[i], o[t], 0, 0, 0);
   }
 
-  // ---- merge the 4 waves, pairwise
+  // ---- merge the waves, pairwise
   lsum = sum_x32(sum_x16(lsum));
   auto store_state = [&](int s) {
 #pragma unroll
@@ -135,14 +167,14 @@ __global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
     lsum = lsum * wa + lb * wb;
     m = M;
   };
-  if (wave >= 2) store_state(wave - 2);
-  __syncthreads();
-  if (wave < 2) merge_state(wave);
-  __syncthreads();
-  if (wave == 1) store_state(0);
-  __syncthreads();
+#pragma unroll
+  for (int half = NW / 2; half > 0; half /= 2) {
+    if (half < NW / 2) __syncthreads();       // the slots of the step before have been read
+    if (wave >= half && wave < 2 * half) store_state(wave - half);
+    __syncthreads();
+    if (wave < half) merge_state(wave);
+  }
   if (wave != 0) return;
-  merge_state(0);
 
   const bool empty = pos < 0 || e0 == e1;
   const float inv = direct ? (empty ? 0.f : 1.0f / lsum) : lsum > 0.f ? 1.0f / lsum : 0.f;
@@ -158,10 +190,11 @@ __global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
   const bool bad = row_ok && !empty && (!(check == 0.f) || lsum != lsum);
   const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
   if (row_ok && !bad) {
-    float *to = direct ? reinterpret_cast<float *>(a.out) + row * D : a.part + slot * D;
+    float *to = direct ? reinterpret_cast<float *>(a.out) + row * D : reinterpret_cast<float *>(a.part) + slot * D;
 #pragma unroll
     for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(to + 16 * t + 4 * grp) = o[t];
-    if (!direct && grp == 0) a.part_ml[slot] = float2{part_max(m, pos >= 0, split), empty ? 0.f : lsum};
+    const float lw = empty ? 0.f : lsum;
+    if (!direct && grp == 0) a.part_ml[slot] = f32x4{part_max(m, pos >= 0, split), lw, lw, 0.f};
   }
   uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && grp == 0);
   while (left) {
@@ -172,14 +205,14 @@ __global__ __launch_bounds__(256) void window_f32_kernel(const WindowArgs a) {
     float res[(D + 63) / 64], ma, la;
     row_again<float, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const float *>(a.q) + rrow * D, rt.past + rtok,
                                  e0, e1, res, ma, la);
-    store_again<float, D>(a, rrow, split, direct, res, ma, la);
+    store_again<float, D, false>(a, rrow, split, direct, res, ma, la);
   }
 }
 
 hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream) {
   const dim3 grid(a.n_units * a.n_splits);
   auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * f32_waves(head_dim)), 0, stream, a);
     return hipGetLastError();
   };
   auto with_d = [&](auto d) {
@@ -197,47 +230,88 @@ hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool ca
 
 namespace {
 
-// Merge of a row's splits: out = sum w_s O_s / sum w_s with w_s = l_s 2^(m_s - M), in split order within each share of
-// the wave.  One wave a (row, query head); lane s holds (m, l) of split s.  Rows of no sequence stay as they are.
-template <bool BF16>
-__global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a, int D, int lpr_shift) {
+// Merge of a row's splits: out = sum w_s O_s / sum w_s, w_s = l_s 2^(m_s - M), in a fixed order.  Rows of no sequence
+// stay as they are.  A partial row lies in 2^lpr_shift lanes, 16 bytes each; 2^spr_shift neighbouring groups of them
+// share the splits of a row, and what is left of the wave takes other rows.  The first eight partials of a group are
+// loaded beside their (m, l): one round trip for rows of up to 16 splits.
+template <bool BF16, bool HALF>
+__global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a, int D, int lpr_shift, int spr_shift) {
+  constexpr int E = HALF ? 8 : 4, kPre = 8;
   const int lane = threadIdx.x & 63;
-  const uint32_t row = blockIdx.x * 4 + (threadIdx.x >> 6);       // row of q and out, times heads, plus head
-  if (row >= (uint32_t)a.n_rows * a.n_q_heads) return;
-  if (a.q_start != nullptr) {
+  const uint32_t n = (uint32_t)a.n_rows * a.n_q_heads;
+  const uint32_t group = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t row = (group << (6 - lpr_shift - spr_shift)) + (lane >> (lpr_shift + spr_shift));
+  bool live = row < n;
+  if (a.q_start != nullptr && live) {
     const int r = row / a.n_q_heads;
-    if (r < row_start(a, 0) || r >= row_start(a, a.n_seqs)) return;
+    live = r >= row_start(a, 0) && r < row_start(a, a.n_seqs);
   }
-  const size_t stride = (size_t)a.n_rows * a.n_q_heads;
-  const float2 ml = lane < a.n_splits ? a.part_ml[lane * stride + row] : float2{-INFINITY, 0.f};
-  const int share = lane >> lpr_shift, n_shares = 64 >> lpr_shift;
-  const int d = 4 * (lane & ((1 << lpr_shift) - 1));
-  float M = ml.x;
-  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-  // (l is NaN where scores were; an empty split's partial holds nothing)
-  const float w = ml.y == 0.f ? 0.f : ml.y * (M == -INFINITY ? 1.f : fast_exp2(ml.x - M));
-  float total = w;
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.n_splits; s0 += n_shares) {
-    const int s = s0 + share;
-    const float ls = __shfl(ml.y, s & 63), ws = __shfl(w, s & 63);
-    if (s < a.n_splits && ls != 0.f)
-      o += *reinterpret_cast<const f32x4 *>(a.part + (s * stride + row) * D + d) * ws;
-  }
-  for (int off = 32; off >= 1 << lpr_shift; off >>= 1)
+  const int spr = 1 << spr_shift, share = (lane >> lpr_shift) & (spr - 1);
+  const int d = E * (lane & ((1 << lpr_shift) - 1));
+  const int S = live ? a.n_splits : 0;
+  auto load = [&](int s) {
+    const size_t slot = (size_t)s * n + row;
+    return *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(a.part) + (slot * D + d) * (16 / E));
+  };
+  u32x4 pre[kPre];
+  f32x4 ml[kPre];
+  float M = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off);
-  if (share != 0) return;
-  // no key at all: zeros
-  if (M == -INFINITY && total == 0.f) total = 1.f;
+  for (int i = 0; i < kPre; ++i) {
+    const int s = share + i * spr;
+    if (s >= S) continue;
+    pre[i] = load(s);
+    ml[i] = a.part_ml[(size_t)s * n + row];
+  }
+#pragma unroll
+  for (int i = 0; i < kPre; ++i)
+    if (share + i * spr < S) M = fmaxf(M, ml[i][0]);
+  for (int s = share + kPre * spr; s < S; s += spr) M = fmaxf(M, a.part_ml[(size_t)s * n + row][0]);
+  for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
+  float o[E], total = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  auto add = [&](const f32x4 &r, const u32x4 &x) {
+    if (r[1] == 0.f) return;                  // nothing seen: the partial holds nothing (l is NaN where scores were)
+    const float f = M == -INFINITY ? 1.f : fast_exp2(r[0] - M);
+    total = fmaf(r[1], f, total);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (HALF) {
+        const f32x2 v = unpack_f16x2(x[w]);
+        o[2 * w] = fmaf(v[0], r[2] * f, o[2 * w]);
+        o[2 * w + 1] = fmaf(v[1], r[2] * f, o[2 * w + 1]);
+      } else {
+        o[w] = fmaf(__uint_as_float(x[w]), r[2] * f, o[w]);
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kPre; ++i)
+    if (share + i * spr < S) add(ml[i], pre[i]);
+  for (int s = share + kPre * spr; s < S; s += spr) add(a.part_ml[(size_t)s * n + row], load(s));
+  for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) {
+    total += __shfl_xor(total, off);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += __shfl_xor(o[e], off);
+  }
+  if (share != 0 || !live) return;
+  if (M == -INFINITY && total == 0.f) total = 1.f;      // no key at all: zeros
   const float inv = 1.0f / total;
-  if (BF16)
-    *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(a.out) + (size_t)row * D + d) =
-        u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
-  else
-    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + (size_t)row * D + d) = o * inv;
+  if constexpr (BF16) {
+    uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + (size_t)row * D + d;
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<u32x2 *>(out + e) =
+          u32x2{pack_bf16x2(o[e] * inv, o[e + 1] * inv), pack_bf16x2(o[e + 2] * inv, o[e + 3] * inv)};
+  } else {
+    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + (size_t)row * D + d) =
+        f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  }
 }
+
+// Whether a launch's partials are fp16.
+bool half_parts(const WindowLaunch &p) { return p.is_bf16 && p.q_start != nullptr; }
 
 int64_t tile_rows(const WindowLaunch &p) {
   return !p.is_bf16 ? kF32Rows : p.head_dim == 256 ? kWideRows : kMfmaRows;
@@ -254,22 +328,54 @@ int64_t window_units(const WindowLaunch &p) {
   return (p.n_rows * group / r + p.n_seqs) * p.n_kv_heads;
 }
 
-// Splits of the keys: as many as fill the chip once, of at least 4 tiles (256 keys) each.
+// Splits of the keys of every row tile.
 int window_splits(const WindowLaunch &p) {
-  const int64_t group = p.n_q_heads / p.n_kv_heads, units = window_units(p);
-  // workgroups the chip holds at once
-  const int64_t slots = p.q_start != nullptr && p.is_bf16 && p.head_dim == 256 ? 256 : 512;
-  const int64_t rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;
-  const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 32, p.max_len);
-  int64_t s = std::min<int64_t>((slots + units - 1) / units, (keys + 255) / 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
+  const int64_t group = p.n_q_heads / p.n_kv_heads;
+  constexpr int64_t kCUs = 256;
+  const int64_t rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;    // tokens of a tile
+  const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len), pages = (keys + 15) / 16;
+  if (p.q_start == nullptr || !p.is_bf16) {
+    // One workgroup a CU, of at least 20 pages in bf16 and 8 in fp32 (whose 8 waves take a page each); from three
+    // quarters of the CUs on one split, which needs no merge, is as fast or faster (8 KV heads of 128, window 4096:
+    // one sequence 49 us, in 12 splits 12.9, in 24 13.9; 8 sequences 55, in 3 or 4 28, in 8 29.5; 24: 73, in 2 82;
+    // 32: 96, in 2 100), but for long windows and between one workgroup a CU and one and a half (40 sequences 142,
+    // in 3 125; window 1024, head_dim 64: 20.6, in 3 20.7).
+    const int64_t units = window_units(p);
+    int64_t s = 4 * units >= 3 * kCUs ? 1 : kCUs / units;
+    if (p.is_bf16 && units > kCUs && 2 * units <= 3 * kCUs && pages >= 128) s = 3;
+    s = std::min<int64_t>(s, p.is_bf16 ? (pages + 19) / 20 : (pages + 7) / 8);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
+  }
+  // Many rows: the split count of least estimated time.  Tiles that the sequences make of the rows, taking each
+  // sequence to be of average length; workgroups spread evenly over the CUs, whose time per key tile was measured with
+  // one to five of them on a CU (microseconds: head_dim 64 and 128, 128 rows x 64 keys; 256, 256 rows x 32 keys); set-up
+  // and end of a workgroup; partials written and read at 4 TB/s.
+  const double r = (double)tile_rows(p), per_seq = (double)p.n_rows * group / r / p.n_seqs;
+  const double units = (per_seq < 1. ? 1. : per_seq + 0.5) * p.n_seqs * p.n_kv_heads;
+  const int64_t kt = p.head_dim == 256 ? 32 : 64, tiles = (keys + kt - 1) / kt;
+  const double elems = (double)p.n_rows * p.n_q_heads * p.head_dim;
+  int best = 1;
+  double best_t = 1e30;
+  for (int s = 1; s <= 16 && 4 * s <= tiles + 3; ++s) {
+    const int64_t on_cu = (int64_t)ceil(units * s / kCUs);
+    const double tile = p.head_dim == 64 ? (on_cu == 1 ? 0.85 : 0.65 * on_cu)
+                        : p.head_dim == 128 ? 2.0 * (on_cu / 2) + 1.2 * (on_cu % 2) : 2.05 * on_cu;
+    const int64_t together = p.head_dim == 64 ? 3 : p.head_dim == 128 ? 2 : 1;
+    double t = tile * ((tiles + s - 1) / s) + 5.0 * ((on_cu + together - 1) / together);
+    if (s > 1) t += 5.0 + elems * (4. * s + 2.) / 4e6;
+    if (t < 0.97 * best_t) {
+      best_t = t;
+      best = s;
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
 size_t window_workspace_bytes(const WindowLaunch &p) {
   const size_t s = (size_t)window_splits(p);
-  return s == 1 ? 0 : s * p.n_rows * p.n_q_heads * (p.head_dim + 2) * sizeof(float);
+  return s == 1 ? 0 : s * p.n_rows * p.n_q_heads * (p.head_dim * (half_parts(p) ? 2 : 4) + sizeof(f32x4));
 }
 
 bool window_grid_ok(const WindowLaunch &p) { return window_units(p) * window_splits(p) < (1 << 24); }
@@ -296,10 +402,12 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   a.n_splits = window_splits(p);
   a.n_cols = (uint32_t)p.n_phys_pages * 16u;
   a.n_units = (uint32_t)window_units(p);
-  a.part = reinterpret_cast<float *>(p.workspace);
+  const bool half = half_parts(p);
+  a.part = p.workspace;
   a.part_ml = a.n_splits == 1 ? nullptr
-                              : reinterpret_cast<float2 *>(a.part + (size_t)a.n_splits * p.n_rows * p.n_q_heads *
-                                                                        p.head_dim);
+                              : reinterpret_cast<f32x4 *>(reinterpret_cast<char *>(p.workspace) +
+                                                          (size_t)a.n_splits * p.n_rows * p.n_q_heads * p.head_dim *
+                                                              (half ? 2 : 4));
   const float log2e = 1.4426950408889634f;
   a.scale_log2 = p.scale * log2e;
   a.cap_in = p.softcap > 0.f ? p.scale / p.softcap : 0.f;
@@ -312,11 +420,17 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   else if (p.head_dim == 256) e = launch_window_d256(a, p.v_transposed, cap, stream);
   else e = launch_window_rows(a, p.head_dim, p.v_transposed, cap, stream);
   if (e != hipSuccess || a.n_splits == 1) return e;
-  const dim3 grid(((uint32_t)p.n_rows * p.n_q_heads + 3) / 4);
-  int lpr_shift = 0;                  // log2 of the lanes that cover a partial row
-  while ((4 << lpr_shift) < p.head_dim) ++lpr_shift;
-  if (p.is_bf16) hipLaunchKernelGGL((window_combine_kernel<true>), grid, dim3(256), 0, stream, a, p.head_dim, lpr_shift);
-  else hipLaunchKernelGGL((window_combine_kernel<false>), grid, dim3(256), 0, stream, a, p.head_dim, lpr_shift);
+  int lpr = 0, spr = 0;               // log2 of the lanes of a partial row, and of the groups that share its splits
+  while ((half ? 8 : 4) << lpr < p.head_dim) ++lpr;
+  while (lpr + spr < 6 && 1 << spr < a.n_splits) ++spr;
+  const uint32_t per_wg = 4u << (6 - lpr - spr);
+  const dim3 grid(((uint32_t)p.n_rows * p.n_q_heads + per_wg - 1) / per_wg);
+  auto merge = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.head_dim, lpr, spr);
+  };
+  if (half) merge(window_combine_kernel<true, true>);
+  else if (p.is_bf16) merge(window_combine_kernel<true, false>);
+  else merge(window_combine_kernel<false, false>);
   return hipGetLastError();
 }
 

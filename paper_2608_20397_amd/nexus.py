@@ -154,10 +154,18 @@ def _dtype_code(t: torch.Tensor) -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# torch.cuda.current_device without its look whether the driver is there (a device tensor says so); no public accessor
+_get_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _current_device() -> int:
+    return torch.cuda.current_device() if _get_device is None else _get_device()
+
+
 def _stream():
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_current_device())
 
 
 def _ptr(t):
@@ -520,7 +528,7 @@ def _all_here(*tensors) -> bool:
     for t in tensors:
         if t is not None and t.get_device() != dev:
             return False
-    return dev >= 0 and dev == torch.cuda.current_device()
+    return dev >= 0 and dev == _current_device()
 
 
 def _here(**tensors):
@@ -740,14 +748,19 @@ class BatchRows:
         return cls(*torch.empty(sum(parts), dtype=torch.int32, device=device).split_with_sizes(parts))
 
 
+_I32 = torch.int32
+
+
 def _vector(name: str, t: torch.Tensor, n):
     """t must be a contiguous int32 vector of n entries (n None: of any)."""
-    if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+    shape = t.shape
+    if t.dtype != _I32 or len(shape) != 1 or (n is not None and shape[0] != n) or not t.is_contiguous():
         raise NexusError(EINVAL, f"{name} must be a contiguous int32 vector" + ("" if n is None else f" of {n}"))
 
 
 def _page_rows(maps: torch.Tensor, n: int):
-    if maps.dtype != torch.int32 or maps.dim() != 2 or maps.shape[0] != n or not maps.is_contiguous():
+    shape = maps.shape
+    if maps.dtype != _I32 or len(shape) != 2 or shape[0] != n or not maps.is_contiguous():
         raise NexusError(EINVAL, "maps must be a contiguous int32 [n_seqs][stride] device tensor")
 
 
@@ -821,14 +834,15 @@ def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.
     return out
 
 
-def _window_operands(q, cache, cc, maps, q_start, seq_len, out, workspace):
+def _window_operands(q, cache, head_dim, maps, q_start, seq_len, out, workspace):
     """Checks the operands of a windowed launch (q_start None: a row a sequence); returns out and n_seqs."""
     shape = q.shape
-    if len(shape) != 3 or shape[2] != cc.head_dim:
+    if len(shape) != 3 or shape[2] != head_dim:
         raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
     if not q.is_contiguous():
         raise NexusError(EINVAL, "q must be contiguous")
-    if q.dtype != cache.k.dtype:
+    dt = q.dtype
+    if dt != cache.k.dtype:
         raise NexusError(EDTYPE, "q dtype differs from the cache")
     if q_start is None:
         n = shape[0]
@@ -837,7 +851,7 @@ def _window_operands(q, cache, cc, maps, q_start, seq_len, out, workspace):
         _vector("q_start", q_start, n + 1)
     _vector("seq_len", seq_len, n)
     _page_rows(maps, n)
-    if out is not None and (out.shape != shape or out.dtype != q.dtype or not out.is_contiguous()):
+    if out is not None and (out.shape != shape or out.dtype != dt or not out.is_contiguous()):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
@@ -853,15 +867,16 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
-    cc = cache.c()
-    out, n = _window_operands(q, cache, cc, maps, q_start, seq_len, out, workspace)
+    L, cc = lib(), cache.c()
+    out, n = _window_operands(q, cache, cc.head_dim, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
-    need = lib().nexus_window_attn_workspace(rows, hq, C.byref(cc), n, max_seq_len, window, n_sink)
-    ws, nbytes = _kv8_workspace(need, q, workspace)
-    _check(lib().nexus_window_attn(_ptr(q), rows, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(q_start),
-                                   _ptr(seq_len), n, max_seq_len, window, n_sink, layer, softcap,
-                                   cache.v_layout if v_layout is None else v_layout, scale, _ptr(out), _ptr(ws),
-                                   nbytes, _stream()), "nexus_window_attn")
+    c = C.byref(cc)
+    ws, nbytes = _kv8_workspace(L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink), q,
+                                workspace)
+    _check(L.nexus_window_attn(q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(),
+                               seq_len.data_ptr(), n, max_seq_len, window, n_sink, layer, softcap,
+                               cc.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws), nbytes,
+                               _stream()), "nexus_window_attn")
     return out
 
 
@@ -879,15 +894,15 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
-    cc = cache.c()
-    out, n = _window_operands(q, cache, cc, maps, None, seq_len, out, workspace)
-    hq = q.shape[1]
-    need = lib().nexus_window_decode_attn_workspace(n, hq, C.byref(cc), max_seq_len, window, n_sink)
-    ws, nbytes = _kv8_workspace(need, q, workspace)
-    _check(lib().nexus_window_decode_attn(_ptr(q), n, hq, C.byref(cc), _ptr(maps), maps.shape[1], _ptr(seq_len),
-                                          max_seq_len, window, n_sink, layer, softcap,
-                                          cache.v_layout if v_layout is None else v_layout, scale, _ptr(out),
-                                          _ptr(ws), nbytes, _stream()), "nexus_window_decode_attn")
+    L, cc = lib(), cache.c()
+    out, n = _window_operands(q, cache, cc.head_dim, maps, None, seq_len, out, workspace)
+    hq, c = q.shape[1], C.byref(cc)
+    ws, nbytes = _kv8_workspace(L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink), q,
+                                workspace)
+    _check(L.nexus_window_decode_attn(q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(),
+                                      max_seq_len, window, n_sink, layer, softcap,
+                                      cc.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws),
+                                      nbytes, _stream()), "nexus_window_decode_attn")
     return out
 
 
