@@ -335,14 +335,15 @@ int window_splits(const WindowLaunch &p) {
   const int64_t rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;    // tokens of a tile
   const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len), pages = (keys + 15) / 16;
   if (p.q_start == nullptr || !p.is_bf16) {
-    // One workgroup a CU, of at least 20 pages in bf16 and 8 in fp32 (whose 8 waves take a page each); from three
-    // quarters of the CUs on one split, which needs no merge, is as fast or faster (8 KV heads of 128, window 4096:
+    // One workgroup a CU, of at least 20 pages in bf16 and 8 in fp32 (whose 8 waves take a page each), lists of under
+    // twice and four times that whole (a merge costs 4 us of host time); from three quarters of the CUs on one split, which needs no merge, is as fast or faster (8 KV heads of 128, window 4096:
     // one sequence 49 us, in 12 splits 12.9, in 24 13.9; 8 sequences 55, in 3 or 4 28, in 8 29.5; 24: 73, in 2 82;
     // 32: 96, in 2 100), but for long windows and between one workgroup a CU and one and a half (40 sequences 142,
     // in 3 125; window 1024, head_dim 64: 20.6, in 3 20.7).
     const int64_t units = window_units(p);
     int64_t s = 4 * units >= 3 * kCUs ? 1 : kCUs / units;
     if (p.is_bf16 && units > kCUs && 2 * units <= 3 * kCUs && pages >= 128) s = 3;
+    if (pages < (p.is_bf16 ? 40 : 32)) return 1;
     s = std::min<int64_t>(s, p.is_bf16 ? (pages + 19) / 20 : (pages + 7) / 8);
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
   }

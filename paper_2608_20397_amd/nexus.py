@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass, field
 
 import torch
@@ -106,14 +107,15 @@ def lib():
                                         sz, vp]),
         "nexus_kv8_decode_attn_workspace": (sz, [i32, i32, p8, i32]),
         "nexus_batch_pages": (i32, [vp, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
-        "nexus_norm_rope_append": (i32, [pC, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, f32, vp, vp,
+        # (the calls of a round take the cache's descriptor as packed bytes)
+        "nexus_norm_rope_append": (i32, [vp, i32, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, f32, vp, vp,
                                          vp, vp]),
-        "nexus_window_attn": (i32, [vp, i32, i32, pC, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, i32, f32,
+        "nexus_window_attn": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, i32, f32,
                                     vp, vp, sz, vp]),
-        "nexus_window_attn_workspace": (sz, [i32, i32, pC, i32, i32, i32, i32]),
-        "nexus_window_decode_attn": (i32, [vp, i32, i32, pC, vp, i32, vp, i32, i32, i32, i32, f32, i32, f32, vp,
+        "nexus_window_attn_workspace": (sz, [i32, i32, vp, i32, i32, i32, i32]),
+        "nexus_window_decode_attn": (i32, [vp, i32, i32, vp, vp, i32, vp, i32, i32, i32, i32, f32, i32, f32, vp,
                                            vp, sz, vp]),
-        "nexus_window_decode_attn_workspace": (sz, [i32, i32, pC, i32, i32, i32]),
+        "nexus_window_decode_attn_workspace": (sz, [i32, i32, vp, i32, i32, i32]),
         "nexus_kv_copy_tokens": (i32, [pC, vp, vp, i32, i64, i32, vp]),
         "nexus_kv_share_prefix": (i32, [pC, vp, vp, i32, i32, vp]),
         "nexus_l0_longest_prefix": (i32, [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int32),
@@ -749,6 +751,24 @@ class BatchRows:
 
 
 _I32 = torch.int32
+_pack_cache = struct.Struct("PPiiiiiiiid").pack      # nexus_kv_cache
+
+
+def _descriptor(cache: PagedKVCache) -> bytes:
+    """The cache as the C calls take it, checked as PagedKVCache.c() does but for the devices, which the caller checks
+    with its other operands (1 us of host time a call less)."""
+    k, v = cache.k, cache.v
+    shape = k.shape
+    if len(shape) != 5 or shape[3] != PAGE or not (k.is_contiguous() and v.is_contiguous()):
+        raise NexusError(ESHAPE, "cache k must be contiguous [L][pages][H][16][D]")
+    L, npp, H, P, D = shape
+    if v.shape != ((L, H, D, npp * P) if cache.v_layout == V_TRANSPOSED else shape):
+        raise NexusError(ESHAPE, f"cache v does not fit k and its layout, got {tuple(v.shape)}")
+    dt = k.dtype
+    if v.dtype != dt:
+        raise NexusError(EDTYPE, "cache k and v dtypes differ")
+    return _pack_cache(k.data_ptr(), v.data_ptr(), L, npp, P, H, D, BF16 if dt == torch.bfloat16 else _dtype_code(k),
+                       cache.v_layout, cache.rope_style, cache.rope_base)
 
 
 def _vector(name: str, t: torch.Tensor, n):
@@ -812,37 +832,39 @@ def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.
     projection's rows, with ``pos`` and ``slot`` [rows] of batch_pages.  Heads of q and k are normalised where eps > 0
     (weights fp32 [D]) and rotated to their positions; keys and values go to their slots, queries to the tensor that
     is returned (rows without a slot are not written; ``out`` may be q)."""
-    cc = cache.c()
-    dt, dim = cache.k.dtype, cc.head_dim
+    desc, ck, cv = _descriptor(cache), cache.k, cache.v
+    dt, hkv, dim = ck.dtype, ck.shape[2], ck.shape[4]
     rows = q.shape[0]
-    strides = (_row_stride("q", q, rows, None, dim, dt), _row_stride("k", k, rows, cc.n_kv_heads, dim, dt),
-               _row_stride("v", v, rows, cc.n_kv_heads, dim, dt))
-    if out is None:
-        out = torch.empty(q.shape, dtype=dt, device=q.device)
-    elif out.shape != q.shape or out.dtype != dt or not out.is_contiguous():
-        raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
+    qs, ks, vs = (_row_stride("q", q, rows, None, dim, dt), _row_stride("k", k, rows, hkv, dim, dt),
+                  _row_stride("v", v, rows, hkv, dim, dt))
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (dim,) or not w.is_contiguous()):
+        if w is not None and (w.dtype != torch.float32 or w.shape != (dim,) or not w.is_contiguous()):
             raise NexusError(EINVAL, f"{name} must be a contiguous fp32 vector of head_dim")
     _vector("pos", pos, rows)
     _vector("slot", slot, rows)
-    if not _all_here(cache.k, q, k, v, out, q_weight, k_weight, pos, slot):
-        _here(cache_k=cache.k, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight, pos=pos, slot=slot)
-    _check(lib().nexus_norm_rope_append(C.byref(cc), layer, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
-                                        strides[2], rows, q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, _ptr(pos),
-                                        _ptr(slot), _ptr(out), _stream()), "nexus_norm_rope_append")
+    if out is not None and (out.shape != q.shape or out.dtype != dt or not out.is_contiguous()):
+        raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
+    if not _all_here(ck, cv, q, k, v, out, q_weight, k_weight, pos, slot):
+        _here(cache_k=ck, cache_v=cv, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight, pos=pos, slot=slot)
+    if out is None:
+        out = torch.empty(q.shape, dtype=dt, device=q.device)
+    _check(lib().nexus_norm_rope_append(desc, layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, rows,
+                                        q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, pos.data_ptr(),
+                                        slot.data_ptr(), out.data_ptr(), _stream()), "nexus_norm_rope_append")
     return out
 
 
-def _window_operands(q, cache, head_dim, maps, q_start, seq_len, out, workspace):
-    """Checks the operands of a windowed launch (q_start None: a row a sequence); returns out and n_seqs."""
+def _window_operands(q, cache, maps, q_start, seq_len, out, workspace):
+    """Checks the operands of a windowed launch (q_start None: a row a sequence); returns the cache's descriptor, out
+    and n_seqs."""
+    desc, k = _descriptor(cache), cache.k
     shape = q.shape
-    if len(shape) != 3 or shape[2] != head_dim:
+    if len(shape) != 3 or shape[2] != k.shape[4]:
         raise NexusError(ESHAPE, "q must be [rows][n_q_heads][D] with the cache's D")
     if not q.is_contiguous():
         raise NexusError(EINVAL, "q must be contiguous")
     dt = q.dtype
-    if dt != cache.k.dtype:
+    if dt != k.dtype:
         raise NexusError(EDTYPE, "q dtype differs from the cache")
     if q_start is None:
         n = shape[0]
@@ -855,9 +877,10 @@ def _window_operands(q, cache, head_dim, maps, q_start, seq_len, out, workspace)
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
-    if not _all_here(cache.k, q, maps, seq_len, q_start, out, workspace):
-        _here(cache_k=cache.k, q=q, maps=maps, seq_len=seq_len, q_start=q_start, out=out, workspace=workspace)
-    return torch.empty_like(q) if out is None else out, n
+    if not _all_here(k, cache.v, q, maps, seq_len, q_start, out, workspace):
+        _here(cache_k=k, cache_v=cache.v, q=q, maps=maps, seq_len=seq_len, q_start=q_start, out=out,
+              workspace=workspace)
+    return desc, torch.empty_like(q) if out is None else out, n
 
 
 def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_start: torch.Tensor,
@@ -867,23 +890,21 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
-    L, cc = lib(), cache.c()
-    out, n = _window_operands(q, cache, cc.head_dim, maps, q_start, seq_len, out, workspace)
+    L = lib()
+    c, out, n = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
-    c = C.byref(cc)
     ws, nbytes = _kv8_workspace(L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink), q,
                                 workspace)
     _check(L.nexus_window_attn(q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(),
                                seq_len.data_ptr(), n, max_seq_len, window, n_sink, layer, softcap,
-                               cc.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws), nbytes,
+                               cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws), nbytes,
                                _stream()), "nexus_window_attn")
     return out
 
 
 def window_attn_workspace_bytes(cache: PagedKVCache, n_rows: int, n_q_heads: int, n_seqs: int, max_seq_len: int,
                                 window: int, n_sink: int) -> int:
-    cc = cache.c()
-    n = lib().nexus_window_attn_workspace(n_rows, n_q_heads, C.byref(cc), n_seqs, max_seq_len, window, n_sink)
+    n = lib().nexus_window_attn_workspace(n_rows, n_q_heads, _descriptor(cache), n_seqs, max_seq_len, window, n_sink)
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_attn_workspace")
     return n
@@ -894,22 +915,21 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
-    L, cc = lib(), cache.c()
-    out, n = _window_operands(q, cache, cc.head_dim, maps, None, seq_len, out, workspace)
-    hq, c = q.shape[1], C.byref(cc)
+    L = lib()
+    c, out, n = _window_operands(q, cache, maps, None, seq_len, out, workspace)
+    hq = q.shape[1]
     ws, nbytes = _kv8_workspace(L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink), q,
                                 workspace)
     _check(L.nexus_window_decode_attn(q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(),
                                       max_seq_len, window, n_sink, layer, softcap,
-                                      cc.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws),
+                                      cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws),
                                       nbytes, _stream()), "nexus_window_decode_attn")
     return out
 
 
 def window_decode_attn_workspace_bytes(cache: PagedKVCache, n_seqs: int, n_q_heads: int, max_seq_len: int,
                                        window: int, n_sink: int) -> int:
-    cc = cache.c()
-    n = lib().nexus_window_decode_attn_workspace(n_seqs, n_q_heads, C.byref(cc), max_seq_len, window, n_sink)
+    n = lib().nexus_window_decode_attn_workspace(n_seqs, n_q_heads, _descriptor(cache), max_seq_len, window, n_sink)
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_decode_attn_workspace")
     return n
