@@ -4,10 +4,15 @@
 //   y = x / sqrt(mean(x^2) + eps) * w,   feature pair i turned by pos * base^(-2i/D)
 //
 // HBM-bound: every row is read once and written once.  A workgroup takes a few tokens: it issues the loads of its
-// first items, forms the cosine and sine of the tokens' angles in LDS meanwhile (fp64 angle reduced modulo 2 pi, fp32
-// head + tail, as every rotation of this library), then normalises, rotates and stores.  A row lies in D / 2N
-// neighbouring lanes, N pairs each (N = 8 in bf16, 4 in fp32: both halves of a NEOX pair in one lane), so its sum of
-// squares takes log2(D / 2N) lane swaps and its pairs none.  Sums and products are fp32; the result is rounded once.
+// first items, forms the cosine and sine of the tokens' angles in LDS meanwhile, then normalises, rotates and stores.  A
+// row lies in D / 2N neighbouring lanes, N pairs each (N = 8 in bf16, 4 in fp32: both halves of a NEOX pair in one
+// lane), so its sum of squares takes log2(D / 2N) lane swaps and its pairs none.  Sums and products are fp32; the result
+// is rounded once.
+// Angles are formed and reduced modulo 2 pi in fp64.  fp32 rows take cosine and sine in fp64 and turn by head + tail
+// pairs with compensated products, as every rotation of this library; bf16 rows, whose half step is 2^16 times the
+// error of an fp32 product, take them in fp32 (within 2^-23) and turn by plain fp32 products.
+// A transposed V is written by workgroups of its own, 16 tokens of two KV heads: through LDS, so that a thread has a
+// feature of all of them and stores 16 bytes where their slots follow one another.
 #include "launch_batch.h"
 #include "rope_math.h"
 
@@ -25,24 +30,78 @@ struct NormRopeArgs {
   RopeFreq f;
   uint32_t lane_shift;      // log2 of the lanes of a row
   FastDiv div_rows;         // by the rows of a token
-  int32_t n_rows;           // n_q_heads + 2 n_kv_heads
+  int32_t n_rows;           // rows of a token that lie in rows of the cache or q_out: without a transposed V
+  uint32_t v_tiles;         // workgroups of a transposed V (the first ones)
 };
 
 }  // namespace
 
+constexpr int kVTok = 16, kVHeads = 2;      // tokens and KV heads of a workgroup that writes a transposed V
+
+// Tokens [kVTok tile, ..) of heads [kVHeads hg, ..) into the feature rows of a transposed V.
+template <typename T>
+__device__ __forceinline__ void transposed_v(const NormRopeLaunch &p, int tile, int hg, char *smem) {
+  constexpr int E = 16 / (int)sizeof(T);    // elements of 16 bytes
+  __shared__ int32_t slots[kVTok];
+  const int D = p.head_dim, t0 = tile * kVTok, n_tok = min(kVTok, p.n_tokens - t0);
+  const int heads = min(kVHeads, p.n_kv_heads - hg * kVHeads);
+  const int row = heads * D, ld = kVHeads * D + E;      // elements of a token here, and of its padded row in LDS
+  T *buf = reinterpret_cast<T *>(smem);
+  const T *src = reinterpret_cast<const T *>(p.v) + (int64_t)hg * kVHeads * D;
+  for (int i = threadIdx.x * E; i < n_tok * row; i += 256 * E) {
+    const int t = i / row, d = i - t * row;
+    *reinterpret_cast<u32x4 *>(buf + t * ld + d) =
+        *reinterpret_cast<const u32x4 *>(src + (int64_t)(t0 + t) * p.v_stride + d);
+  }
+  if (threadIdx.x < kVTok) {
+    const int s = (int)threadIdx.x < n_tok ? p.slot[t0 + threadIdx.x] : -1;
+    slots[threadIdx.x] = (uint32_t)s < (uint32_t)p.n_phys_pages * kPage ? s : -1;
+  }
+  __syncthreads();
+  const int64_t n_cols = (int64_t)p.n_phys_pages * kPage;
+  for (int d = threadIdx.x; d < row; d += 256) {
+    T *dst = reinterpret_cast<T *>(p.cache_v) + ((int64_t)hg * kVHeads * D + d) * n_cols;
+    for (int t = 0; t < n_tok;) {
+      const int s = slots[t];
+      bool run = s >= 0 && s % E == 0 && t + E <= n_tok;
+#pragma unroll
+      for (int e = 1; e < E; ++e) run = run && slots[min(t + e, kVTok - 1)] == s + e;
+      if (run) {
+        T x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = buf[(t + e) * ld + d];
+        *reinterpret_cast<u32x4 *>(dst + s) = *reinterpret_cast<u32x4 *>(x);
+        t += E;
+      } else {
+        if (s >= 0) dst[s] = buf[t * ld + d];
+        ++t;
+      }
+    }
+  }
+}
+
 template <typename T, bool INTERLEAVED, bool NORM, bool VT, int TOK>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
   constexpr int N = Pack<T>::N;
-  __shared__ float cs_tab[4][TOK][kTabPairs];
-  __shared__ __align__(16) float w_tab[2][2 * kTabPairs];
+  constexpr bool TAIL = sizeof(T) == 4;        // cosines and sines as head + tail
+  constexpr int TAB = (TAIL ? 4 : 2) * TOK * kTabPairs, WTAB = 4 * kTabPairs;
+  constexpr int VBYTES = VT ? kVTok * (kVHeads * 2 * kTabPairs * (int)sizeof(T) + 16) : 0;
+  constexpr int BYTES = 4 * (TAB + WTAB) > VBYTES ? 4 * (TAB + WTAB) : VBYTES;
+  __shared__ __align__(16) char smem[BYTES];
+  float *cs_tab = reinterpret_cast<float *>(smem);           // [cos, sin(, tails)][TOK][pairs]
+  float *w_tab = cs_tab + TAB;                               // [q, k][head_dim]
   const NormRopeLaunch &p = a.p;
+  uint32_t tile = blockIdx.x;
+  if constexpr (VT) {
+    if (tile < a.v_tiles) {
+      const uint32_t groups = (p.n_kv_heads + kVHeads - 1) / kVHeads;
+      transposed_v<T>(p, tile / groups, tile % groups, smem);
+      return;
+    }
+    tile -= a.v_tiles;
+  }
   const int D = p.head_dim, n_pairs = D / 2;
-  // transposed V: neighbouring tokens are neighbours in a feature row, so runs of tokens go to one XCD (ids 8 apart),
-  // whose L2 joins the elements to whole lines
-  const int per = VT ? (gridDim.x + 7) / 8 : 0;
-  const int tile = VT ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
   const int t0 = tile * TOK;
-  if (VT && t0 >= p.n_tokens) return;         // padding of the grid
   const int n_tok = min(TOK, p.n_tokens - t0);
   const uint32_t items = (uint32_t)(n_tok * a.n_rows) << a.lane_shift;
   const int c = threadIdx.x & ((1u << a.lane_shift) - 1);     // (the lanes of a row divide 256)
@@ -73,27 +132,34 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
   if constexpr (NORM) {
     for (int i = threadIdx.x; i < 2 * D; i += 256) {
       const float *w = i < D ? p.q_weight : p.k_weight;
-      w_tab[i >= D][i < D ? i : i - D] = w ? w[i < D ? i : i - D] : 1.f;
+      w_tab[i] = w ? w[i < D ? i : i - D] : 1.f;
     }
   }
   {
     // a thread keeps its pair (n_pairs is a power of two)
     const int i = threadIdx.x & (n_pairs - 1);
     const double theta = a.f.a[i >> 3] * a.f.b[i & 7];
-    for (int t = threadIdx.x / n_pairs; t < n_tok; t += 256 / n_pairs)
-      pair_cs_theta(p.pos[t0 + t], theta, cs_tab[0][t][i], cs_tab[1][t][i], cs_tab[2][t][i], cs_tab[3][t][i]);
+    for (int t = threadIdx.x / n_pairs; t < n_tok; t += 256 / n_pairs) {
+      float *at = cs_tab + t * kTabPairs + i;
+      constexpr int P = TOK * kTabPairs;
+      if constexpr (TAIL) {
+        pair_cs_theta(p.pos[t0 + t], theta, at[0], at[2 * P], at[P], at[3 * P]);
+      } else {
+        const double ang = (double)p.pos[t0 + t] * theta;
+        const double k = rint(ang / kTwoPiHi);
+        sincosf((float)fma(-k, kTwoPiLo, fma(-k, kTwoPiHi, ang)), at + P, at);
+      }
+    }
   }
   // LDS-only barrier: the item loads above stay in flight
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 
-  for (uint32_t it0 = 0; it0 < items; it0 += 256) {
-    const Item x0 = cur;
-    if (it0 + 256 < items) load(it0 + 256 + threadIdx.x, cur);
+  auto item = [&](uint32_t it, const Item &x0) {
     const bool is_q = x0.r < p.n_q_heads, is_v = x0.r >= p.n_q_heads + p.n_kv_heads;
     const int slot = p.slot[t0 + x0.t];
-    const bool live = it0 + threadIdx.x < items && (uint32_t)slot < (uint32_t)p.n_phys_pages * kPage;
+    const bool live = it < items && (uint32_t)slot < (uint32_t)p.n_phys_pages * kPage;
     u32x4 ya = x0.xa, yb = x0.xb;
     if (!is_v) {
       float x[2 * N], u[N], v[N];
@@ -105,7 +171,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
         for (int e = 0; e < 2 * N; ++e) ss = fmaf(x[e], x[e], ss);
         for (uint32_t off = 1u << a.lane_shift >> 1; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
         const float mean = ss / D + p.eps;
-        const float *wa = w_tab[!is_q] + ea, *wb = w_tab[!is_q] + eb;
+        const float *wa = w_tab + (is_q ? 0 : D) + ea, *wb = w_tab + (is_q ? 0 : D) + eb;
         if (mean > 1e-28f && mean < 1e36f) {
           const float r = 1.0f / sqrtf(mean);
 #pragma unroll
@@ -132,15 +198,26 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
         u[e] = INTERLEAVED ? x[2 * e] : x[e];
         v[e] = INTERLEAVED ? x[2 * e + 1] : x[N + e];
       }
-      float ch[N], cl[N], sh[N], sl[N];
+      const float *at = cs_tab + x0.t * kTabPairs + N * c;
+      constexpr int P = TOK * kTabPairs;
+      if constexpr (TAIL) {
+        float ch[N], cl[N], sh[N], sl[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        ch[e] = cs_tab[0][x0.t][N * c + e];
-        cl[e] = cs_tab[1][x0.t][N * c + e];
-        sh[e] = cs_tab[2][x0.t][N * c + e];
-        sl[e] = cs_tab[3][x0.t][N * c + e];
+        for (int e = 0; e < N; ++e) {
+          ch[e] = at[e];
+          sh[e] = at[P + e];
+          cl[e] = at[2 * P + e];
+          sl[e] = at[3 * P + e];
+        }
+        rotate<N>(u, v, ch, cl, sh, sl);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float co = at[e], si = at[P + e], xu = u[e], xv = v[e];
+          u[e] = fmaf(xu, co, -(xv * si));
+          v[e] = fmaf(xv, co, xu * si);
+        }
       }
-      rotate<N>(u, v, ch, cl, sh, sl);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         x[INTERLEAVED ? 2 * e : e] = u[e];
@@ -149,25 +226,18 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
       ya = Pack<T>::pack(x);
       yb = Pack<T>::pack(x + N);
     }
-    if (!live) continue;
+    if (!live) return;
     const int h = is_q ? x0.r : is_v ? x0.r - p.n_q_heads - p.n_kv_heads : x0.r - p.n_q_heads;
-    if (VT && is_v) {
-      // one element a feature row
-      const int64_t n_cols = (int64_t)p.n_phys_pages * kPage;
-      T *dst = reinterpret_cast<T *>(p.cache_v) + (int64_t)h * D * n_cols + slot;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        constexpr int PER = 4 / (int)sizeof(T);
-        dst[(ea + e) * n_cols] = (T)(ya[e / PER] >> (e % PER * 16));
-        dst[(eb + e) * n_cols] = (T)(yb[e / PER] >> (e % PER * 16));
-      }
-      continue;
-    }
     T *dst = is_q ? reinterpret_cast<T *>(p.q_out) + ((int64_t)(t0 + x0.t) * p.n_q_heads + h) * D
                   : reinterpret_cast<T *>(is_v ? p.cache_v : p.cache_k) +
                         (((int64_t)(slot >> kPageShift) * p.n_kv_heads + h) * kPage + (slot & (kPage - 1))) * D;
     *reinterpret_cast<u32x4 *>(dst + ea) = ya;
     *reinterpret_cast<u32x4 *>(dst + eb) = yb;
+  };
+  for (uint32_t it0 = 0; it0 < items; it0 += 256) {
+    const Item x = cur;
+    if (it0 + 256 < items) load(it0 + 256 + threadIdx.x, cur);
+    item(it0 + threadIdx.x, x);
   }
 }
 
@@ -183,16 +253,20 @@ hipError_t launch_norm_rope(const NormRopeLaunch &p, hipStream_t stream) {
   for (int i = 0; i < (p.head_dim / 2 + 7) / 8; ++i, x *= r8) a.f.a[i] = (double)x;
   const uint32_t lanes = (uint32_t)p.head_dim * p.dtype_bytes / 32;
   while ((1u << a.lane_shift) < lanes) ++a.lane_shift;
-  a.n_rows = p.n_q_heads + 2 * p.n_kv_heads;
+  a.n_rows = p.n_q_heads + (p.v_transposed ? 1 : 2) * p.n_kv_heads;
   a.div_rows = make_fastdiv((uint32_t)a.n_rows);
-  constexpr int TOK = 4;
-  const uint32_t tiles = (p.n_tokens + TOK - 1) / TOK;
-  const dim3 grid(p.v_transposed ? (tiles + 7) / 8 * 8 : tiles);
-  auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
+  a.v_tiles = p.v_transposed ? (uint32_t)((p.n_tokens + kVTok - 1) / kVTok) *
+                                   ((p.n_kv_heads + kVHeads - 1) / kVHeads) : 0;
+  // One token a workgroup, so that few tokens spread over the chip (32 rows of 40 + 16 heads of 128 bf16: 4.3 us, four
+  // tokens a workgroup 8.6; 1001 rows in fp32, transposed V: 14.2, 17.9); four where bf16 rows fill it all the same
+  // (4096 such rows 21.4 us, four 20.9; 8000 rows of 32 + 16 heads of 64: 19.7, 17.8).
+  const bool four = p.dtype_bytes == 2 && p.n_tokens >= 2048;
+  auto run = [&](auto kernel, int tok) {
+    hipLaunchKernelGGL(kernel, dim3((p.n_tokens + tok - 1) / tok + a.v_tiles), dim3(256), 0, stream, a);
     return hipGetLastError();
   };
-#define NEXUS_NORM(T, IL, NO, VT) run(norm_rope_kernel<T, IL, NO, VT, TOK>)
+#define NEXUS_NORM(T, IL, NO, VT) \
+  (four ? run(norm_rope_kernel<T, IL, NO, VT, 4>, 4) : run(norm_rope_kernel<T, IL, NO, VT, 1>, 1))
 #define NEXUS_NORM_V(T, IL, NO) (p.v_transposed ? NEXUS_NORM(T, IL, NO, true) : NEXUS_NORM(T, IL, NO, false))
 #define NEXUS_NORM_N(T, IL) (p.eps > 0.f ? NEXUS_NORM_V(T, IL, true) : NEXUS_NORM_V(T, IL, false))
 #define NEXUS_NORM_I(T) (p.interleaved ? NEXUS_NORM_N(T, true) : NEXUS_NORM_N(T, false))
