@@ -328,6 +328,16 @@ int64_t window_units(const WindowLaunch &p) {
   return (p.n_rows * group / r + p.n_seqs) * p.n_kv_heads;
 }
 
+// Microseconds per key tile of n workgroups that are on the chip together (128 rows x 64 keys, head_dim 256: 256 rows
+// x 32 keys), by launches of 96 to 1280 equal workgroups: those of a CU share its units, and a chip that is not full
+// clocks higher.
+double tile_us(const WindowLaunch &p, double n) {
+  const double layers = n / 256.;
+  if (p.head_dim == 64) return layers <= 1. ? 0.85 : 0.65 * ceil(layers);
+  if (p.head_dim == 128) return layers <= 1. ? 1.2 : 1.2 + 0.8 * (layers - 1.);
+  return 1.6 + 0.8 * layers;           // (with a soft cap 1.6 + 1.1 layers, without 1.6 + 0.45: the workspace knows of none)
+}
+
 // Splits of the keys of every row tile.
 int window_splits(const WindowLaunch &p) {
   const int64_t group = p.n_q_heads / p.n_kv_heads;
@@ -347,10 +357,9 @@ int window_splits(const WindowLaunch &p) {
     s = std::min<int64_t>(s, p.is_bf16 ? (pages + 19) / 20 : (pages + 7) / 8);
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
   }
-  // Many rows: the split count of least estimated time.  Tiles that the sequences make of the rows, taking each
-  // sequence to be of average length; workgroups spread evenly over the CUs, whose time per key tile was measured with
-  // one to five of them on a CU (microseconds: head_dim 64 and 128, 128 rows x 64 keys; 256, 256 rows x 32 keys); set-up
-  // and end of a workgroup; partials written and read at 4 TB/s.
+  // Many rows: the split count of least estimated time.  The tiles are those that sequences of average length make of
+  // the rows; workgroups take the CUs in rounds, whose time per key tile was measured (tile_us); 5 us for the set-up and
+  // end of a round's workgroups, 4 for the merge's launch, and partials written and read at 6 TB/s.
   const double r = (double)tile_rows(p), per_seq = (double)p.n_rows * group / r / p.n_seqs;
   const double units = (per_seq < 1. ? 1. : per_seq + 0.5) * p.n_seqs * p.n_kv_heads;
   const int64_t kt = p.head_dim == 256 ? 32 : 64, tiles = (keys + kt - 1) / kt;
@@ -358,12 +367,11 @@ int window_splits(const WindowLaunch &p) {
   int best = 1;
   double best_t = 1e30;
   for (int s = 1; s <= 16 && 4 * s <= tiles + 3; ++s) {
-    const int64_t on_cu = (int64_t)ceil(units * s / kCUs);
-    const double tile = p.head_dim == 64 ? (on_cu == 1 ? 0.85 : 0.65 * on_cu)
-                        : p.head_dim == 128 ? 2.0 * (on_cu / 2) + 1.2 * (on_cu % 2) : 2.05 * on_cu;
-    const int64_t together = p.head_dim == 64 ? 3 : p.head_dim == 128 ? 2 : 1;
-    double t = tile * ((tiles + s - 1) / s) + 5.0 * ((on_cu + together - 1) / together);
-    if (s > 1) t += 5.0 + elems * (4. * s + 2.) / 4e6;
+    double t = 0.;
+    const double round = p.head_dim == 64 ? 3 * kCUs : p.head_dim == 128 ? 2 * kCUs : kCUs;
+    for (double left = ceil(units * s); left > 0.; left -= round)
+      t += tile_us(p, std::min(left, round)) * (double)((tiles + s - 1) / s) + 5.;
+    if (s > 1) t += 4. + elems * (4. * s + 2.) / 6e6;
     if (t < 0.97 * best_t) {
       best_t = t;
       best = s;
