@@ -11,6 +11,7 @@
 #include "decode_common.h"
 #include "window_common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace nexus {
@@ -22,7 +23,7 @@ constexpr int kMinRun = 8;         // pages of a split at least
 
 }  // namespace
 
-template <int D, bool VT, bool CAP>
+template <int D, bool VT, bool CAP, bool NT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_decode_kernel(const WindowArgs a) {
   constexpr int NW = kDecWaves;
   constexpr int NP = D == 256 ? 1 : 2;   // pages per step of a wave
@@ -94,25 +95,29 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
     u32x4 v[VT ? 1 : VL];
     u32x2 vt[VT ? DT : 1];
   };
+  auto read = [](const auto *p) {
+    if constexpr (NT) return ld_stream(p);
+    else return *p;
+  };
   auto load_page = [&](int key0, uint32_t phys, Page &pg) {
     auto from = [&](int s) { return kl.stand_in(key0 + s) & (kPage - 1); };
     const char *kp = kbase + (size_t)phys * page_elems * 2;
     const int krow = from(qn);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      pg.k[s] = *reinterpret_cast<const u32x4 *>(kp + krow * ROWB + 64 * s + 16 * grp);
+      pg.k[s] = read(reinterpret_cast<const u32x4 *>(kp + krow * ROWB + 64 * s + 16 * grp));
     if constexpr (!VT) {
       const char *vp = vbase + (size_t)phys * page_elems * 2;
 #pragma unroll
       for (int j = 0; j < VL; ++j) {
         const int byte = 16 * lane + 1024 * j;
-        pg.v[j] = *reinterpret_cast<const u32x4 *>(vp + from(byte / ROWB) * ROWB + byte % ROWB);
+        pg.v[j] = read(reinterpret_cast<const u32x4 *>(vp + from(byte / ROWB) * ROWB + byte % ROWB));
       }
     } else {
       const char *vp = vbase + ((size_t)phys * 16 + 4 * grp) * 2;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
-        pg.vt[t] = *reinterpret_cast<const u32x2 *>(vp + (size_t)(16 * t + qn) * a.n_cols * 2);
+        pg.vt[t] = read(reinterpret_cast<const u32x2 *>(vp + (size_t)(16 * t + qn) * a.n_cols * 2));
     }
   };
 
@@ -323,15 +328,22 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
 
 hipError_t launch_window_decode(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream) {
   const dim3 grid((uint32_t)a.n_kv_heads * a.n_qgroups * a.n_splits * a.n_seqs);
+  // Keys and values that the 256 MB last-level cache cannot keep are read past it (32 sequences, window 4096, 538 MB:
+  // 95.5 -> 85.0 us); of smaller launches it keeps some for the next one (64 sequences, window 1024, 269 MB, the same
+  // layer again: 43.5, past it 49.1).
+  const int64_t keys = std::min<int64_t>((int64_t)a.window + a.sinks, a.max_len);
+  const bool past = a.n_seqs * keys * a.n_kv_heads * head_dim * 4 > (int64_t)384 << 20;
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
     return hipGetLastError();
   };
-  auto with_d = [&](auto d) {
-    if (vt)
-      return cap ? run(window_decode_kernel<d(), true, true>) : run(window_decode_kernel<d(), true, false>);
-    return cap ? run(window_decode_kernel<d(), false, true>) : run(window_decode_kernel<d(), false, false>);
+  auto with_c = [&](auto d, auto v, auto c) {
+    return past ? run(window_decode_kernel<d(), v(), c(), true>) : run(window_decode_kernel<d(), v(), c(), false>);
   };
+  auto with_v = [&](auto d, auto v) {
+    return cap ? with_c(d, v, std::true_type{}) : with_c(d, v, std::false_type{});
+  };
+  auto with_d = [&](auto d) { return vt ? with_v(d, std::true_type{}) : with_v(d, std::false_type{}); };
   if (head_dim == 64) return with_d(std::integral_constant<int, 64>{});
   if (head_dim == 128) return with_d(std::integral_constant<int, 128>{});
   return with_d(std::integral_constant<int, 256>{});
