@@ -240,15 +240,24 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
         for (int v = 0; v < 16; ++v) sc[kb][v] = a.cap_out * window_tanh(sc[kb][v] * a.cap_in);
     }
   };
+  // the mask of S(t), a page at a time: most edges of a wave's rows lie in one or two
   auto mask = [&](f32x16 *sc, int t) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int k0 = group_key(t, g) + (VT ? 8 : 4) * hh;
-      const int up = pos - k0, low = pos - a.window - k0, snk = a.sinks - k0;
+      const int k = group_key(t, g), k0 = k + (VT ? 8 : 4) * hh;
+      if (k + kPage - 1 > pa) {                                   // keys ahead of some row
+        const int up = pos - k0;
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        const int off = VT ? v : 8 * (v >> 2) + (v & 3);
-        if (off > up || (off <= low && off >= snk)) sc[g >> 1][8 * (g & 1) + v] = -INFINITY;
+        for (int v = 0; v < 8; ++v)
+          if ((VT ? v : 8 * (v >> 2) + (v & 3)) > up) sc[g >> 1][8 * (g & 1) + v] = -INFINITY;
+      }
+      if (k <= pb - a.window && k + kPage - 1 >= a.sinks) {       // keys that left some row's window
+        const int low = pos - a.window - k0, snk = a.sinks - k0;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          const int off = VT ? v : 8 * (v >> 2) + (v & 3);
+          if (off <= low && off >= snk) sc[g >> 1][8 * (g & 1) + v] = -INFINITY;
+        }
       }
     }
   };

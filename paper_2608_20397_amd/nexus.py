@@ -533,6 +533,20 @@ def _all_here(*tensors) -> bool:
     return dev >= 0 and dev == _current_device()
 
 
+def _current_of(*tensors) -> int:
+    """The current device's index where the given tensors (None among them) are all on it, else -1."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            return -1
+    return dev if dev >= 0 and dev == _current_device() else -1
+
+
+def _stream_of(dev: int):
+    """The current stream of the current device, dev."""
+    return _stream() if _raw_stream is None else _raw_stream(dev)
+
+
 def _here(**tensors):
     """The given tensors must be on the current device, to whose stream the launch goes."""
     dev = None
@@ -795,7 +809,8 @@ def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, f
     _vector("free_pages", free_pages, None)
     _vector("n_free", n_free, 1)
     _page_rows(maps, n)
-    if not _all_here(maps, cached, fresh, free_pages, n_free):
+    dev = _current_of(maps, cached, fresh, free_pages, n_free)
+    if dev < 0:
         _here(maps=maps, cached=cached, fresh=fresh, free_pages=free_pages, n_free=n_free)
     if out is None:
         out = BatchRows.empty(n, max(0, max_tokens), maps.device)
@@ -804,10 +819,12 @@ def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, f
             _vector(name, getattr(out, name), size)
         if not _all_here(out.q_start, out.seq_len, out.pos, out.slot, out.n_left):
             _here(q_start=out.q_start, seq_len=out.seq_len, pos=out.pos, slot=out.slot, n_left=out.n_left)
-    _check(lib().nexus_batch_pages(_ptr(cached), _ptr(fresh), n, _ptr(free_pages), _ptr(n_free),
-                                   free_pages.shape[0], _ptr(maps), maps.shape[1], max_tokens, _ptr(out.q_start),
-                                   _ptr(out.seq_len), _ptr(out.pos), _ptr(out.slot), _ptr(out.n_left), _stream()),
-           "nexus_batch_pages")
+    st = lib().nexus_batch_pages(cached.data_ptr(), fresh.data_ptr(), n, free_pages.data_ptr(), n_free.data_ptr(),
+                                 free_pages.shape[0], maps.data_ptr(), maps.shape[1], max_tokens,
+                                 out.q_start.data_ptr(), out.seq_len.data_ptr(), out.pos.data_ptr(),
+                                 out.slot.data_ptr(), out.n_left.data_ptr(), _stream_of(dev))
+    if st != OK:
+        raise NexusError(st, "nexus_batch_pages")
     return out
 
 
@@ -844,19 +861,22 @@ def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.
     _vector("slot", slot, rows)
     if out is not None and (out.shape != q.shape or out.dtype != dt or not out.is_contiguous()):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
-    if not _all_here(ck, cv, q, k, v, out, q_weight, k_weight, pos, slot):
+    dev = _current_of(ck, cv, q, k, v, out, q_weight, k_weight, pos, slot)
+    if dev < 0:
         _here(cache_k=ck, cache_v=cv, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight, pos=pos, slot=slot)
     if out is None:
         out = torch.empty(q.shape, dtype=dt, device=q.device)
-    _check(lib().nexus_norm_rope_append(desc, layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, rows,
-                                        q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, pos.data_ptr(),
-                                        slot.data_ptr(), out.data_ptr(), _stream()), "nexus_norm_rope_append")
+    st = lib().nexus_norm_rope_append(desc, layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, rows,
+                                      q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, pos.data_ptr(),
+                                      slot.data_ptr(), out.data_ptr(), _stream_of(dev))
+    if st != OK:
+        raise NexusError(st, "nexus_norm_rope_append")
     return out
 
 
 def _window_operands(q, cache, maps, q_start, seq_len, out, workspace):
-    """Checks the operands of a windowed launch (q_start None: a row a sequence); returns the cache's descriptor, out
-    and n_seqs."""
+    """Checks the operands of a windowed launch (q_start None: a row a sequence); returns the cache's descriptor, out,
+    n_seqs and the stream."""
     desc, k = _descriptor(cache), cache.k
     shape = q.shape
     if len(shape) != 3 or shape[2] != k.shape[4]:
@@ -877,10 +897,20 @@ def _window_operands(q, cache, maps, q_start, seq_len, out, workspace):
         raise NexusError(EINVAL, "out must be contiguous, shaped and typed like q")
     if workspace is not None and not workspace.is_contiguous():
         raise NexusError(EINVAL, "workspace must be contiguous")
-    if not _all_here(k, cache.v, q, maps, seq_len, q_start, out, workspace):
+    dev = _current_of(k, cache.v, q, maps, seq_len, q_start, out, workspace)
+    if dev < 0:
         _here(cache_k=k, cache_v=cache.v, q=q, maps=maps, seq_len=seq_len, q_start=q_start, out=out,
               workspace=workspace)
-    return desc, torch.empty_like(q) if out is None else out, n
+    return desc, torch.empty_like(q) if out is None else out, n, _stream_of(dev)
+
+
+def _window_workspace(nbytes: int, q: torch.Tensor, workspace):
+    """(tensor, pointer, bytes) of the caller's workspace, or of one allocated here, held until the call returns."""
+    if nbytes == 0 or nbytes == (1 << 64) - 1:
+        return None, 0, 0          # none needed, or invalid arguments: the call itself reports which check failed
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_start: torch.Tensor,
@@ -891,14 +921,16 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
     L = lib()
-    c, out, n = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
+    c, out, n, stream = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
-    ws, nbytes = _kv8_workspace(L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink), q,
-                                workspace)
-    _check(L.nexus_window_attn(q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(),
-                               seq_len.data_ptr(), n, max_seq_len, window, n_sink, layer, softcap,
-                               cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws), nbytes,
-                               _stream()), "nexus_window_attn")
+    ws, ws_ptr, nbytes = _window_workspace(
+        L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink), q, workspace)
+    st = L.nexus_window_attn(q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(),
+                             seq_len.data_ptr(), n, max_seq_len, window, n_sink, layer, softcap,
+                             cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), ws_ptr,
+                             nbytes, stream)
+    if st != OK:
+        raise NexusError(st, "nexus_window_attn")
     return out
 
 
@@ -916,14 +948,16 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
     L = lib()
-    c, out, n = _window_operands(q, cache, maps, None, seq_len, out, workspace)
+    c, out, n, stream = _window_operands(q, cache, maps, None, seq_len, out, workspace)
     hq = q.shape[1]
-    ws, nbytes = _kv8_workspace(L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink), q,
-                                workspace)
-    _check(L.nexus_window_decode_attn(q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(),
-                                      max_seq_len, window, n_sink, layer, softcap,
-                                      cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), _ptr(ws),
-                                      nbytes, _stream()), "nexus_window_decode_attn")
+    ws, ws_ptr, nbytes = _window_workspace(
+        L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink), q, workspace)
+    st = L.nexus_window_decode_attn(q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(),
+                                    max_seq_len, window, n_sink, layer, softcap,
+                                    cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), ws_ptr,
+                                    nbytes, stream)
+    if st != OK:
+        raise NexusError(st, "nexus_window_decode_attn")
     return out
 
 
