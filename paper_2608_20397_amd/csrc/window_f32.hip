@@ -431,7 +431,9 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   if (e != hipSuccess || a.n_splits == 1) return e;
   int lpr = 0, spr = 0;               // log2 of the lanes of a partial row, and of the groups that share its splits
   while ((half ? 8 : 4) << lpr < p.head_dim) ++lpr;
-  while (lpr + spr < 6 && 1 << spr < a.n_splits) ++spr;
+  // (few rows: their splits side by side; many: rows side by side, whose eight loads are as many as a split row's)
+  const bool many = a.n_splits <= 8 && ((int64_t)p.n_rows * p.n_q_heads << lpr) >= 64 * 2048;
+  while (!many && lpr + spr < 6 && 1 << spr < a.n_splits) ++spr;
   const uint32_t per_wg = 4u << (6 - lpr - spr);
   const dim3 grid(((uint32_t)p.n_rows * p.n_q_heads + per_wg - 1) / per_wg);
   auto merge = [&](auto kernel) {
