@@ -69,19 +69,15 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
   const int pb = __builtin_amdgcn_readfirstlane(rt.past + min(iw + 31, rt.n - 1) / G);
 
   KeyList kl{};
-  int e0 = 0, n_le = 0;                       // the split's first entry, its entries
+  TileOrder<4> order{};
   if (p1 >= 0) {
     kl = key_list(a.window, a.sinks, p0, p1);
-    const int all = (kl.n + 3) >> 2;          // tiles
-    const int t0 = (int)((int64_t)all * split / a.n_splits), t1 = (int)((int64_t)all * (split + 1) / a.n_splits);
-    e0 = 4 * t0;
-    n_le = min(4 * t1, kl.n) - e0;
-    if (t1 == t0) n_le = 0;
+    order = tile_order<4>(kl, a.period, split, a.n_splits);
   }
-  const int n_tiles = (n_le + 3) >> 2;
+  const int n_tiles = order.t1 - order.t0, n_le = 4 * n_tiles;      // steps, and entries of the ring
   const int32_t *map = a.maps + (size_t)rt.b * a.map_stride;
   // the page ring: entries 0 .. kRing - 1 here, the next half every 256 tiles
-  for (int i = tid; i < min(n_le, kRing); i += 256) pg[i] = map[kl.page(e0 + i)];
+  for (int i = tid; i < min(n_le, kRing); i += 256) pg[i] = map[kl.page(min(order.entry(i), kl.n - 1))];
 
   bf16x8 qreg[NS];
   if (active) {
@@ -149,10 +145,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
 
   auto page_of = [&](int it) -> uint32_t { return __builtin_amdgcn_readfirstlane(ring(4 * it + wave)); };
   // first key of tile `it`, and whether its 64 keys are neighbours that some row sees each
-  auto tile_key = [&](int it) { return kl.page(e0 + 4 * it) * kPage; };
+  auto tile_key = [&](int it) { return kl.page(4 * order.tile(it)) * kPage; };
   auto inner = [&](int it) {
     const int k = tile_key(it);
-    return e0 + 4 * it >= kl.sp && k >= kl.lo && k + KT <= kl.hi;
+    return 4 * order.tile(it) >= kl.sp && k >= kl.lo && k + KT <= kl.hi;
   };
   // DMA of one K or V tile (`sel` 0 = K, 1 = V) of tile `it` into this wave's quarter of the buffer at `dstp`
   auto dma_tile = [&](int it, int sel, char *dstp, uint32_t page) {
@@ -176,7 +172,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
       for (int i = 0; i < NI; ++i)
         go(i, ps, sel ? vdo ^ (16u * vswz(i * RPI)) : kdo ^ (16u * kswz(i * RPI)));
     } else {
-      const int key0 = kl.page(e0 + min(4 * it + wave, n_le - 1)) * kPage;
+      const int key0 = kl.page(min(4 * order.tile(it) + wave, kl.n - 1)) * kPage;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int slot = i * RPI + lr;
@@ -188,8 +184,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
   };
   // first key of 16-key group g of tile `it`; past every position behind the list's end
   auto group_key = [&](int it, int g) {
-    const int le = 4 * it + g;
-    return le < n_le ? kl.page(e0 + le) * kPage : 1 << 30;
+    const int e = 4 * order.tile(it) + g;
+    return e < kl.n ? kl.page(e) * kPage : 1 << 30;
   };
   // transposed V: slots that no row sees may hold anything; once such a tile has landed, the wave clears their keys
   // in its quarter
@@ -330,7 +326,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
     if ((t & 255) == 0 && t > 0) {
       // the ring's half behind this tile takes the entries 1024 ahead (looked up 254 iterations from here)
       for (int i = 4 * t + kRing / 2 + tid; i < min(4 * t + kRing, n_le); i += 256)
-        pg[i & (kRing - 1)] = map[kl.page(e0 + i)];
+        pg[i & (kRing - 1)] = map[kl.page(min(order.entry(i), kl.n - 1))];
     }
     if (active) {
       // the maximum of S(t) was taken before its mask: where there is one, mask and take it again
@@ -404,7 +400,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
   }
 
   if (!active) return;
-  store_rows<D, VT, CAP>(a, kl, rt, kvh, split, direct, e0, n_le, pair, row, pos, row_ok, hh, m_ref, l, o);
+  store_rows<D, VT, CAP>(a, kl, order, rt, kvh, split, direct, pair, row, pos, row_ok, hh, m_ref, l, o);
 }
 
 hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream) {

@@ -11,6 +11,8 @@
 
 namespace nexus {
 
+constexpr int kNoPeriod = 1 << 28;      // no list has as many tiles: each is taken from its start
+
 struct WindowArgs {
   const void *q;
   void *out;
@@ -29,6 +31,7 @@ struct WindowArgs {
   int32_t window, sinks, n_splits;
   uint32_t n_cols;        // transposed V: NPP * 16
   uint32_t n_units;       // (row tile, KV head) pairs of the launch
+  int32_t period;         // key tiles of a window, or kNoPeriod (TileOrder)
   float scale_log2;       // scale * log2(e)
   float cap_in;           // scale / softcap
   float cap_out;          // softcap * log2(e)
@@ -136,6 +139,33 @@ __device__ __forceinline__ float window_sum_halves(float x) {     // over lanes 
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The order in which a workgroup takes the tiles of PT entries that its list makes: from the first one whose place among
+// the sequence's tiles is a multiple of the period (the tiles of a window, the same for the whole launch) to the list's
+// end, then from its start.  The row tiles of a sequence, whose windows are shifted by some tokens each, then read the
+// same keys at the same time and out of one another's L2 instead of in turn.  A split has a run of this order.
+template <int PT>
+struct TileOrder {
+  int all, first, t0, t1;      // tiles of the list, the one taken first; the split's run
+  __host__ __device__ __forceinline__ int tile(int t) const {     // of the split's step t
+    const int x = t0 + t + first;
+    return x >= all ? x - all : x;
+  }
+  __host__ __device__ __forceinline__ int entry(int i) const {    // PT a step
+    return PT * tile(i / PT) + i % PT;
+  }
+};
+template <int PT>
+__host__ __device__ __forceinline__ TileOrder<PT> tile_order(const KeyList &l, int period, int split, int n_splits) {
+  TileOrder<PT> o;
+  o.all = (l.n + PT - 1) / PT;
+  const int at = (l.wp / PT) % period;
+  o.first = at == 0 ? 0 : period - at + l.sp / PT;
+  if (l.wp == 0 || o.first >= o.all) o.first = 0;
+  o.t0 = (int)((int64_t)o.all * split / n_splits);
+  o.t1 = (int)((int64_t)o.all * (split + 1) / n_splits);
+  return o;
+}
+
 // tanh x = 1 - 2 / (e^{2x} + 1); exp2 overflow to +inf gives 1, underflow to 0 gives -1.
 __device__ __forceinline__ float window_tanh(float x) {
   return 1.0f - 2.0f * __builtin_amdgcn_rcpf(fast_exp2(x * 2.8853900817779268f) + 1.0f);
@@ -148,14 +178,14 @@ __device__ __forceinline__ float part_max(float m, bool any, int split) {
   return any && split == 0 ? fmaxf(m, -3.0e38f) : m;
 }
 
-// One row taken again, key by key, from the list's entries [e0, e1): the way of rows whose result is not finite.  In a
+// One row taken again, key by key, from the list's entries entry(0) .. entry(n - 1): the way of rows whose result is not finite.  In a
 // tile of several tokens a key that one row sees is hidden from another, and the matrix product of its probability 0
 // with a value that is infinite or NaN is NaN; so the tile's product may be used where it is finite, and where it is
 // not the row is formed from the keys that it sees alone.  It costs about 1 us for 64 keys, which only such rows pay.
 // Called by a whole wave; `res` gives lane l features l, l + 64, ... of O / l, then m and l.
-template <typename T, int D, bool VT, bool CAP>
+template <typename T, int D, bool VT, bool CAP, typename Entry>
 __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl, int b, int h, const T *q, int pos,
-                                          int e0, int e1, float (&res)[(D + 63) / 64], float &m_out, float &l_out) {
+                                          int n, Entry entry, float (&res)[(D + 63) / 64], float &m_out, float &l_out) {
   constexpr int N = (D + 63) / 64, E = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63;
   const T *kc = reinterpret_cast<const T *>(a.kc), *vc = reinterpret_cast<const T *>(a.vc);
@@ -169,9 +199,10 @@ __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl
   for (int i = 0; i < N; ++i) o[i] = 0.;
   float m = -INFINITY;
   double l = 0.;
-  for (int e = e0; e < e1; e += 4) {
-    const int en = e + (lane >> 4), page = kl.page(min(en, e1 - 1)), key = page * kPage + (lane & 15);
-    const bool vis = en < e1 && key <= pos && (key > pos - a.window || key < a.sinks);
+  for (int i = 0; i < n; i += 4) {
+    const int e = entry(min(i + (lane >> 4), n - 1));
+    const int page = kl.page(min(e, kl.n - 1)), key = page * kPage + (lane & 15);
+    const bool vis = i + (lane >> 4) < n && e < kl.n && key <= pos && (key > pos - a.window || key < a.sinks);
     const uint32_t phys = vis ? (uint32_t)map[page] : 0u;
     float s = -INFINITY;
     if (vis) {
@@ -253,11 +284,13 @@ __device__ __forceinline__ void store_again(const WindowArgs &a, size_t row, int
 
 // The end of the 32x32 MFMA kernels, for a wave with rows: lane pair (j, j + 32) holds a pair's row, feature
 // 32 db + 8 gq + 4 hh + i in o[db][4 gq + i].  Rows that are not finite are taken again.
-template <int D, bool VT, bool CAP>
-__device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &kl, const RowTile &rt, int kvh,
-                                           int split, bool direct, int e0, int n_le, int pair, size_t row, int pos,
+template <int D, bool VT, bool CAP, int PT>
+__device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &kl, const TileOrder<PT> &order,
+                                           const RowTile &rt, int kvh, int split, bool direct, int pair, size_t row,
+                                           int pos,
                                            bool row_ok, int hh, float m_ref, float l, f32x16 (&o)[D / 32]) {
   constexpr int NDB = D / 32;
+  const int n_le = PT * (order.t1 - order.t0);
   const int G = a.group;
   const float l_tot = window_sum_halves(l);
   const bool empty = pos < 0 || n_le == 0;
@@ -315,7 +348,7 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
     const size_t rrow = (size_t)(rt.row0 + rtok) * a.n_q_heads + rhead;
     float res[(D + 63) / 64], m, lr_;
     row_again<uint16_t, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const uint16_t *>(a.q) + rrow * D,
-                                    rt.past + rtok, e0, e0 + n_le, res, m, lr_);
+                                    rt.past + rtok, n_le, [&](int i) { return order.entry(i); }, res, m, lr_);
     store_again<uint16_t, D, true>(a, rrow, split, direct, res, m, lr_);
   }
 }

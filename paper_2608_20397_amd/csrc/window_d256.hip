@@ -69,17 +69,14 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
   const int pb_ = __builtin_amdgcn_readfirstlane(rt.past + min(iw + 31, rt.n - 1) / G);
 
   KeyList kl{};
-  int e0 = 0, n_le = 0;                       // the split's first entry, its entries
+  TileOrder<2> order{};
   if (p1 >= 0) {
     kl = key_list(a.window, a.sinks, p0, p1);
-    const int all = (kl.n + 1) >> 1;          // tiles
-    const int t0 = (int)((int64_t)all * split / a.n_splits), t1 = (int)((int64_t)all * (split + 1) / a.n_splits);
-    e0 = 2 * t0;
-    n_le = t1 > t0 ? min(2 * t1, kl.n) - e0 : 0;
+    order = tile_order<2>(kl, a.period, split, a.n_splits);
   }
-  const int T = (n_le + 1) >> 1;
+  const int T = order.t1 - order.t0, n_le = 2 * T;                  // steps, and entries of the ring
   const int32_t *map = a.maps + (size_t)rt.b * a.map_stride;
-  for (int i = tid; i < min(n_le, kWideRing); i += 64 * W) pg[i] = map[kl.page(e0 + i)];
+  for (int i = tid; i < min(n_le, kWideRing); i += 64 * W) pg[i] = map[kl.page(min(order.entry(i), kl.n - 1))];
 
   // Q as B operands: lane (hh, j) holds Q[16 s + 8 hh .. + 7] of pair j; k-steps from NSR on in LDS (the offsets live in
   // registers, hidden from the compiler, so that buffer and block offsets fit the immediate of the LDS reads)
@@ -144,10 +141,10 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
   auto ring = [&](int le) { return pg[max(min(le, n_le - 1), 0) & (kWideRing - 1)]; };
   auto k_page = [&](int it) { return ring(2 * it + (wave >> 2)); };
   auto v_page = [&](int it) { return VT ? ring(2 * it + (vchunk >> 1)) : 0; };
-  auto tile_key = [&](int it) { return kl.page(e0 + 2 * it) * kPage; };
+  auto tile_key = [&](int it) { return kl.page(2 * order.tile(it)) * kPage; };
   auto inner = [&](int it) {
     const int k = tile_key(it);
-    return e0 + 2 * it >= kl.sp && k >= kl.lo && k + KT <= kl.hi;
+    return 2 * order.tile(it) >= kl.sp && k >= kl.lo && k + KT <= kl.hi;
   };
   // rows of this wave's page, into K (sel 0) or row-major V (sel 1)
   auto dma_rows = [&](int it, int sel, char *dstp, int page) {
@@ -159,7 +156,7 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
       dma_s<0>(dst, ps + s0 * ROWB, sel ? vdo[0] : kdo);
       dma_s<0>(dst + step, ps + (s0 + 2) * ROWB, sel ? vdo[1] : kdo);
     } else {
-      const int key0 = kl.page(e0 + min(2 * it + (wave >> 2), n_le - 1)) * kPage;
+      const int key0 = kl.page(min(2 * order.tile(it) + (wave >> 2), kl.n - 1)) * kPage;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t from = (uint32_t)kl.stand_in(key0 + s0 + 2 * i + h1) & (kPage - 1);
@@ -179,8 +176,8 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
     }
   };
   auto group_key = [&](int it, int g) {
-    const int le = 2 * it + g;
-    return le < n_le ? kl.page(e0 + le) * kPage : 1 << 30;
+    const int e = 2 * order.tile(it) + g;
+    return e < kl.n ? kl.page(e) * kPage : 1 << 30;
   };
   // transposed V: keys that no row sees, cleared in the feature rows that this wave loaded once they have landed
   auto clear_unseen = [&](int it, char *vl) {
@@ -363,7 +360,7 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
     if ((t & 511) == 0 && t > 0) {
       // the ring's half behind this tile takes the entries 1024 ahead
       for (int i = 2 * t + kWideRing / 2 + tid; i < min(2 * t + kWideRing, n_le); i += 64 * W)
-        pg[i & (kWideRing - 1)] = map[kl.page(e0 + i)];
+        pg[i & (kWideRing - 1)] = map[kl.page(min(order.entry(i), kl.n - 1))];
     }
     kp_v = kp_next;
     kp_next = k_page(t + 3);
@@ -400,7 +397,7 @@ __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a)
   }
 
   if (!active) return;
-  store_rows<D, VT, CAP>(a, kl, rt, kvh, split, direct, e0, n_le, pair, row, pos, row_ok, hh, m_ref, l, o);
+  store_rows<D, VT, CAP>(a, kl, order, rt, kvh, split, direct, pair, row, pos, row_ok, hh, m_ref, l, o);
 }
 
 hipError_t launch_window_d256(const WindowArgs &a, bool vt, bool cap, hipStream_t stream) {

@@ -38,6 +38,28 @@ static long check_list(int window, int sinks, int p0, int p1) {
   return 0;
 }
 
+// The splits' steps go through every tile of a list once.
+template <int PT>
+static bool check_order(int window, int sinks, int p0, int p1, int period) {
+  const KeyList l = key_list(window, sinks, p0, p1);
+  for (int n_splits : {1, 2, 3, 7}) {
+    const int all = (l.n + PT - 1) / PT;
+    std::vector<int> taken(all, 0);
+    for (int s = 0; s < n_splits; ++s) {
+      const TileOrder<PT> o = tile_order<PT>(l, period, s, n_splits);
+      for (int t = 0; t < o.t1 - o.t0; ++t) {
+        const int x = o.tile(t);
+        if (x < 0 || x >= all || taken[x]++) return false;
+        for (int g = 0; g < PT; ++g)
+          if (o.entry(PT * t + g) != PT * x + g) return false;
+      }
+    }
+    for (int x : taken)
+      if (x != 1) return false;
+  }
+  return true;
+}
+
 template <int R>
 static bool check_tiles(std::mt19937 &rng) {
   const int n_seqs = 1 + rng() % 70, group = 1 + rng() % 40;
@@ -66,6 +88,11 @@ int main() {
             printf("list %ld: window %d sinks %d rows %d..%d\n", e, window, sinks, p0, p1);
             return 0;
           }
+          for (int period : {1, 2, 5, 9, 1000})
+            if (!check_order<4>(window, sinks, p0, p1, period) || !check_order<2>(window, sinks, p0, p1, period)) {
+              printf("order: window %d sinks %d rows %d..%d period %d\n", window, sinks, p0, p1, period);
+              return 0;
+            }
           ++lists;
         }
   std::mt19937 rng(7);
