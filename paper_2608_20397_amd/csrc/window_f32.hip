@@ -358,19 +358,20 @@ int window_splits(const WindowLaunch &p) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
   }
   // Many rows: the split count of least estimated time.  The tiles are those that sequences of average length make of
-  // the rows; workgroups take the CUs in rounds, whose time per key tile was measured (tile_us); 5 us for the set-up and
-  // end of a round's workgroups, 4 for the merge's launch, and partials written and read at 6 TB/s.
+  // the rows, half of one more each but for one alone; workgroups take the CUs in rounds, whose time per key tile was
+  // measured (tile_us); 5 us for the set-up and end of a round's workgroups, 4 for the merge's launch, and partials
+  // written and read at 6 TB/s.
   const double r = (double)tile_rows(p), per_seq = (double)p.n_rows * group / r / p.n_seqs;
-  const double units = (per_seq < 1. ? 1. : per_seq + 0.5) * p.n_seqs * p.n_kv_heads;
+  const double units = (p.n_seqs == 1 ? ceil(per_seq) : per_seq < 1. ? 1. : per_seq + 0.5) * p.n_seqs * p.n_kv_heads;
   const int64_t kt = p.head_dim == 256 ? 32 : 64, tiles = (keys + kt - 1) / kt;
   const double elems = (double)p.n_rows * p.n_q_heads * p.head_dim;
   int best = 1;
   double best_t = 1e30;
   for (int s = 1; s <= 16 && 4 * s <= tiles + 3; ++s) {
-    double t = 0.;
     const double round = p.head_dim == 64 ? 3 * kCUs : p.head_dim == 128 ? 2 * kCUs : kCUs;
-    for (double left = ceil(units * s); left > 0.; left -= round)
-      t += tile_us(p, std::min(left, round)) * (double)((tiles + s - 1) / s) + 5.;
+    const double wgs = ceil(units * s), full = floor(wgs / round), left = wgs - full * round;
+    const double steps = (double)((tiles + s - 1) / s);
+    double t = full * (tile_us(p, round) * steps + 5.) + (left > 0. ? tile_us(p, left) * steps + 5. : 0.);
     if (s > 1) t += 4. + elems * (4. * s + 2.) / 6e6;
     if (t < 0.97 * best_t) {
       best_t = t;
