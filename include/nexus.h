@@ -437,7 +437,7 @@ size_t nexus_kv8_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const 
  * (refused for want of pages or not) are more than there are; one that needs no page is not refused for their want.
  * Checks: non-NULL arrays (free_pages too), n_seqs, map_stride, max_tokens > 0, free_capacity >= 0, written arrays
  * that overlap neither each other nor the ones read (NEXUS_EINVAL); n_seqs <= 8192, n_seqs * map_stride < 2^31
- * (NEXUS_ESHAPE); map_stride <= 2^25 (NEXUS_ERANGE).
+ * (NEXUS_ESHAPE); map_stride <= 2^25, max_tokens <= 2^30 (NEXUS_ERANGE).
  */
 nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int32_t n_seqs,
                                const int32_t *free_pages, const int32_t *n_free, int32_t free_capacity,
@@ -458,8 +458,8 @@ nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int3
  * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.
  * Checks: non-NULL q, k, v, pos, slot, q_out, n_tokens > 0, pointers (cache, rows) 16-byte aligned and strides in
  * multiples of 16 bytes that cover a row, eps finite and >= 0, no weights without a norm, q_out apart from the rows
- * read (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens *
- * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
+ * read (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens <=
+ * 2^22, n_tokens * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
  */
 nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride,
                                     const void *k, int64_t k_stride, const void *v, int64_t v_stride,

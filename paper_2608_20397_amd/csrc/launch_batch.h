@@ -48,12 +48,13 @@ struct WindowLaunch {
   bool v_transposed, is_bf16;
   float scale;                        // resolved (never 0)
   float softcap;                      // 0 = off
+  int32_t n_splits;                   // of the keys (plan_window)
   void *workspace;
 };
-// Workspace bytes of a launch (by its sizes; pointers are not looked at).
+// Chooses n_splits by the sizes (of pointers only q_start's being there counts); false: too many workgroups.
+bool plan_window(WindowLaunch &p);
+// Workspace bytes of a planned launch.
 size_t window_workspace_bytes(const WindowLaunch &p);
-// Whether its workgroups fit one grid dimension (fewer than 2^32 threads).
-bool window_grid_ok(const WindowLaunch &p);
 hipError_t launch_window(const WindowLaunch &p, hipStream_t stream);
 
 }  // namespace nexus

@@ -50,8 +50,7 @@ nexus_status window_sizes(int32_t n_rows, int32_t n_q_heads, const nexus_kv_cach
   L.is_bf16 = cache->dtype == NEXUS_BF16;
   L.window = std::min(window, std::max(max_seq_len, 1));
   L.sinks = std::min(n_sink, max_seq_len);
-  if (!window_grid_ok(L)) return NEXUS_ESHAPE;
-  return NEXUS_OK;
+  return plan_window(L) ? NEXUS_OK : NEXUS_ESHAPE;
 }
 
 nexus_status run_window(const void *q, const nexus_kv_cache *cache, const int32_t *maps, int32_t map_stride,
@@ -97,7 +96,7 @@ nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int3
     return NEXUS_EINVAL;
   if (n_seqs <= 0 || map_stride <= 0 || max_tokens <= 0 || free_capacity < 0) return NEXUS_EINVAL;
   if (n_seqs > kMaxBatchSeqs || (int64_t)n_seqs * map_stride >= kMaxElems32) return NEXUS_ESHAPE;
-  if (map_stride > kMaxWindowLen / kPageSize) return NEXUS_ERANGE;
+  if (map_stride > kMaxWindowLen / kPageSize || max_tokens > (1 << 30)) return NEXUS_ERANGE;
   // workgroups read the lengths and the list while others write: what is written stands apart
   const uint64_t seqs = 4ull * n_seqs, rows = 4ull * max_tokens;
   const struct { const void *p; uint64_t n; } out[] = {
@@ -139,7 +138,7 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
   if (layer < 0 || layer >= cache->n_layers) return NEXUS_ERANGE;
   if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads || n_q_heads > 65535 || cache->head_dim > 256)
     return NEXUS_ESHAPE;
-  if ((int64_t)n_tokens * n_q_heads * cache->head_dim >= kMaxElems32) return NEXUS_ESHAPE;
+  if ((int64_t)n_tokens * n_q_heads * cache->head_dim >= kMaxElems32 || n_tokens > (1 << 22)) return NEXUS_ESHAPE;
   if (!(eps >= 0.f) || !isfinite(eps) || (eps == 0.f && (q_weight || k_weight))) return NEXUS_EINVAL;
   const int es = dtype_bytes(cache->dtype);
   const int64_t q_row = (int64_t)n_q_heads * cache->head_dim, kv_row = (int64_t)cache->n_kv_heads * cache->head_dim;

@@ -16,6 +16,8 @@
 #include "launch_batch.h"
 #include "rope_math.h"
 
+#include <type_traits>
+
 namespace nexus {
 
 namespace {
@@ -267,16 +269,21 @@ hipError_t launch_norm_rope(const NormRopeLaunch &p, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((p.n_tokens + tok - 1) / tok + a.v_tiles), dim3(256), 0, stream, a);
     return hipGetLastError();
   };
-#define NEXUS_NORM(T, IL, NO, VT) \
-  (four ? run(norm_rope_kernel<T, IL, NO, VT, 4>, 4) : run(norm_rope_kernel<T, IL, NO, VT, 1>, 1))
-#define NEXUS_NORM_V(T, IL, NO) (p.v_transposed ? NEXUS_NORM(T, IL, NO, true) : NEXUS_NORM(T, IL, NO, false))
-#define NEXUS_NORM_N(T, IL) (p.eps > 0.f ? NEXUS_NORM_V(T, IL, true) : NEXUS_NORM_V(T, IL, false))
-#define NEXUS_NORM_I(T) (p.interleaved ? NEXUS_NORM_N(T, true) : NEXUS_NORM_N(T, false))
-  return p.dtype_bytes == 2 ? NEXUS_NORM_I(uint16_t) : NEXUS_NORM_I(uint32_t);
-#undef NEXUS_NORM_I
-#undef NEXUS_NORM_N
-#undef NEXUS_NORM_V
-#undef NEXUS_NORM
+  auto with_v = [&](auto t, auto il, auto no, auto vt) {
+    using T = decltype(t);
+    if constexpr (sizeof(T) == 2) {
+      if (four) return run(norm_rope_kernel<T, il(), no(), vt(), 4>, 4);
+    }
+    return run(norm_rope_kernel<T, il(), no(), vt(), 1>, 1);
+  };
+  using yes = std::true_type;
+  using no = std::false_type;
+  auto with_n = [&](auto t, auto il, auto n) {
+    return p.v_transposed ? with_v(t, il, n, yes{}) : with_v(t, il, n, no{});
+  };
+  auto with_i = [&](auto t, auto il) { return p.eps > 0.f ? with_n(t, il, yes{}) : with_n(t, il, no{}); };
+  auto with_t = [&](auto t) { return p.interleaved ? with_i(t, yes{}) : with_i(t, no{}); };
+  return p.dtype_bytes == 2 ? with_t(uint16_t{}) : with_t(uint32_t{});
 }
 
 }  // namespace nexus

@@ -383,12 +383,15 @@ int window_splits(const WindowLaunch &p) {
 
 }  // namespace
 
-size_t window_workspace_bytes(const WindowLaunch &p) {
-  const size_t s = (size_t)window_splits(p);
-  return s == 1 ? 0 : s * p.n_rows * p.n_q_heads * (p.head_dim * (half_parts(p) ? 2 : 4) + sizeof(f32x4));
+bool plan_window(WindowLaunch &p) {
+  p.n_splits = window_splits(p);
+  return window_units(p) * p.n_splits < (1 << 24);      // (one grid dimension holds fewer than 2^32 threads)
 }
 
-bool window_grid_ok(const WindowLaunch &p) { return window_units(p) * window_splits(p) < (1 << 24); }
+size_t window_workspace_bytes(const WindowLaunch &p) {
+  const size_t s = (size_t)p.n_splits;
+  return s == 1 ? 0 : s * p.n_rows * p.n_q_heads * (p.head_dim * (half_parts(p) ? 2 : 4) + sizeof(f32x4));
+}
 
 hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   WindowArgs a{};
@@ -409,7 +412,7 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   a.n_qgroups = (a.group + 15) / 16;
   a.window = p.window;
   a.sinks = p.sinks;
-  a.n_splits = window_splits(p);
+  a.n_splits = p.n_splits;
   a.n_cols = (uint32_t)p.n_phys_pages * 16u;
   a.n_units = (uint32_t)window_units(p);
   const bool half = half_parts(p);

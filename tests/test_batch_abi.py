@@ -64,6 +64,7 @@ def test_pages_refuses_missing_arrays(field):
 @pytest.mark.parametrize("kw,status", [
     (dict(n=0), N.EINVAL), (dict(n=-1), N.EINVAL), (dict(n=8193), N.ESHAPE), (dict(capacity=-1), N.EINVAL),
     (dict(stride=0), N.EINVAL), (dict(max_tokens=0), N.EINVAL), (dict(stride=(1 << 25) + 1), N.ERANGE),
+    (dict(max_tokens=(1 << 30) + 1, pos=1 << 40, slot=1 << 41), N.ERANGE),
     (dict(n=8192, stride=1 << 18), N.ESHAPE),
     # written arrays that meet what is read or each other: lengths in place, a count in place, one array twice
     (dict(seq_len=STEP), N.EINVAL), (dict(seq_len=2 * STEP + 8), N.EINVAL), (dict(n_left=4 * STEP), N.EINVAL),
@@ -85,7 +86,7 @@ def test_append_refuses_missing_arrays(field):
     (dict(qs=508), N.EINVAL), (dict(qs=504), N.EINVAL), (dict(ks=248), N.EINVAL), (dict(vs=0), N.EINVAL),
     (dict(qs=-512), N.EINVAL), (dict(vs=1 << 41), N.EINVAL), (dict(eps=-1e-6), N.EINVAL),
     (dict(eps=float("nan")), N.EINVAL), (dict(eps=float("inf")), N.EINVAL), (dict(eps=0.0), N.EINVAL),
-    (dict(eps=0.0, qw=0), N.EINVAL), (dict(n=1 << 24, hq=2), N.ESHAPE),
+    (dict(eps=0.0, qw=0), N.EINVAL), (dict(n=1 << 24, hq=2), N.ESHAPE), (dict(n=(1 << 22) + 1, hq=2), N.ESHAPE),
     # queries written over rows that are read: over k, into v, over q with rows of another distance, shifted by a row
     (dict(out=2 * STEP), N.EINVAL), (dict(out=3 * STEP - 16), N.EINVAL), (dict(out=STEP, qs=1024), N.EINVAL),
     (dict(out=STEP + 1024), N.EINVAL),
