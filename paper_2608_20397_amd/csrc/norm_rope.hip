@@ -11,6 +11,8 @@
 // Angles are formed and reduced modulo 2 pi in fp64.  fp32 rows take cosine and sine in fp64 and turn by head + tail
 // pairs with compensated products, as every rotation of this library; bf16 rows, whose half step is 2^16 times the
 // error of an fp32 product, take them in fp32 (within 2^-23) and turn by plain fp32 products.
+// 4096 rows of 40 + 16 heads of 128 bf16 20.8 us (117 MB, 5.6 TB/s); 1001 such rows in fp32 with a transposed V 12.7 (57
+// MB, 4.5 TB/s); one row 4.1.
 // A transposed V is written by workgroups of its own, 16 tokens of two KV heads: through LDS, so that a thread has a
 // feature of all of them and stores 16 bytes where their slots follow one another.
 #include "launch_batch.h"

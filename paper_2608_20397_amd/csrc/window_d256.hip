@@ -6,8 +6,8 @@
 // phases of 16 chunks - one MFMA, operand reads two MFMAs ahead, a few vector instructions - whose order is pinned by
 // sched_barrier: S(t + 1) = K(t + 1) Q^T beside the exponentials of S(t), then O^T += V(t)^T P(t)^T beside the soft
 // cap of S(t + 1) (in the form 1 / (2^(2 s scale log2(e) / cap) + 1), whose reciprocal is split over both phases).
-// MFMA-bound by intensity; with the schedule of window_rows_kernel (4 waves, 64-key tiles, one wave per SIMD) 1536
-// rows of 16 heads over 8 in a window of 4096, transposed V, capped, took 366 us.
+// MFMA-bound by intensity.  1536 rows of 16 heads over 8 in a window of 4096, transposed V, capped: 150 us and 11 of
+// merge, MFMA busy 44% (with the schedule of window_rows_kernel, 4 waves and 64-key tiles, 366 us).
 // LDS tiles: K rows in pairs, pair p at 1056 p (32 bytes of padding), row r of a pair at 512 r, chunk c at c ^ r.
 // Transposed V: 64-byte feature rows, chunk c at c ^ ((d >> 2) & 3), and K rows of a page permuted (bits 2 and 3 of the
 // slot swapped) so that a lane's scores are 8 consecutive keys.  Row-major V: 512-byte key rows, chunk c at

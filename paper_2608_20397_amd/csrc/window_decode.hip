@@ -3,10 +3,14 @@
 //
 // HBM-bound: window + sinks key and value rows a (sequence, KV head), read once for up to 16 query heads.  A workgroup
 // is one (sequence, KV head, query group, split) and takes a run of the list of seen pages (sinks', then window's);
-// its 4 waves take pairs of them in turn (8 waves: as fast over
-// 17473 tokens of one sequence or 32, slower with two workgroups' worth of pairs on a CU), S^T = K.Q^T and O^T += V^T.P^T on 16x16x32 MFMA straight from global memory
+// its 4 waves take pairs of them in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x32 MFMA straight from global memory
 // as decode_bf16 does (layouts there), and merge their (m, l, O) through LDS.  Slots of a listed page that the query
 // does not see are read as one that it sees (transposed V: zeroed) and masked, so that nothing in them matters.
+// 32 sequences of 17000 tokens, window 4096, 40 heads over 8 of 128: 85 us, 6.3 TB/s; one such sequence 14.0 us, 9 of them
+// in 13 splits (a chain of round trips: length, pages, keys) and the merge.  8 waves a workgroup were as fast there, slower
+// with 64 sequences (43.5, 47.6) and at head_dim 256, where two buffers of a wave do not fit.  A transposed V is read 32
+// bytes of a feature's 128-byte line at a time where neighbouring pages are not neighbours in memory (16 sequences of
+// 4096, head_dim 256: 215 us, row-major 90; 16 bytes a lane instead of 8 were no faster).
 #include "attn_dma.h"
 #include "decode_common.h"
 #include "window_common.h"
