@@ -113,11 +113,15 @@ struct KeyList {
   int n;            // entries
 
   __host__ __device__ __forceinline__ int page(int e) const { return e < sp ? e : wp + e - sp; }
-  // whether some row sees key k of a listed page
-  __host__ __device__ __forceinline__ bool seen(int k) const { return k < hi && (k >= lo || k < sink_end); }
+  // whether some row sees key k of a listed page (without a branch, as the next)
+  __host__ __device__ __forceinline__ bool seen(int k) const {
+    return (int)(k < hi) & ((int)(k >= lo) | (int)(k < sink_end));
+  }
   // a seen key of k's page, k itself if it is seen
   __host__ __device__ __forceinline__ int stand_in(int k) const {
-    return seen(k) ? k : k >= hi ? hi - 1 : (lo >> kPageShift) == (k >> kPageShift) ? lo : sink_end - 1;
+    const int in_front = (lo >> kPageShift) == (k >> kPageShift) ? lo : sink_end - 1;
+    const int other = k >= hi ? hi - 1 : in_front;
+    return seen(k) ? k : other;
   }
 };
 __host__ __device__ __forceinline__ KeyList key_list(int window, int sinks, int p0, int p1) {

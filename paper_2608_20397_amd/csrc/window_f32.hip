@@ -91,14 +91,17 @@ __global__ __launch_bounds__(64 * f32_waves(D)) void window_f32_kernel(const Win
   for (; e < e1; e += NW) {
     const int key0 = page * kPage;
     f32x4 v[DT];
+    if constexpr (VT) {
+      const float *vr = vc + ((size_t)kvh * D + qn) * a.n_cols + (size_t)phys * kPage + 4 * grp;
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      if constexpr (VT) {
-        v[t] = *reinterpret_cast<const f32x4 *>(vc + ((size_t)kvh * D + 16 * t + qn) * a.n_cols +
-                                                (size_t)phys * kPage + 4 * grp);
-      } else {
+      for (int t = 0; t < DT; ++t) v[t] = *reinterpret_cast<const f32x4 *>(vr + (size_t)(16 * t) * a.n_cols);
+    } else {
+      const float *vr = vc + page_base(phys) + qn;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[t][i] = vc[page_base(phys) + from(key0 + 4 * grp + i) * D + 16 * t + qn];
+      for (int i = 0; i < 4; ++i) {
+        const float *row = vr + from(key0 + 4 * grp + i) * D;       // (once a key, not once a feature block)
+#pragma unroll
+        for (int t = 0; t < DT; ++t) v[t][i] = row[16 * t];
       }
     }
     // two chains of MFMAs, added at the end

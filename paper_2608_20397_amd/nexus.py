@@ -759,9 +759,10 @@ class BatchRows:
 
     @classmethod
     def empty(cls, n_seqs: int, max_tokens: int, device):
-        """Unwritten, in one allocation."""
+        """Unwritten, in one allocation (the "unsafe" split skips autograd's view tracking, which integers have no use
+        for)."""
         parts = (n_seqs + 1, n_seqs, max_tokens, max_tokens, 1)
-        return cls(*torch.empty(sum(parts), dtype=torch.int32, device=device).split_with_sizes(parts))
+        return cls(*torch.empty(sum(parts), dtype=torch.int32, device=device).unsafe_split_with_sizes(parts))
 
 
 _I32 = torch.int32
