@@ -430,7 +430,8 @@ size_t nexus_kv8_decode_attn_workspace(int32_t n_seqs, int32_t n_q_heads, const 
  *                          max_tokens
  *   seq_len  [n_seqs]      cached[b] + fresh[b], or 0 for a sequence that is refused
  *   pos, slot [max_tokens] position of each row in its sequence and its place in the cache, page * 16 + token of the
- *                          page; -1 for the rows of refused sequences and for those behind the last sequence
+ *                          page; -1 for the rows of refused sequences and for those behind the last sequence (slot
+ *                          also where the map or the list holds a page outside [0, 2^27))
  *   n_left   [1]           free pages left: the first n_left[0] entries of free_pages
  * A sequence is refused, and its map row left as it is, where a length is negative, cached + fresh is more than
  * 16 * map_stride, it has rows and they pass max_tokens, or the pages that it and the sequences before it need
@@ -458,7 +459,7 @@ nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int3
  * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.
  * Checks: non-NULL q, k, v, pos, slot, q_out, n_tokens > 0, pointers (cache, rows) 16-byte aligned and strides in
  * multiples of 16 bytes that cover a row, eps finite and >= 0, no weights without a norm, q_out apart from the rows
- * read (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens <=
+ * read and both apart from the layer's K and V (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens <=
  * 2^22, n_tokens * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
  */
 nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride,
@@ -472,7 +473,8 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
  * key k when k <= p and (k > p - window or k < n_sink).
  *   q, out    [n_rows][n_q_heads][head_dim] of the cache dtype, 16-byte aligned; queries are rotated.  Rows
  *             q_start[b] .. q_start[b + 1] - 1 belong to sequence b and sit at its last positions, seq_len[b] - 1 for
- *             the last of them; rows of no sequence are left as they are in out.  out may be q.
+ *             the last of them; rows of no sequence are left as they are in out.  out may be q, but
+ *             not meet it otherwise, nor the workspace (NEXUS_EINVAL).
  *   q_start   DEVICE int32 [n_seqs + 1], not decreasing, within [0, n_rows] (clamped to it).
  *   maps, map_stride, seq_len, max_seq_len: as nexus_decode_attn (lengths clamped to [0, max_seq_len]; a row that would
  *             sit before position 0 gets zeros).  Only entries of pages that hold a key some row sees are read, so
@@ -480,7 +482,7 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
  *   window    >= 1; n_sink >= 0.  A window of max_seq_len or more is plain causal attention.
  *   layer, softcap, v_layout, scale: as nexus_suffix_attn.
  *   workspace nexus_window_attn_workspace() bytes (NULL allowed when that is 0), 16-byte aligned; contents on entry do
- *             not matter.
+ *             not matter.  Calls that overlap in time (on other streams) each need their own.
  * A key or value that is not finite reaches the queries that see it and no others; slots that no query sees may hold
  * anything.  bf16 caches: MFMA, probabilities rounded to bf16 as in nexus_suffix_attn, head_dim 64, 128 or 256.  f32
  * caches: fp32 MFMA, head_dim 16 .. 256.  Checks: the sizes and pointers above, positive n_rows and n_seqs

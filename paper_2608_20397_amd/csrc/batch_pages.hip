@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads) void batch_pages_kernel(const BatchPagesL
         phys = p.free_pages[n_free - 1 - (ahead[lo] + page)];
         if ((pos & (kPage - 1)) == 0) *entry = phys;
       }
-      slot = phys * kPage + (pos & (kPage - 1));
+      if ((uint32_t)phys < (1u << 27)) slot = phys * kPage + (pos & (kPage - 1));      // (no page's number: no slot)
     }
     p.pos[t] = pos;
     p.slot[t] = slot;

@@ -19,9 +19,13 @@ bool overlap(const void *a, uint64_t an, const void *b, uint64_t bn) {
   return x < y + bn && y < x + an;
 }
 
+// Bytes of one layer of K or V.
+uint64_t layer_bytes(const nexus_kv_cache *c) {
+  return (uint64_t)c->n_phys_pages * c->n_kv_heads * kPageSize * c->head_dim * dtype_bytes(c->dtype);
+}
+
 const char *layer_base(const void *p, const nexus_kv_cache *c, int32_t layer) {
-  return (const char *)p +
-         (size_t)layer * c->n_phys_pages * c->n_kv_heads * kPageSize * c->head_dim * dtype_bytes(c->dtype);
+  return (const char *)p + layer * layer_bytes(c);
 }
 
 // What the workspace of a windowed launch depends on (q_start: any non-null pointer stands for many rows).
@@ -68,6 +72,10 @@ nexus_status run_window(const void *q, const nexus_kv_cache *cache, const int32_
   const size_t need = window_workspace_bytes(L);
   if (need > 0 && (!workspace || workspace_bytes < need)) return NEXUS_EWORKSPACE;
   if (need > 0 && !aligned16(workspace)) return NEXUS_EINVAL;
+  // a workgroup reads its own queries before it writes their rows, so q itself may be written over
+  const uint64_t bytes = (uint64_t)L.n_rows * L.n_q_heads * L.head_dim * dtype_bytes(cache->dtype);
+  if (out != q && overlap(out, bytes, q, bytes)) return NEXUS_EINVAL;
+  if (need > 0 && (overlap(workspace, need, q, bytes) || overlap(workspace, need, out, bytes))) return NEXUS_EINVAL;
   L.q = q;
   L.out = out;
   L.cache_k = layer_base(cache->k, cache, layer);
@@ -145,7 +153,7 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
   for (const void *p : {(const void *)cache->k, (const void *)cache->v, q, k, v, (const void *)q_out})
     if (!aligned16(p)) return NEXUS_EINVAL;
   for (const int64_t s : {q_stride, k_stride, v_stride})
-    if (s <= 0 || s >= ((int64_t)1 << 40) || s * es % 16 != 0) return NEXUS_EINVAL;
+    if (s <= 0 || s >= ((int64_t)1 << 38) || s * es % 16 != 0) return NEXUS_EINVAL;
   if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row) return NEXUS_EINVAL;
   const uint64_t out_bytes = (uint64_t)n_tokens * q_row * es;
   auto bytes = [&](int64_t stride, int64_t row) { return (uint64_t)((n_tokens - 1) * stride + row) * es; };
@@ -154,6 +162,13 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
     return NEXUS_EINVAL;
   if (overlap(q_out, out_bytes, k, bytes(k_stride, kv_row)) || overlap(q_out, out_bytes, v, bytes(v_stride, kv_row)))
     return NEXUS_EINVAL;
+  const char *cache_k = layer_base(cache->k, cache, layer), *cache_v = layer_base(cache->v, cache, layer);
+  for (const char *to : {cache_k, cache_v})
+    if (overlap(to, layer_bytes(cache), q, bytes(q_stride, q_row)) ||
+        overlap(to, layer_bytes(cache), k, bytes(k_stride, kv_row)) ||
+        overlap(to, layer_bytes(cache), v, bytes(v_stride, kv_row)) ||
+        overlap(to, layer_bytes(cache), q_out, out_bytes))
+      return NEXUS_EINVAL;
   NormRopeLaunch L{};
   L.q = q;
   L.k = k;
@@ -162,8 +177,8 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
   L.k_stride = k_stride;
   L.v_stride = v_stride;
   L.q_out = q_out;
-  L.cache_k = (void *)layer_base(cache->k, cache, layer);
-  L.cache_v = (void *)layer_base(cache->v, cache, layer);
+  L.cache_k = (void *)cache_k;
+  L.cache_v = (void *)cache_v;
   L.q_weight = q_weight;
   L.k_weight = k_weight;
   L.pos = pos;

@@ -5,7 +5,8 @@
 // is one (sequence, KV head, query group, split) and takes a run of the list of seen pages (sinks', then window's);
 // its 4 waves take pairs of them in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x32 MFMA straight from global memory
 // as decode_bf16 does (layouts there), and merge their (m, l, O) through LDS.  Slots of a listed page that the query
-// does not see are read as one that it sees (transposed V: zeroed) and masked, so that nothing in them matters.
+// does not see are read as one that it sees (transposed V: zeroed) and masked, so that nothing in them matters; rows
+// that come out not finite are formed key by key (row_again).
 // 32 sequences of 17000 tokens, window 4096, 40 heads over 8 of 128: 85 us, 6.3 TB/s; one such sequence 14.0 us, 9 of them
 // in 13 splits (a chain of round trips: length, pages, keys) and the merge.  8 waves a workgroup were as fast there, slower
 // with 64 sequences (43.5, 47.6) and at head_dim 256, where two buffers of a wave do not fit.  A transposed V is read 32
@@ -314,19 +315,40 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
     if (wave < half) merge_state(wave);
   }
   if (wave != 0) return;
-  if (!q_ok) return;
-  if (direct) {
-    const float inv = 1.0f / lsum;
+  const float inv = direct || lsum > 0.f ? 1.0f / lsum : 0.f;
+  float check = 0.f;                             // NaN where a result is not finite
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<u32x2 *>(out + row * D + 16 * t + 4 * grp) =
-          u32x2{pack_bf16x2(o[t][0] * inv, o[t][1] * inv), pack_bf16x2(o[t][2] * inv, o[t][3] * inv)};
-  } else {
-    const float inv = lsum > 0.f ? 1.0f / lsum : 0.f;
+  for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.part) + slot * D + 16 * t + 4 * grp) = o[t] * inv;
-    if (grp == 0) a.part_ml[slot] = f32x4{part_max(m_ref, true, split), lsum, lsum, 0.f};
+    for (int i = 0; i < 4; ++i) {
+      o[t][i] *= inv;
+      check = fmaf(o[t][i], 0.f, check);
+    }
+  check = sum_x32(sum_x16(check));
+  const bool bad = q_ok && (!(check == 0.f) || lsum != lsum);
+  if (q_ok && !bad) {
+    if (direct) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+        *reinterpret_cast<u32x2 *>(out + row * D + 16 * t + 4 * grp) =
+            u32x2{pack_bf16x2(o[t][0], o[t][1]), pack_bf16x2(o[t][2], o[t][3])};
+    } else {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.part) + slot * D + 16 * t + 4 * grp) = o[t];
+      if (grp == 0) a.part_ml[slot] = f32x4{part_max(m_ref, true, split), lsum, lsum, 0.f};
+    }
+  }
+  // a stand-in's value that is infinite times its probability 0 is NaN
+  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && grp == 0);
+  while (left) {
+    const int r = __builtin_ctz(left);
+    left &= left - 1;
+    const size_t rrow = (size_t)b * a.n_q_heads + hq0 + r;
+    float res[D / 64], ma, la;
+    row_again<uint16_t, D, VT, CAP>(a, kl, b, h, reinterpret_cast<const uint16_t *>(a.q) + rrow * D, len - 1,
+                                    e_end - e_begin, [&](int i) { return e_begin + i; }, res, ma, la);
+    store_again<uint16_t, D, false>(a, rrow, split, direct, res, ma, la);
   }
 }
 

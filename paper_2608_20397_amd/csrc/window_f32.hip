@@ -4,9 +4,9 @@
 // fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its 8 waves (4 at head_dim 256)
 // take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory
 // (a page's values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O)
-// through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 9.5 us,
-// a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 190 us, 57 TFLOP/s (two blocks of pairs a wave:
-// 181 to 211).
+// through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3 us,
+// a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s.  4 waves, two to three
+// workgroups a CU: 146 us there, 334 rows with a transposed V 34 -> 27, but 60 rows of depth 1000 31 -> 46.
 #include "decode_common.h"
 #include "window_common.h"
 

@@ -766,6 +766,7 @@ class BatchRows:
 
 
 _I32 = torch.int32
+_TOP = (1 << 31) - 1                                 # of an int32 argument: no window, all tokens
 _pack_cache = struct.Struct("PPiiiiiiiid").pack      # nexus_kv_cache
 
 
@@ -921,6 +922,7 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
+    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
@@ -937,6 +939,7 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
 
 def window_attn_workspace_bytes(cache: PagedKVCache, n_rows: int, n_q_heads: int, n_seqs: int, max_seq_len: int,
                                 window: int, n_sink: int) -> int:
+    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
     n = lib().nexus_window_attn_workspace(n_rows, n_q_heads, _descriptor(cache), n_seqs, max_seq_len, window, n_sink)
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_attn_workspace")
@@ -948,6 +951,7 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
+    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, None, seq_len, out, workspace)
     hq = q.shape[1]
@@ -964,6 +968,7 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
 
 def window_decode_attn_workspace_bytes(cache: PagedKVCache, n_seqs: int, n_q_heads: int, max_seq_len: int,
                                        window: int, n_sink: int) -> int:
+    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
     n = lib().nexus_window_decode_attn_workspace(n_seqs, n_q_heads, _descriptor(cache), max_seq_len, window, n_sink)
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_decode_attn_workspace")

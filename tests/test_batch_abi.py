@@ -90,6 +90,9 @@ def test_append_refuses_missing_arrays(field):
     # queries written over rows that are read: over k, into v, over q with rows of another distance, shifted by a row
     (dict(out=2 * STEP), N.EINVAL), (dict(out=3 * STEP - 16), N.EINVAL), (dict(out=STEP, qs=1024), N.EINVAL),
     (dict(out=STEP + 1024), N.EINVAL),
+    # rows that lie in the layer they are written to, queries written into it; (another layer's may be read)
+    (dict(k=P), N.EINVAL), (dict(v=P + 256), N.EINVAL), (dict(q=P), N.EINVAL), (dict(out=P + 65520), N.EINVAL),
+    (dict(k=P + 65536, layer=1), N.EINVAL),
 ])
 def test_append_refuses(kw, status):
     assert append(**kw) == status
@@ -112,6 +115,16 @@ def test_window_refuses(call, kw, status):
     if call is rows and "n" in kw and kw["n"] > 0:
         kw = dict(kw, n_rows=kw["n"])
     assert call(**kw) == status
+
+
+@pytest.mark.parametrize("call", [rows, decode])
+def test_window_refuses_results_over_other_queries(call):
+    row = 4 * 128 * 2
+    for out in (P + row, P - row, P + 16):
+        assert call(out=out) == N.EINVAL
+    args = dict(n=1, max_len=4096, window=2048, stride=256)
+    for at in (P, P + row - 16, 2 * STEP - 16):
+        assert call(out=2 * STEP, ws=at, nbytes=1 << 24, **args) == N.EINVAL
 
 
 def test_window_rows_refuses():

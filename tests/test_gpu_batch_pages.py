@@ -63,6 +63,15 @@ def test_many(n, top, n_free, seed):
     run(cached, fresh, n_free, max(1, sum(fresh) // 2), (60 + top + 15) // 16, seed)
 
 
+def test_a_page_that_is_none_gives_no_slot():
+    """Numbers whose slots would pass 32 bits and come round to the cache, in the map and in the list."""
+    maps = i32([[1 << 28, 3], [-1, 2], [1, (1 << 27) - 1]])
+    rows = N.batch_pages(maps, i32([3, 2, 17]), i32([15, 1, 1]), i32([(1 << 27) + 4]), i32([1]), 17)
+    pos, slot = rows.pos.tolist(), rows.slot.tolist()
+    assert pos == list(range(3, 18)) + [2, 17]
+    assert slot == [-1] * 16 + [((1 << 27) - 1) * 16 + 1] and rows.n_left.item() == 0
+
+
 def test_refusals():
     m, c, f = i32(np.zeros((2, 4))), i32([1, 1]), i32([1, 1])
     free, n = i32(range(9)), i32([9])

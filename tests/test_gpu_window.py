@@ -157,6 +157,39 @@ def test_values_that_are_not_finite_stay_with_their_queries(dtype, dim, vt):
     within(f64(got), ref, bound, "not finite")
 
 
+@pytest.mark.parametrize("dtype,dim,vt", [(B, 64, False), (B, 64, True), (B, 128, False), (B, 256, True), (F, 64, False)])
+@pytest.mark.parametrize("lens", [[37, 1, 20], [3000, 37, 20]])
+def test_values_that_are_not_finite_in_a_decode_step(dtype, dim, vt, lens):
+    """An infinite last value (whose page's other places are read as it), one in the sinks, a key of NaN: in features
+    and sequences that see them, whole or split."""
+    window, sinks, hq, hkv = 2048, 2, 6, 2
+    pg = Paged(lens, hkv, dim, dtype, vt, seed=21)
+    inf = float("inf")
+    for b, n, head, what, value in ((0, lens[0] - 1, 0, pg.v, inf), (0, 1, 1, pg.v, -inf), (2, 7, 1, pg.k, float("nan"))):
+        what[pg.maps[b, n // 16], head, n % 16, 5] = value
+    q = torch.randn((3, hq, dim), generator=torch.Generator().manual_seed(6)).to(dtype)
+    cache, maps = pg.device()
+    got = N.window_decode_attn(q.cuda(), cache, maps, i32(lens), max(lens), window, sinks, 0)
+    ref, parts = pg.exact(q, [0, 1, 2, 3], window, sinks)
+    assert np.isposinf(ref[0, :3, 5]).all() and np.isneginf(ref[0, 3:, 5]).all() and np.isnan(ref[2, 3:]).all()
+    with np.errstate(all="ignore"):
+        bound = window_bound(ref, parts, dtype)
+    within(f64(got), ref, bound, "not finite")
+
+
+def test_a_window_past_32_bits_is_no_window():
+    pg = Paged([300, 40], 2, 64, B, seed=22)
+    cache, maps = pg.device()
+    q, lens = torch.randn((2, 4, 64), generator=torch.Generator().manual_seed(7)).to(B).cuda(), i32([300, 40])
+    want = N.window_decode_attn(q, cache, maps, lens, 300, 300, 0, 0)
+    for window, sinks in (((1 << 32) + 5, 0), (1 << 62, 0), (5, (1 << 32) + 1)):
+        got = N.window_decode_attn(q, cache, maps, lens, 300, window, sinks, 0)
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+        got = N.window_attn(q, cache, maps, i32([0, 1, 2]), lens, 300, window, sinks, 0)
+        assert torch.equal(got.view(torch.int16), N.window_attn(q, cache, maps, i32([0, 1, 2]), lens, 300, 300, 0,
+                                                                0).view(torch.int16))
+
+
 def test_rows_before_the_sequence_are_zero():
     """A length below the rows it has (a refused sequence's is 0): rows before position 0 get zeros, the others see
     what there is."""
