@@ -21,6 +21,7 @@ namespace {
 constexpr int kF32Rows = 16;       // (token, head) pairs of an fp32 workgroup
 constexpr int kMfmaRows = 128;     // of a bf16 one (window_attn.hip)
 constexpr int kWideRows = 256;     // of one of head_dim 256 (window_d256.hip)
+constexpr int kPre = 8;            // partials of a row that a lane of the merge loads at once
 constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in each lane
 
 }  // namespace
@@ -241,7 +242,7 @@ namespace {
 // loaded beside their (m, l): one round trip for rows of up to 16 splits.
 template <bool BF16, bool HALF>
 __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a, int D, int lpr_shift, int spr_shift) {
-  constexpr int E = HALF ? 8 : 4, kPre = 8;
+  constexpr int E = HALF ? 8 : 4;
   const int lane = threadIdx.x & 63;
   const uint32_t n = (uint32_t)a.n_rows * a.n_q_heads;
   const uint32_t group = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -447,8 +448,10 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   if (e != hipSuccess || a.n_splits == 1) return e;
   int lpr = 0, spr = 0;               // log2 of the lanes of a partial row, and of the groups that share its splits
   while ((half ? 8 : 4) << lpr < p.head_dim) ++lpr;
-  // (few rows: their splits side by side; many: rows side by side, whose eight loads are as many as a split row's)
-  const bool many = a.n_splits <= 8 && ((int64_t)p.n_rows * p.n_q_heads << lpr) >= 64 * 2048;
+  // Up to eight splits of rows that fill two waves a CU: rows side by side, all of a row's loads in flight (with their
+  // attention 192 rows of 40 heads of 128 in 4 splits 28.1 us, splits side by side 30.0; 64 rows 14.9, 15.4).  Few rows, and
+  // more splits: the splits side by side (4 decode rows 11.2, rows side by side 12.2).
+  const bool many = a.n_splits <= kPre && ((int64_t)p.n_rows * p.n_q_heads << lpr) >= 64 * 512;
   while (!many && lpr + spr < 6 && 1 << spr < a.n_splits) ++spr;
   const uint32_t per_wg = 4u << (6 - lpr - spr);
   const dim3 grid(((uint32_t)p.n_rows * p.n_q_heads + per_wg - 1) / per_wg);
