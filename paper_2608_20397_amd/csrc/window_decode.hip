@@ -9,9 +9,10 @@
 // that come out not finite are formed key by key (row_again).
 // 32 sequences of 17000 tokens, window 4096, 40 heads over 8 of 128: 85 us, 6.3 TB/s; one such sequence 14.0 us, 9 of them
 // in 13 splits (a chain of round trips: length, pages, keys) and the merge.  8 waves a workgroup were as fast there, slower
-// with 64 sequences (43.5, 47.6) and at head_dim 256, where two buffers of a wave do not fit.  A transposed V is read 32
-// bytes of a feature's 128-byte line at a time where neighbouring pages are not neighbours in memory (16 sequences of
-// 4096, head_dim 256: 215 us, row-major 90; 16 bytes a lane instead of 8 were no faster).
+// with 64 sequences (43.5, 47.6) and at head_dim 256, where two buffers of a wave do not fit.  A page of a transposed V
+// is 32 bytes of each feature's 128-byte lines, which come whole from memory (16 sequences of 4096, head_dim 256: 178 us
+// where the pages of a line are other sequences', 111 where they follow one another, row-major 90; 16 bytes a lane instead
+// of 8 were no faster, runs of four pages a wave slower).
 #include "attn_dma.h"
 #include "decode_common.h"
 #include "window_common.h"
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
       const char *vp = vbase + ((size_t)phys * 16 + 4 * grp) * 2;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
-        pg.vt[t] = read(reinterpret_cast<const u32x2 *>(vp + (size_t)(16 * t + qn) * a.n_cols * 2));
+        pg.vt[t] = *reinterpret_cast<const u32x2 *>(vp + (size_t)(16 * t + qn) * a.n_cols * 2);
     }
   };
 
@@ -356,7 +357,8 @@ hipError_t launch_window_decode(const WindowArgs &a, int head_dim, bool vt, bool
   const dim3 grid((uint32_t)a.n_kv_heads * a.n_qgroups * a.n_splits * a.n_seqs);
   // Keys and values that the 256 MB last-level cache cannot keep are read past it (32 sequences, window 4096, 538 MB:
   // 95.5 -> 85.0 us); of smaller launches it keeps some for the next one (64 sequences, window 1024, 269 MB, the same
-  // layer again: 43.5, past it 49.1).
+  // layer again: 43.5, past it 49.1)  A transposed V never is: its lines serve several pages (the two
+  // launches above 215 -> 178 and 176 -> 111).
   const int64_t keys = std::min<int64_t>((int64_t)a.window + a.sinks, a.max_len);
   const bool past = a.n_seqs * keys * a.n_kv_heads * head_dim * 4 > (int64_t)384 << 20;
   auto run = [&](auto kernel) {
