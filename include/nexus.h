@@ -459,8 +459,8 @@ nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int3
  * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.
  * Checks: non-NULL q, k, v, pos, slot, q_out, n_tokens > 0, pointers (cache, rows) 16-byte aligned and strides in
  * multiples of 16 bytes that cover a row, eps finite and >= 0, no weights without a norm, q_out apart from the rows
- * read and both apart from the layer's K and V (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of n_kv_heads, head_dim <= 256, n_tokens <=
- * 2^22, n_tokens * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
+ * read and both apart from the layer's K and V (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of
+ * n_kv_heads, head_dim <= 256, n_tokens <= 2^22, n_tokens * n_q_heads * head_dim < 2^31 (NEXUS_ESHAPE).
  */
 nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, const void *q, int64_t q_stride,
                                     const void *k, int64_t k_stride, const void *v, int64_t v_stride,

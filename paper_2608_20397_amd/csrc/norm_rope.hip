@@ -236,7 +236,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
                   : reinterpret_cast<T *>(is_v ? p.cache_v : p.cache_k) +
                         (((int64_t)(slot >> kPageShift) * p.n_kv_heads + h) * kPage + (slot & (kPage - 1))) * D;
     // (past the caches: 4096 rows of 40 + 16 heads of 128 bf16 after other data 28.2 -> 27.2 us, 1001 fp32 rows 20.0 ->
-    // 17.8, the same rows over and over 20.9 -> 20.8 and 14.5 -> 12.7; the loads, often of what was just computed, are not)
+    // 17.8, the same rows over and over 20.9 -> 20.8 and 14.5 -> 12.7; the loads, often of what was just computed, are
+    // not)
     st_stream(ya, reinterpret_cast<u32x4 *>(dst + ea));
     st_stream(yb, reinterpret_cast<u32x4 *>(dst + eb));
   };

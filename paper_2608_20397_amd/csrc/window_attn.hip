@@ -1,5 +1,6 @@
-// Windowed attention of many rows, bf16, head_dim 64 and 128 (MFMA): every row of a ragged batch sees the last `window` keys of its own
-// sequence and the first `sinks` ones (Sec. III-A's attention, restricted as models with local layers do).
+// Windowed attention of many rows, bf16, head_dim 64 and 128 (MFMA): every row of a ragged batch sees the last `window`
+// keys of its own sequence and the first `sinks` ones (Sec. III-A's attention, restricted as models with local layers
+// do).
 //
 // softmax(s) V with s = scale q.k (soft-capped or not) over the keys that the row sees, in one pass with a running
 // maximum and sum (log2 units), O^T += V^T.P^T and S^T = K.Q^T on 32x32x16 MFMA.
@@ -160,9 +161,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
     const uint32_t dst = smem_base + (uint32_t)(dstp - smem) + wave * QTRB;
     auto go = [&](int i, const char *s, uint32_t voff) {
       if (i == 0) dma_s<0>(dst, s, voff);
-      else if (i == 1) dma_s<1024>(dst, s, voff);
-      else if (i == 2) dma_s<2048>(dst, s, voff);
-      else dma_s<3072>(dst, s, voff);
+      else if (i == 1) dma_s<1 * 1024>(dst, s, voff);
+      else if (i == 2) dma_s<2 * 1024>(dst, s, voff);
+      else dma_s<3 * 1024>(dst, s, voff);
     };
     if (VT && sel) {
 #pragma unroll

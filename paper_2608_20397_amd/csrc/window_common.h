@@ -182,8 +182,8 @@ __device__ __forceinline__ float part_max(float m, bool any, int split) {
   return any && split == 0 ? fmaxf(m, -3.0e38f) : m;
 }
 
-// One row taken again, key by key, from the list's entries entry(0) .. entry(n - 1): the way of rows whose result is not finite.  In a
-// tile of several tokens a key that one row sees is hidden from another, and the matrix product of its probability 0
+// One row taken again, key by key, from the list's entries entry(0) .. entry(n - 1): the way of rows whose result is not
+// finite.  In a tile of several tokens a key that one row sees is hidden from another, and the matrix product of its probability 0
 // with a value that is infinite or NaN is NaN; so the tile's product may be used where it is finite, and where it is
 // not the row is formed from the keys that it sees alone.  It costs about 1 us for 64 keys, which only such rows pay.
 // Called by a whole wave; `res` gives lane l features l, l + 64, ... of O / l, then m and l.
@@ -291,8 +291,7 @@ __device__ __forceinline__ void store_again(const WindowArgs &a, size_t row, int
 template <int D, bool VT, bool CAP, int PT>
 __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &kl, const TileOrder<PT> &order,
                                            const RowTile &rt, int kvh, int split, bool direct, int pair, size_t row,
-                                           int pos,
-                                           bool row_ok, int hh, float m_ref, float l, f32x16 (&o)[D / 32]) {
+                                           int pos, bool row_ok, int hh, float m_ref, float l, f32x16 (&o)[D / 32]) {
   constexpr int NDB = D / 32;
   const int n_le = PT * (order.t1 - order.t0);
   const int G = a.group;

@@ -7,12 +7,12 @@
 // as decode_bf16 does (layouts there), and merge their (m, l, O) through LDS.  Slots of a listed page that the query
 // does not see are read as one that it sees (transposed V: zeroed) and masked, so that nothing in them matters; rows
 // that come out not finite are formed key by key (row_again).
-// 32 sequences of 17000 tokens, window 4096, 40 heads over 8 of 128: 85 us, 6.3 TB/s; one such sequence 14.0 us, 9 of them
-// in 13 splits (a chain of round trips: length, pages, keys) and the merge.  8 waves a workgroup were as fast there, slower
+// 32 sequences of 17000 tokens, window 4096, 40 heads over 8 of 128: 85 us, 6.3 TB/s; one such sequence 14 us: 9 in 13
+// splits (a chain of round trips: length, pages, keys) and the merge.  8 waves a workgroup were as fast there, slower
 // with 64 sequences (43.5, 47.6) and at head_dim 256, where two buffers of a wave do not fit.  A page of a transposed V
-// is 32 bytes of each feature's 128-byte lines, which come whole from memory (16 sequences of 4096, head_dim 256: 178 us
-// where the pages of a line are other sequences', 111 where they follow one another, row-major 90; 16 bytes a lane instead
-// of 8 were no faster, runs of four pages a wave slower).
+// is 32 bytes of each feature's 128-byte lines, which come whole from memory (16 sequences of 4096, head_dim 256: 178
+// us where the pages of a line are other sequences', 111 where they follow one another, row-major 90; 16 bytes a lane
+// instead of 8 were no faster, runs of four pages a wave slower).
 #include "attn_dma.h"
 #include "decode_common.h"
 #include "window_common.h"

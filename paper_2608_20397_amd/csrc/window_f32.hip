@@ -4,9 +4,10 @@
 // fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its 8 waves (4 at head_dim 256)
 // take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory
 // (a page's values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O)
-// through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3 us,
-// a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s.  4 waves, two to three
-// workgroups a CU: 146 us there, 334 rows with a transposed V 34 -> 27, but 60 rows of depth 1000 31 -> 46.
+// through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3
+// us, a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a CU of
+// which two run together.  4 waves: 146 us there, 334 rows with a transposed V 34 -> 27, but 60 rows of depth 1000 31 ->
+// 46; two blocks of pairs a workgroup: 164, 62 -> 71 and 12 -> 19 in other launches.
 #include "decode_common.h"
 #include "window_common.h"
 
@@ -341,7 +342,8 @@ double tile_us(const WindowLaunch &p, double n) {
   const double layers = n / 256.;
   if (p.head_dim == 64) return layers <= 1. ? 0.85 : 0.65 * ceil(layers);
   if (p.head_dim == 128) return layers <= 1. ? 1.2 : 1.2 + 0.8 * (layers - 1.);
-  return 1.6 + 0.8 * layers;           // (with a soft cap 1.6 + 1.1 layers, without 1.6 + 0.45: the workspace knows of none)
+  // (with a soft cap 1.6 + 1.1 layers, without 1.6 + 0.45: the workspace knows of none)
+  return 1.6 + 0.8 * layers;
 }
 
 // Splits of the keys of every row tile.
@@ -352,10 +354,11 @@ int window_splits(const WindowLaunch &p) {
   const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len), pages = (keys + 15) / 16;
   if (p.q_start == nullptr || !p.is_bf16) {
     // One workgroup a CU, of at least 20 pages in bf16 and 8 in fp32 (whose 8 waves take a page each), lists of under
-    // twice and four times that whole (a merge costs 4 us of host time); from three quarters of the CUs on one split, which needs no merge, is as fast or faster (8 KV heads of 128, window 4096:
-    // one sequence 49 us, in 12 splits 12.9, in 24 13.9; 8 sequences 55, in 3 or 4 28, in 8 29.5; 24: 73, in 2 82;
-    // 32: 96, in 2 100), but for long windows and between one workgroup a CU and one and a half (40 sequences 142,
-    // in 3 125; window 1024, head_dim 64: 20.6, in 3 20.7).
+    // twice and four times that whole (a merge costs 4 us of host time); from three quarters of the CUs on one split,
+    // which needs no merge, is as fast or faster (8 KV heads of 128, window 4096: one sequence 49 us, in 12 splits 12.9,
+    // in 24 13.9; 8 sequences 55, in 3 or 4 28, in 8 29.5; 24: 73, in 2 82; 32: 96, in 2 100), but for long windows and
+    // between one workgroup a CU and one and a half (40 sequences 142, in 3 125; window 1024, head_dim 64: 20.6, in 3
+    // 20.7).
     const int64_t units = window_units(p);
     int64_t s = 4 * units >= 3 * kCUs ? 1 : kCUs / units;
     if (p.is_bf16 && units > kCUs && 2 * units <= 3 * kCUs && pages >= 128) s = 3;
@@ -449,8 +452,8 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   int lpr = 0, spr = 0;               // log2 of the lanes of a partial row, and of the groups that share its splits
   while ((half ? 8 : 4) << lpr < p.head_dim) ++lpr;
   // Up to eight splits of rows that fill two waves a CU: rows side by side, all of a row's loads in flight (with their
-  // attention 192 rows of 40 heads of 128 in 4 splits 28.1 us, splits side by side 30.0; 64 rows 14.9, 15.4).  Few rows, and
-  // more splits: the splits side by side (4 decode rows 11.2, rows side by side 12.2).
+  // attention 192 rows of 40 heads of 128 in 4 splits 28.1 us, splits side by side 30.0; 64 rows 14.9, 15.4).  Few rows,
+  // and more splits: the splits side by side (4 decode rows 11.2, rows side by side 12.2).
   const bool many = a.n_splits <= kPre && ((int64_t)p.n_rows * p.n_q_heads << lpr) >= 64 * 512;
   while (!many && lpr + spr < 6 && 1 << spr < a.n_splits) ++spr;
   const uint32_t per_wg = 4u << (6 - lpr - spr);
