@@ -1,13 +1,12 @@
 // Windowed attention over fp32 caches (many rows or one a sequence), the merge of split results and the launch of all
 // windowed attention.
 //
-// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its 8 waves (4 at head_dim 256)
-// take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory
-// (a page's values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O)
-// through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3
-// us, a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a CU of
-// which two run together.  4 waves: 146 us there, 334 rows with a transposed V 34 -> 27, but 60 rows of depth 1000 31 ->
-// 46; two blocks of pairs a workgroup: 164, 62 -> 71 and 12 -> 19 in other launches.
+// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its waves (f32_waves) take the
+// pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory (a page's
+// values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O) through LDS.
+// Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3 us, a chain of
+// round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a CU of which four run
+// together; two blocks of pairs a workgroup 164.
 #include "decode_common.h"
 #include "window_common.h"
 
@@ -27,11 +26,8 @@ constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in ea
 
 }  // namespace
 
-constexpr int f32_waves(int head_dim) { return head_dim == 256 ? 4 : 8; }
-
-template <int D, bool VT, bool CAP>
-__global__ __launch_bounds__(64 * f32_waves(D)) void window_f32_kernel(const WindowArgs a) {
-  constexpr int NW = f32_waves(D);
+template <int D, bool VT, bool CAP, int NW>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void window_f32_kernel(const WindowArgs a) {
   constexpr int DT = D / 16;          // O^T tiles, and 16-feature steps of S^T
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer
   __shared__ float mo[NW / 2 * 16 * MO_LD];
@@ -216,16 +212,23 @@ __global__ __launch_bounds__(64 * f32_waves(D)) void window_f32_kernel(const Win
   }
 }
 
-hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream) {
+hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, hipStream_t stream) {
   const dim3 grid(a.n_units * a.n_splits);
   auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * f32_waves(head_dim)), 0, stream, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a);
     return hipGetLastError();
   };
-  auto with_d = [&](auto d) {
-    if (vt) return cap ? run(window_f32_kernel<d(), true, true>) : run(window_f32_kernel<d(), true, false>);
-    return cap ? run(window_f32_kernel<d(), false, true>) : run(window_f32_kernel<d(), false, false>);
+  auto with_w = [&](auto d, auto v, auto c) {
+    if (waves == 2) return run(window_f32_kernel<d(), v(), c(), 2>);
+    if constexpr (d() < 256) {
+      if (waves == 8) return run(window_f32_kernel<d(), v(), c(), 8>);
+    }
+    return run(window_f32_kernel<d(), v(), c(), 4>);
   };
+  auto with_v = [&](auto d, auto v) {
+    return cap ? with_w(d, v, std::true_type{}) : with_w(d, v, std::false_type{});
+  };
+  auto with_d = [&](auto d) { return vt ? with_v(d, std::true_type{}) : with_v(d, std::false_type{}); };
   switch (head_dim) {
     case 16: return with_d(std::integral_constant<int, 16>{});
     case 32: return with_d(std::integral_constant<int, 32>{});
@@ -346,12 +349,28 @@ double tile_us(const WindowLaunch &p, double n) {
   return 1.6 + 0.8 * layers;
 }
 
+// Pages of the longest list of a row tile.
+int64_t list_pages(const WindowLaunch &p) {
+  const int64_t group = p.n_q_heads / p.n_kv_heads, rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;
+  return (std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len) + 15) / 16;
+}
+
+// Waves of an fp32 workgroup.  Eight (head_dim 256, whose registers leave a SIMD one wave: four) where the chip has room
+// for every workgroup at once and a list's length is what a launch takes; with more workgroups fewer merge less, and of
+// short lists two (8, 4, 2 waves; 40 heads over 8 of 128 and 32 of 64: 60 rows at 1000 30, 50, 61 us; 334 at 0 31, 27, 31;
+// 1024 at 0, head_dim 64, 62, 57, 71; 43 sequences of 62 rows at 10 101, 72, 60, at 100 232, 165, 115; 2000 rows, window 64,
+// 96, 71, 60; 64 x 16 at 200 101, 79, 82; head_dim 256, 10 x 200 at 0 -, 138, 91, 400 at 500 -, 95, 106).
+int f32_waves(const WindowLaunch &p) {
+  const int64_t wgs = window_units(p) * p.n_splits;
+  if (wgs > 4 * 256 && list_pages(p) <= 16) return 2;
+  return wgs > 2 * 256 || p.head_dim == 256 ? 4 : 8;
+}
+
 // Splits of the keys of every row tile.
 int window_splits(const WindowLaunch &p) {
   const int64_t group = p.n_q_heads / p.n_kv_heads;
   constexpr int64_t kCUs = 256;
-  const int64_t rows = p.q_start == nullptr ? 1 : tile_rows(p) / group + 1;    // tokens of a tile
-  const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len), pages = (keys + 15) / 16;
+  const int64_t pages = list_pages(p);
   if (p.q_start == nullptr || !p.is_bf16) {
     // One workgroup a CU, of at least 20 pages in bf16 and 8 in fp32 (whose 8 waves take a page each), lists of under
     // twice and four times that whole (a merge costs 4 us of host time); from three quarters of the CUs on one split,
@@ -372,7 +391,7 @@ int window_splits(const WindowLaunch &p) {
   // written and read at 6 TB/s.
   const double r = (double)tile_rows(p), per_seq = (double)p.n_rows * group / r / p.n_seqs;
   const double units = (p.n_seqs == 1 ? ceil(per_seq) : per_seq < 1. ? 1. : per_seq + 0.5) * p.n_seqs * p.n_kv_heads;
-  const int64_t kt = p.head_dim == 256 ? 32 : 64, tiles = (keys + kt - 1) / kt;
+  const int64_t kt = p.head_dim == 256 ? 2 : 4, tiles = (pages + kt - 1) / kt;       // pages of a tile
   const double elems = (double)p.n_rows * p.n_q_heads * p.head_dim;
   int best = 1;
   double best_t = 1e30;
@@ -444,7 +463,7 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   a.cap_k = p.softcap > 0.f ? 2.0f * p.scale * log2e / p.softcap : 0.f;
   const bool cap = p.softcap > 0.f;
   hipError_t e;
-  if (!p.is_bf16) e = launch_window_f32(a, p.head_dim, p.v_transposed, cap, stream);
+  if (!p.is_bf16) e = launch_window_f32(a, p.head_dim, p.v_transposed, cap, f32_waves(p), stream);
   else if (p.q_start == nullptr) e = launch_window_decode(a, p.head_dim, p.v_transposed, cap, stream);
   else if (p.head_dim == 256) e = launch_window_d256(a, p.v_transposed, cap, stream);
   else e = launch_window_rows(a, p.head_dim, p.v_transposed, cap, stream);

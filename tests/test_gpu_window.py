@@ -71,6 +71,33 @@ def test_forms(hq, hkv, dim, dtype, vt, cap):
     run([(100, 130), (0, 1)], 100000, 0, seed=4, **kw)
 
 
+@pytest.mark.parametrize("dim,vt,cap", [(16, False, 0.0), (32, True, 10.0), (64, False, 0.0), (64, True, 0.0),
+                                        (128, False, 20.0), (128, True, 0.0), (256, False, 0.0), (256, True, 50.0)])
+def test_many_fp32_workgroups(dim, vt, cap):
+    """More of them than run together: fewer waves each, two where lists are short, four where they are long."""
+    few = [(20 + b % 31, 1 + b % 24) for b in range(60)]
+    run(few, 40, 3, hq=8, hkv=8, dim=dim, dtype=F, vt=vt, cap=cap, seed=31, pad=2)
+    run([(7 * b, 300 - 5 * b) for b in range(6)] + [(350, 3)], 290, 3, hq=8, hkv=8, dim=dim, dtype=F, vt=vt, cap=cap,
+        seed=32)
+
+
+def test_many_fp32_workgroups_with_values_that_are_not_finite():
+    lens = [40 + b for b in range(60)]
+    q_start = [20 * b for b in range(61)]
+    pg = Paged(lens, 8, 32, F, False, seed=33)
+    for b in range(0, 60, 7):
+        n = lens[b] - 5
+        pg.v[pg.maps[b, n // 16], b % 8, n % 16, b % 32] = float("inf")
+    q = torch.randn((1200, 8, 32), generator=torch.Generator().manual_seed(34)).to(F)
+    cache, maps = pg.device()
+    got = N.window_attn(q.cuda(), cache, maps, i32(q_start), i32(lens), 99, 30, 2, 0)
+    ref, parts = pg.exact(q, q_start, 30, 2)
+    assert np.isinf(ref).any() and not np.isnan(ref).any()
+    with np.errstate(all="ignore"):
+        bound = window_bound(ref, parts, F)
+    within(f64(got), ref, bound, "not finite")
+
+
 def test_peaked_scores_and_scale():
     """Scores of standard deviation about 11 (the running maximum moves), a scale of its own, another layer."""
     run([(200, 100)], 150, 3, hq=8, hkv=2, dim=128, std=11.0, seed=5)
