@@ -906,13 +906,18 @@ def _window_operands(q, cache, maps, q_start, seq_len, out, workspace):
     return desc, torch.empty_like(q) if out is None else out, n, _stream_of(dev)
 
 
-def _window_workspace(nbytes: int, q: torch.Tensor, workspace):
-    """(tensor, pointer, bytes) of the caller's workspace, or of one allocated here, held until the call returns."""
-    if nbytes == 0 or nbytes == (1 << 64) - 1:
-        return None, 0, 0          # none needed, or invalid arguments: the call itself reports which check failed
+def _window_call(call, need, args, q: torch.Tensor, workspace, stream, what: str):
+    """call(*args, workspace, bytes, stream); need() are the bytes of a workspace that the caller has not given, asked for
+    only where the call says that it needs one (nothing is enqueued then)."""
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        st = call(*args, 0, 0, stream)
+        if st == EWORKSPACE:
+            workspace = torch.empty(need(), dtype=torch.uint8, device=q.device)     # held until the call returns
+            st = call(*args, workspace.data_ptr(), workspace.numel(), stream)
+    else:
+        st = call(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    if st != OK:
+        raise NexusError(st, what)
 
 
 def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_start: torch.Tensor,
@@ -922,18 +927,15 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
-    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
+    window, n_sink = window if window < _TOP else _TOP, n_sink if n_sink < _TOP else _TOP
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
-    ws, ws_ptr, nbytes = _window_workspace(
-        L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink), q, workspace)
-    st = L.nexus_window_attn(q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(),
-                             seq_len.data_ptr(), n, max_seq_len, window, n_sink, layer, softcap,
-                             cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), ws_ptr,
-                             nbytes, stream)
-    if st != OK:
-        raise NexusError(st, "nexus_window_attn")
+    _window_call(L.nexus_window_attn,
+                 lambda: L.nexus_window_attn_workspace(rows, hq, c, n, max_seq_len, window, n_sink),
+                 (q.data_ptr(), rows, hq, c, maps.data_ptr(), maps.shape[1], q_start.data_ptr(), seq_len.data_ptr(), n,
+                  max_seq_len, window, n_sink, layer, softcap, cache.v_layout if v_layout is None else v_layout, scale,
+                  out.data_ptr()), q, workspace, stream, "nexus_window_attn")
     return out
 
 
@@ -951,18 +953,15 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
-    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
+    window, n_sink = window if window < _TOP else _TOP, n_sink if n_sink < _TOP else _TOP
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, None, seq_len, out, workspace)
     hq = q.shape[1]
-    ws, ws_ptr, nbytes = _window_workspace(
-        L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink), q, workspace)
-    st = L.nexus_window_decode_attn(q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(),
-                                    max_seq_len, window, n_sink, layer, softcap,
-                                    cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr(), ws_ptr,
-                                    nbytes, stream)
-    if st != OK:
-        raise NexusError(st, "nexus_window_decode_attn")
+    _window_call(L.nexus_window_decode_attn,
+                 lambda: L.nexus_window_decode_attn_workspace(n, hq, c, max_seq_len, window, n_sink),
+                 (q.data_ptr(), n, hq, c, maps.data_ptr(), maps.shape[1], seq_len.data_ptr(), max_seq_len, window,
+                  n_sink, layer, softcap, cache.v_layout if v_layout is None else v_layout, scale, out.data_ptr()),
+                 q, workspace, stream, "nexus_window_decode_attn")
     return out
 
 
