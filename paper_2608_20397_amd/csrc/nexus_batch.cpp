@@ -52,6 +52,7 @@ nexus_status window_sizes(int32_t n_rows, int32_t n_q_heads, const nexus_kv_cach
   L.n_q_heads = n_q_heads;
   L.head_dim = cache->head_dim;
   L.is_bf16 = cache->dtype == NEXUS_BF16;
+  L.v_transposed = cache->v_layout == NEXUS_V_TRANSPOSED;
   L.window = std::min(window, std::max(max_seq_len, 1));
   L.sinks = std::min(n_sink, max_seq_len);
   return plan_window(L) ? NEXUS_OK : NEXUS_ESHAPE;
@@ -83,7 +84,6 @@ nexus_status run_window(const void *q, const nexus_kv_cache *cache, const int32_
   L.maps = maps;
   L.seq_len = seq_len;
   L.map_stride = map_stride;
-  L.v_transposed = cache->v_layout == NEXUS_V_TRANSPOSED;
   L.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim);
   L.softcap = softcap;
   L.workspace = workspace;

@@ -360,6 +360,6 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
 hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_d256(const WindowArgs &a, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_decode(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
-hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, hipStream_t stream);
+hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks, hipStream_t stream);
 
 }  // namespace nexus

@@ -6,7 +6,7 @@
 // values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O) through LDS.
 // Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3 us, a chain of
 // round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a CU of which four run
-// together; two blocks of pairs a workgroup 164.
+// together.
 #include "decode_common.h"
 #include "window_common.h"
 
@@ -26,8 +26,8 @@ constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in ea
 
 }  // namespace
 
-template <int D, bool VT, bool CAP, int NW>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void window_f32_kernel(const WindowArgs a) {
+template <int D, bool VT, bool CAP, int NW, int RB>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? (RB == 2 ? 2 : 3) : 4) void window_f32_kernel(const WindowArgs a) {
   constexpr int DT = D / 16;          // O^T tiles, and 16-feature steps of S^T
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer
   __shared__ float mo[NW / 2 * 16 * MO_LD];
@@ -40,16 +40,22 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void wind
   const uint32_t rest = blockIdx.x / a.n_kv_heads;
   const int split = rest % a.n_splits;
   const uint32_t u = a.n_units / a.n_kv_heads - 1 - rest / a.n_splits;
-  const RowTile rt = find_tile<kF32Rows>(a, u);
+  constexpr int R = 16 * RB;          // pairs of the workgroup, in RB blocks
+  const RowTile rt = find_tile<R>(a, u);
   if (rt.b < 0) return;
   const int G = a.group;
   const bool direct = a.n_splits == 1;
-  const int pair = min(rt.i0 + qn, rt.n - 1);
-  const bool row_ok = rt.i0 + qn < rt.n;
-  const int tok = pair / G, qhead = kvh * G + pair - tok * G;
-  const size_t row = (size_t)(rt.row0 + tok) * a.n_q_heads + qhead;
-  const int pos = rt.past + tok;
-  const int p0 = rt.past + rt.i0 / G, p1 = rt.past + min(rt.i0 + kF32Rows - 1, rt.n - 1) / G;
+  // this lane's pair in each block
+  int pair[RB], pos[RB];
+  size_t row[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    pair[r] = min(rt.i0 + 16 * r + qn, rt.n - 1);
+    const int tok = pair[r] / G;
+    row[r] = (size_t)(rt.row0 + tok) * a.n_q_heads + kvh * G + pair[r] - tok * G;
+    pos[r] = rt.past + tok;
+  }
+  const int p0 = rt.past + rt.i0 / G, p1 = rt.past + min(rt.i0 + R - 1, rt.n - 1) / G;
   KeyList kl{};
   int e0 = 0, e1 = 0;
   if (p1 >= 0) {
@@ -57,15 +63,18 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void wind
     e0 = (int)((int64_t)kl.n * split / a.n_splits);
     e1 = (int)((int64_t)kl.n * (split + 1) / a.n_splits);
   }
-  const float *q = reinterpret_cast<const float *>(a.q) + row * D;
-  f32x4 qreg[DT];
+  f32x4 qreg[RB][DT], o[RB][DT];
+  float m[RB], lsum[RB];
 #pragma unroll
-  for (int s = 0; s < DT; ++s) qreg[s] = *reinterpret_cast<const f32x4 *>(q + 16 * s + 4 * grp);
-
-  f32x4 o[DT];
+  for (int r = 0; r < RB; ++r) {
+    const float *q = reinterpret_cast<const float *>(a.q) + row[r] * D;
 #pragma unroll
-  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, lsum = 0.f;
+    for (int s = 0; s < DT; ++s) qreg[r][s] = *reinterpret_cast<const f32x4 *>(q + 16 * s + 4 * grp);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[r] = -INFINITY;
+    lsum[r] = 0.f;
+  }
   const float *kc = reinterpret_cast<const float *>(a.kc), *vc = reinterpret_cast<const float *>(a.vc);
   const int32_t *map = a.maps + (size_t)rt.b * a.map_stride;
   const float c_scale = CAP ? 1.0f : a.scale_log2;
@@ -102,36 +111,45 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void wind
         for (int t = 0; t < DT; ++t) v[t][i] = row[16 * t];
       }
     }
-    // two chains of MFMAs, added at the end
-    f32x4 s2[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    // two chains of MFMAs a block, added at the end
+    f32x4 s2[RB][2];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) s2[r][0] = s2[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int st = 0; st < DT; ++st)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        s2[i & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[st][i], qreg[st][i], s2[i & 1], 0, 0, 0);
-    const f32x4 s = s2[0] + s2[1];
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+          s2[r][i & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[st][i], qreg[r][st][i], s2[r][i & 1], 0, 0, 0);
     // the next page's keys (past the list's end the last page's again, unused)
     page = kl.page(min(e + NW, e1 - 1));
     phys = phys_next;
     load_k(page * kPage, phys);
     phys_next = (uint32_t)map[kl.page(min(e + 2 * NW, e1 - 1))];
     // the lane's scores: keys 4 grp + i of query column qn
-    float x[4], mx = -INFINITY;
+    float p[RB][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 4 * grp + i;
-      const bool vis = key <= pos && (key > pos - a.window || key < a.sinks);
-      x[i] = vis ? (CAP ? a.cap_out * tanhf(s[i] * a.cap_in) : s[i]) : -INFINITY;
-      mx = fmaxf(mx, x[i]);
+    for (int r = 0; r < RB; ++r) {
+      const f32x4 s = s2[r][0] + s2[r][1];
+      float x[4], mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + 4 * grp + i;
+        const bool vis = key <= pos[r] && (key > pos[r] - a.window || key < a.sinks);
+        x[i] = vis ? (CAP ? a.cap_out * tanhf(s[i] * a.cap_in) : s[i]) : -INFINITY;
+        mx = fmaxf(mx, x[i]);
+      }
+      mx = max_x32(max_x16(mx)) * c_scale;
+      const float nm = fmaxf(m[r], mx), ref = nm == -INFINITY ? 0.f : nm;
+      const float alpha = nm == -INFINITY ? 1.f : fast_exp2(m[r] - nm);
+      m[r] = nm;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[r][i] = fast_exp2(fmaf(x[i], c_scale, -ref));
+      lsum[r] = fmaf(lsum[r], alpha, (p[r][0] + p[r][1]) + (p[r][2] + p[r][3]));
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[r][t] *= alpha;
     }
-    mx = max_x32(max_x16(mx)) * c_scale;
-    const float nm = fmaxf(m, mx), ref = nm == -INFINITY ? 0.f : nm;
-    const float alpha = nm == -INFINITY ? 1.f : fast_exp2(m - nm);
-    m = nm;
-    float p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(x[i], c_scale, -ref));
-    lsum = fmaf(lsum, alpha, (p[0] + p[1]) + (p[2] + p[3]));
     if constexpr (VT) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -141,89 +159,97 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? 3 : 4) void wind
       }
     }
 #pragma unroll
-    for (int t = 0; t < DT; ++t) o[t] *= alpha;
-#pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], p[i], o[t], 0, 0, 0);
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+          o[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], p[r][i], o[r][t], 0, 0, 0);
   }
 
-  // ---- merge the waves, pairwise
-  lsum = sum_x32(sum_x16(lsum));
-  auto store_state = [&](int s) {
+  // ---- merge the waves, pairwise, a block at a time; wave 0 writes it
+  auto finish = [&](f32x4 (&o)[DT], float m, float lsum, int pair, int pos, size_t row, bool row_ok, bool first) {
+    lsum = sum_x32(sum_x16(lsum));
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<f32x4 *>(mo + (s * 16 + qn) * MO_LD + 16 * t + 4 * grp) = o[t];
-    if (grp == 0) {
-      mml[2 * (s * 16 + qn)] = m;
-      mml[2 * (s * 16 + qn) + 1] = lsum;
+    for (int half = NW / 2; half > 0; half /= 2) {
+      if (!first || half < NW / 2) __syncthreads();       // the slots of the step before have been read
+      if (wave >= half && wave < 2 * half) {
+        const int s = wave - half;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+          *reinterpret_cast<f32x4 *>(mo + (s * 16 + qn) * MO_LD + 16 * t + 4 * grp) = o[t];
+        if (grp == 0) {
+          mml[2 * (s * 16 + qn)] = m;
+          mml[2 * (s * 16 + qn) + 1] = lsum;
+        }
+      }
+      __syncthreads();
+      if (wave < half) {
+        const int s = wave;
+        const float mb = mml[2 * (s * 16 + qn)], lb = mml[2 * (s * 16 + qn) + 1];
+        const float M = fmaxf(m, mb);
+        const float wa = m > -INFINITY ? fast_exp2(m - M) : m == M ? 1.f : 0.f;
+        const float wb = mb > -INFINITY ? fast_exp2(mb - M) : mb == M ? 1.f : 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+          o[t] = o[t] * wa + *reinterpret_cast<const f32x4 *>(mo + (s * 16 + qn) * MO_LD + 16 * t + 4 * grp) * wb;
+        lsum = lsum * wa + lb * wb;
+        m = M;
+      }
     }
-  };
-  auto merge_state = [&](int s) {
-    const float mb = mml[2 * (s * 16 + qn)], lb = mml[2 * (s * 16 + qn) + 1];
-    const float M = fmaxf(m, mb);
-    const float wa = m > -INFINITY ? fast_exp2(m - M) : m == M ? 1.f : 0.f;
-    const float wb = mb > -INFINITY ? fast_exp2(mb - M) : mb == M ? 1.f : 0.f;
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-      o[t] = o[t] * wa + *reinterpret_cast<const f32x4 *>(mo + (s * 16 + qn) * MO_LD + 16 * t + 4 * grp) * wb;
-    lsum = lsum * wa + lb * wb;
-    m = M;
-  };
-#pragma unroll
-  for (int half = NW / 2; half > 0; half /= 2) {
-    if (half < NW / 2) __syncthreads();       // the slots of the step before have been read
-    if (wave >= half && wave < 2 * half) store_state(wave - half);
-    __syncthreads();
-    if (wave < half) merge_state(wave);
-  }
-  if (wave != 0) return;
+    if (wave != 0) return;
 
-  const bool empty = pos < 0 || e0 == e1;
-  const float inv = direct ? (empty ? 0.f : 1.0f / lsum) : lsum > 0.f ? 1.0f / lsum : 0.f;
-  float check = 0.f;
+    const bool empty = pos < 0 || e0 == e1;
+    const float inv = direct ? (empty ? 0.f : 1.0f / lsum) : lsum > 0.f ? 1.0f / lsum : 0.f;
+    float check = 0.f;
 #pragma unroll
-  for (int t = 0; t < DT; ++t)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      o[t][i] = empty ? 0.f : o[t][i] * inv;       // (0 x NaN is NaN)
-      check = fmaf(o[t][i], 0.f, check);
+      for (int i = 0; i < 4; ++i) {
+        o[t][i] = empty ? 0.f : o[t][i] * inv;       // (0 x NaN is NaN)
+        check = fmaf(o[t][i], 0.f, check);
+      }
+    check = sum_x32(sum_x16(check));
+    const bool bad = row_ok && !empty && (!(check == 0.f) || lsum != lsum);
+    const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
+    if (row_ok && !bad) {
+      float *to = direct ? reinterpret_cast<float *>(a.out) + row * D : reinterpret_cast<float *>(a.part) + slot * D;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(to + 16 * t + 4 * grp) = o[t];
+      const float lw = empty ? 0.f : lsum;
+      if (!direct && grp == 0) a.part_ml[slot] = f32x4{part_max(m, pos >= 0, split), lw, lw, 0.f};
     }
-  check = sum_x32(sum_x16(check));
-  const bool bad = row_ok && !empty && (!(check == 0.f) || lsum != lsum);
-  const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
-  if (row_ok && !bad) {
-    float *to = direct ? reinterpret_cast<float *>(a.out) + row * D : reinterpret_cast<float *>(a.part) + slot * D;
-#pragma unroll
-    for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(to + 16 * t + 4 * grp) = o[t];
-    const float lw = empty ? 0.f : lsum;
-    if (!direct && grp == 0) a.part_ml[slot] = f32x4{part_max(m, pos >= 0, split), lw, lw, 0.f};
-  }
-  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && grp == 0);
-  while (left) {
-    const int r = __builtin_ctz(left);
-    left &= left - 1;
-    const int rp = __builtin_amdgcn_readlane(pair, r), rtok = rp / G, rhead = kvh * G + rp - rtok * G;
-    const size_t rrow = (size_t)(rt.row0 + rtok) * a.n_q_heads + rhead;
-    float res[(D + 63) / 64], ma, la;
-    row_again<float, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const float *>(a.q) + rrow * D, rt.past + rtok,
-                                 e1 - e0, [&](int i) { return e0 + i; }, res, ma, la);
-    store_again<float, D, false>(a, rrow, split, direct, res, ma, la);
-  }
+    uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && grp == 0);
+    while (left) {
+      const int j = __builtin_ctz(left);
+      left &= left - 1;
+      const int rp = __builtin_amdgcn_readlane(pair, j), rtok = rp / G, rhead = kvh * G + rp - rtok * G;
+      const size_t rrow = (size_t)(rt.row0 + rtok) * a.n_q_heads + rhead;
+      float res[(D + 63) / 64], ma, la;
+      row_again<float, D, VT, CAP>(a, kl, rt.b, kvh, reinterpret_cast<const float *>(a.q) + rrow * D, rt.past + rtok,
+                                   e1 - e0, [&](int i) { return e0 + i; }, res, ma, la);
+      store_again<float, D, false>(a, rrow, split, direct, res, ma, la);
+    }
+  };
+  finish(o[0], m[0], lsum[0], pair[0], pos[0], row[0], rt.i0 + qn < rt.n, true);
+  if constexpr (RB == 2) finish(o[1], m[1], lsum[1], pair[1], pos[1], row[1], rt.i0 + 16 + qn < rt.n, false);
 }
 
-hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, hipStream_t stream) {
+hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks, hipStream_t stream) {
   const dim3 grid(a.n_units * a.n_splits);
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a);
     return hipGetLastError();
   };
   auto with_w = [&](auto d, auto v, auto c) {
-    if (waves == 2) return run(window_f32_kernel<d(), v(), c(), 2>);
-    if constexpr (d() < 256) {
-      if (waves == 8) return run(window_f32_kernel<d(), v(), c(), 8>);
+    if constexpr (d() == 128) {
+      if (blocks == 2) return run(window_f32_kernel<d(), v(), c(), 4, 2>);
     }
-    return run(window_f32_kernel<d(), v(), c(), 4>);
+    if (waves == 2) return run(window_f32_kernel<d(), v(), c(), 2, 1>);
+    if constexpr (d() < 256) {
+      if (waves == 8) return run(window_f32_kernel<d(), v(), c(), 8, 1>);
+    }
+    return run(window_f32_kernel<d(), v(), c(), 4, 1>);
   };
   auto with_v = [&](auto d, auto v) {
     return cap ? with_w(d, v, std::true_type{}) : with_w(d, v, std::false_type{});
@@ -323,8 +349,20 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a,
 // Whether a launch's partials are fp16.
 bool half_parts(const WindowLaunch &p) { return p.is_bf16 && p.q_start != nullptr; }
 
+// Blocks of 16 pairs of an fp32 workgroup.  Two (of 4 waves) read keys and values half as often and leave a SIMD two
+// waves; for that a launch has to have long lists and workgroups enough, sooner with a transposed V, whose pieces of 64
+// bytes cost the caches more (head_dim 128, 40 heads over 8, one block and two: 263 + 130 rows, window 2420, transposed V
+// 386, 211 us; 16 x 100 rows at 500 319, 223, row-major 235, 231; 2000 rows from 0 503, 450; but 512 rows, window 1024,
+// 140, 152; 256 rows, window 512, transposed V 50, 55; 334 rows from 0 28, 31; head_dim 64, 16 x 100 at 500 95, 99).
+int f32_blocks(const WindowLaunch &p) {
+  if (p.is_bf16 || p.q_start == nullptr || p.head_dim != 128) return 1;
+  const int64_t wgs = ((int64_t)p.n_rows * (p.n_q_heads / p.n_kv_heads) / (2 * kF32Rows) + p.n_seqs) * p.n_kv_heads;
+  const int64_t keys = std::min<int64_t>((int64_t)p.window + p.sinks, p.max_len);
+  return keys > 512 && wgs > (p.v_transposed ? 384 : 1024) ? 2 : 1;
+}
+
 int64_t tile_rows(const WindowLaunch &p) {
-  return !p.is_bf16 ? kF32Rows : p.head_dim == 256 ? kWideRows : kMfmaRows;
+  return !p.is_bf16 ? kF32Rows * f32_blocks(p) : p.head_dim == 256 ? kWideRows : kMfmaRows;
 }
 
 // (row tile, KV head) pairs of a launch; sequences of a decode step take theirs by query group in bf16.
@@ -363,7 +401,7 @@ int64_t list_pages(const WindowLaunch &p) {
 int f32_waves(const WindowLaunch &p) {
   const int64_t wgs = window_units(p) * p.n_splits;
   if (wgs > 4 * 256 && list_pages(p) <= 16) return 2;
-  return wgs > 2 * 256 || p.head_dim == 256 ? 4 : 8;
+  return wgs > 2 * 256 || p.head_dim == 256 || f32_blocks(p) == 2 ? 4 : 8;
 }
 
 // Splits of the keys of every row tile.
@@ -463,7 +501,7 @@ hipError_t launch_window(const WindowLaunch &p, hipStream_t stream) {
   a.cap_k = p.softcap > 0.f ? 2.0f * p.scale * log2e / p.softcap : 0.f;
   const bool cap = p.softcap > 0.f;
   hipError_t e;
-  if (!p.is_bf16) e = launch_window_f32(a, p.head_dim, p.v_transposed, cap, f32_waves(p), stream);
+  if (!p.is_bf16) e = launch_window_f32(a, p.head_dim, p.v_transposed, cap, f32_waves(p), f32_blocks(p), stream);
   else if (p.q_start == nullptr) e = launch_window_decode(a, p.head_dim, p.v_transposed, cap, stream);
   else if (p.head_dim == 256) e = launch_window_d256(a, p.v_transposed, cap, stream);
   else e = launch_window_rows(a, p.head_dim, p.v_transposed, cap, stream);

@@ -81,6 +81,30 @@ def test_many_fp32_workgroups(dim, vt, cap):
         seed=32)
 
 
+@pytest.mark.parametrize("vt,cap", [(False, 0.0), (True, 0.0), (True, 20.0), (False, 20.0)])
+def test_long_lists_of_many_fp32_workgroups(vt, cap):
+    """Two blocks of pairs a workgroup: blocks that are full, begun, empty; windows whose edge lies in one block."""
+    batch = [(500, 45)] + [(3 * b % 40, 1 + 7 * b % 48) for b in range(63)] + [(0, 540)]
+    run(batch, 1000, 0, hq=8, hkv=8, dim=128, dtype=F, vt=vt, cap=cap, seed=35, pad=3)
+    run(batch, 510, 5, hq=16, hkv=8, dim=128, dtype=F, vt=vt, cap=cap, seed=36)
+
+
+def test_long_lists_with_values_that_are_not_finite():
+    """... in keys and values that the second block sees and the first does not."""
+    lens, q_start = [560] + [30] * 60, [0, 700] + [700 + 10 * b for b in range(1, 61)]
+    pg = Paged(lens, 8, 128, F, True, seed=37)
+    pg.v[pg.maps[0, 20], 3, 5, 17] = float("inf")
+    pg.k[pg.maps[7, 1], 2, 8, 4] = float("nan")
+    q = torch.randn((q_start[-1], 8, 128), generator=torch.Generator().manual_seed(38)).to(F)
+    cache, maps = pg.device()
+    got = N.window_attn(q.cuda(), cache, maps, i32(q_start), i32(lens), 560, 1000, 0, 0)
+    ref, parts = pg.exact(q, q_start, 1000, 0)
+    assert np.isinf(ref).any() and np.isnan(ref).any()
+    with np.errstate(all="ignore"):
+        bound = window_bound(ref, parts, F)
+    within(f64(got), ref, bound, "not finite")
+
+
 def test_many_fp32_workgroups_with_values_that_are_not_finite():
     lens = [40 + b for b in range(60)]
     q_start = [20 * b for b in range(61)]
