@@ -27,7 +27,7 @@ constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in ea
 }  // namespace
 
 template <int D, bool VT, bool CAP, int NW, int RB>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? (RB == 2 ? 2 : 3) : 4) void window_f32_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : D == 128 ? (RB == 2 ? 2 : 3) : 4) void window_f32_kernel(const WindowArgs a) {
   constexpr int DT = D / 16;          // O^T tiles, and 16-feature steps of S^T
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer
   __shared__ float mo[NW / 2 * 16 * MO_LD];
@@ -80,55 +80,93 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? (RB == 2 ? 2 : 3
   const float c_scale = CAP ? 1.0f : a.scale_log2;
   auto from = [&](int k) { return kl.stand_in(k) & (kPage - 1); };
   auto page_base = [&](uint32_t phys) { return ((size_t)phys * a.n_kv_heads + kvh) * kPage * D; };
+  // A page's keys and values come in NH parts of the features.  In one: a page's values are loading while its scores are
+  // formed, the next page's keys from there on.  In two (head_dim 256): both take the same registers in turn, a part's
+  // values as soon as its keys have been used, the next page's keys as soon as the values have, so that a SIMD has two
+  // waves (four sequences of 700 to 1557 rows from 0, transposed V, capped: 708 -> 594 us; 20 x 100 rows at 100 122 -> 90).
+  constexpr int NH = D == 256 ? 2 : 1, HT = DT / NH;
   // lane qn feeds key row qn, features 16 s + 4 grp + i as the k index grp of step (s, i); Q alike
-  f32x4 k[DT];
-  auto load_k = [&](int key0, uint32_t phys) {
-    const float *kr = kc + page_base(phys) + from(key0 + qn) * D + 4 * grp;
+  auto load_k = [&](f32x4 (&to)[HT], int h, int key0, uint32_t phys) {
+    const float *kr = kc + page_base(phys) + from(key0 + qn) * D + 4 * grp + 16 * HT * h;
 #pragma unroll
-    for (int st = 0; st < DT; ++st) k[st] = *reinterpret_cast<const f32x4 *>(kr + 16 * st);
+    for (int st = 0; st < HT; ++st) to[st] = *reinterpret_cast<const f32x4 *>(kr + 16 * st);
   };
+  auto load_v = [&](f32x4 (&to)[HT], int h, int key0, uint32_t phys) {
+    if constexpr (VT) {
+      const float *vr = vc + ((size_t)kvh * D + 16 * HT * h + qn) * a.n_cols + (size_t)phys * kPage + 4 * grp;
+#pragma unroll
+      for (int t = 0; t < HT; ++t) to[t] = *reinterpret_cast<const f32x4 *>(vr + (size_t)(16 * t) * a.n_cols);
+    } else {
+      const float *vr = vc + page_base(phys) + qn + 16 * HT * h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float *row = vr + from(key0 + 4 * grp + i) * D;       // (once a key, not once a feature block)
+#pragma unroll
+        for (int t = 0; t < HT; ++t) to[t][i] = row[16 * t];
+      }
+    }
+  };
+  f32x4 s2[RB][2];                    // two chains of MFMAs a block, added at the end
+  auto scores = [&](const f32x4 (&k)[HT], int h) {
+#pragma unroll
+    for (int st = 0; st < HT; ++st)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+          s2[r][i & 1] =
+              __builtin_amdgcn_mfma_f32_16x16x4f32(k[st][i], qreg[r][HT * h + st][i], s2[r][i & 1], 0, 0, 0);
+  };
+  float p[RB][4];
+  auto outputs = [&](f32x4 (&v)[HT], int h, int key0) {
+    if constexpr (VT) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = kl.seen(key0 + 4 * grp + i);    // other slots may hold anything
+#pragma unroll
+        for (int t = 0; t < HT; ++t) v[t][i] = in ? v[t][i] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+          o[r][HT * h + t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], p[r][i], o[r][HT * h + t], 0, 0, 0);
+  };
+  f32x4 k[NH][HT], v[HT];
   int e = e0 + wave, page = 0;
   uint32_t phys = 0, phys_next = 0;
   if (e < e1) {
     page = kl.page(e);
     phys = (uint32_t)map[page];
     phys_next = (uint32_t)map[kl.page(min(e + NW, e1 - 1))];
-    load_k(page * kPage, phys);
+#pragma unroll
+    for (int h = 0; h < NH; ++h) load_k(k[h], h, page * kPage, phys);
   }
   for (; e < e1; e += NW) {
     const int key0 = page * kPage;
-    f32x4 v[DT];
-    if constexpr (VT) {
-      const float *vr = vc + ((size_t)kvh * D + qn) * a.n_cols + (size_t)phys * kPage + 4 * grp;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) v[t] = *reinterpret_cast<const f32x4 *>(vr + (size_t)(16 * t) * a.n_cols);
-    } else {
-      const float *vr = vc + page_base(phys) + qn;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float *row = vr + from(key0 + 4 * grp + i) * D;       // (once a key, not once a feature block)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) v[t][i] = row[16 * t];
-      }
-    }
-    // two chains of MFMAs a block, added at the end
-    f32x4 s2[RB][2];
 #pragma unroll
     for (int r = 0; r < RB; ++r) s2[r][0] = s2[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (NH == 1) {
+      load_v(v, 0, key0, phys);
+      scores(k[0], 0);
+    } else {
 #pragma unroll
-    for (int st = 0; st < DT; ++st)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < RB; ++r)
-          s2[r][i & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[st][i], qreg[r][st][i], s2[r][i & 1], 0, 0, 0);
-    // the next page's keys (past the list's end the last page's again, unused)
+      for (int h = 0; h < NH; ++h) {
+        scores(k[h], h);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(k[h], h, key0, phys);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // the next page (past the list's end the last one again, unused)
     page = kl.page(min(e + NW, e1 - 1));
     phys = phys_next;
-    load_k(page * kPage, phys);
+    if constexpr (NH == 1) load_k(k[0], 0, page * kPage, phys);
     phys_next = (uint32_t)map[kl.page(min(e + 2 * NW, e1 - 1))];
     // the lane's scores: keys 4 grp + i of query column qn
-    float p[RB][4];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       const f32x4 s = s2[r][0] + s2[r][1];
@@ -150,21 +188,17 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : D == 128 ? (RB == 2 ? 2 : 3
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[r][t] *= alpha;
     }
-    if constexpr (VT) {
+    if constexpr (NH == 1) {
+      outputs(v, 0, key0);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool in = kl.seen(key0 + 4 * grp + i);    // other slots may hold anything
-#pragma unroll
-        for (int t = 0; t < DT; ++t) v[t][i] = in ? v[t][i] : 0.f;
+      for (int h = 0; h < NH; ++h) {
+        outputs(k[h], h, key0);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(k[h], h, page * kPage, phys);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int r = 0; r < RB; ++r)
-          o[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], p[r][i], o[r][t], 0, 0, 0);
   }
 
   // ---- merge the waves, pairwise, a block at a time; wave 0 writes it
@@ -393,11 +427,11 @@ int64_t list_pages(const WindowLaunch &p) {
   return (std::min<int64_t>((int64_t)p.window + p.sinks + rows + 16, p.max_len) + 15) / 16;
 }
 
-// Waves of an fp32 workgroup.  Eight (head_dim 256, whose registers leave a SIMD one wave: four) where the chip has room
-// for every workgroup at once and a list's length is what a launch takes; with more workgroups fewer merge less, and of
-// short lists two (8, 4, 2 waves; 40 heads over 8 of 128 and 32 of 64: 60 rows at 1000 30, 50, 61 us; 334 at 0 31, 27, 31;
-// 1024 at 0, head_dim 64, 62, 57, 71; 43 sequences of 62 rows at 10 101, 72, 60, at 100 232, 165, 115; 2000 rows, window 64,
-// 96, 71, 60; 64 x 16 at 200 101, 79, 82; head_dim 256, 10 x 200 at 0 -, 138, 91, 400 at 500 -, 95, 106).
+// Waves of an fp32 workgroup.  Eight where the chip has room for every workgroup at once and a list's length is what a
+// launch takes; with more workgroups fewer merge less, and of short lists two (8, 4, 2 waves; 40 heads over 8 of 128 and
+// 32 of 64: 60 rows at 1000 30, 50, 61 us; 334 at 0 31, 27, 31; 1024 at 0, head_dim 64, 62, 57, 71; 43 sequences of 62
+// rows at 10 101, 72, 60, at 100 232, 165, 115; 2000 rows, window 64, 96, 71, 60; 64 x 16 at 200 101, 79, 82).  head_dim
+// 256 has four for eight (200 rows at 1000 70, 62, 108; 20 x 100 at 100 -, 102, 90; 480 at 0 50, 52, 64).
 int f32_waves(const WindowLaunch &p) {
   const int64_t wgs = window_units(p) * p.n_splits;
   if (wgs > 4 * 256 && list_pages(p) <= 16) return 2;
