@@ -185,7 +185,8 @@ __device__ __forceinline__ float part_max(float m, bool any, int split) {
 // One row taken again, key by key, from the list's entries entry(0) .. entry(n - 1): the way of rows whose result is not
 // finite.  In a tile of several tokens a key that one row sees is hidden from another, and the matrix product of its
 // probability 0 with a value that is infinite or NaN is NaN; so the tile's product may be used where it is finite, and
-// where it is not the row is formed from the keys that it sees alone.  It costs about 1 us for 64 keys, which only such rows pay.
+// where it is not the row is formed from the keys that it sees alone.  It costs about 1 us for 64 keys, which only such rows
+// pay.
 // Called by a whole wave; `res` gives lane l features l, l + 64, ... of O / l, then m and l.
 template <typename T, int D, bool VT, bool CAP, typename Entry>
 __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl, int b, int h, const T *q, int pos,
@@ -360,6 +361,7 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
 hipError_t launch_window_rows(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_d256(const WindowArgs &a, bool vt, bool cap, hipStream_t stream);
 hipError_t launch_window_decode(const WindowArgs &a, int head_dim, bool vt, bool cap, hipStream_t stream);
-hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks, hipStream_t stream);
+hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks,
+                             hipStream_t stream);
 
 }  // namespace nexus

@@ -1,12 +1,12 @@
 // Windowed attention over fp32 caches (many rows or one a sequence), the merge of split results and the launch of all
 // windowed attention.
 //
-// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head; its waves (f32_waves) take the
-// pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from global memory (a page's
-// values and the next one's keys are loading while a page's scores are formed), and merge their (m, l, O) through LDS.
-// Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of 256: 8.3 us, a chain of
-// round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a CU of which four run
-// together.
+// fp32: a workgroup is 16 (token, head of the group) pairs of one sequence and KV head, or 32 (f32_blocks); its waves
+// (f32_waves) take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from
+// global memory (a page's values and the next one's keys are loading while a page's scores are formed), and merge their
+// (m, l, O) through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of
+// 256: 8.3 us, a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a
+// CU of which four run together.
 #include "decode_common.h"
 #include "window_common.h"
 
@@ -27,7 +27,8 @@ constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in ea
 }  // namespace
 
 template <int D, bool VT, bool CAP, int NW, int RB>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : D == 128 ? (RB == 2 ? 2 : 3) : 4) void window_f32_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(64 * NW, D == 256 || RB == 2 ? 2 : D == 128 ? 3 : 4) void window_f32_kernel(
+    const WindowArgs a) {
   constexpr int DT = D / 16;          // O^T tiles, and 16-feature steps of S^T
   constexpr int MO_LD = D + 4;        // padded row of the merge buffer
   __shared__ float mo[NW / 2 * 16 * MO_LD];
@@ -83,7 +84,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : D == 128 ? (RB == 2 ? 2 : 3
   // A page's keys and values come in NH parts of the features.  In one: a page's values are loading while its scores are
   // formed, the next page's keys from there on.  In two (head_dim 256): both take the same registers in turn, a part's
   // values as soon as its keys have been used, the next page's keys as soon as the values have, so that a SIMD has two
-  // waves (four sequences of 700 to 1557 rows from 0, transposed V, capped: 708 -> 594 us; 20 x 100 rows at 100 122 -> 90).
+  // waves (four sequences of 700 to 1557 rows from 0, transposed V, capped: 708 -> 594 us; 20 x 100 rows at 100 122 ->
+  // 90).
   constexpr int NH = D == 256 ? 2 : 1, HT = DT / NH;
   // lane qn feeds key row qn, features 16 s + 4 grp + i as the k index grp of step (s, i); Q alike
   auto load_k = [&](f32x4 (&to)[HT], int h, int key0, uint32_t phys) {
@@ -269,7 +271,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : D == 128 ? (RB == 2 ? 2 : 3
   if constexpr (RB == 2) finish(o[1], m[1], lsum[1], pair[1], pos[1], row[1], rt.i0 + 16 + qn < rt.n, false);
 }
 
-hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks, hipStream_t stream) {
+hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool cap, int waves, int blocks,
+                             hipStream_t stream) {
   const dim3 grid(a.n_units * a.n_splits);
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a);
