@@ -38,13 +38,6 @@ __global__ __launch_bounds__(kThreads) void batch_pages_kernel(const BatchPagesL
   if (tid == 0) granted = 0;
 
   const int64_t capacity = (int64_t)p.map_stride * kPage;
-  auto held_of = [](int64_t c) { return (int)((c + kPage - 1) >> kPageShift); };
-  // rows and pages that a sequence asks for; pages -1: its lengths are not valid
-  auto ask = [&](int c, int f, int &rows, int &pages) {
-    rows = min(max(f, 0), p.max_tokens);
-    const int64_t n = (int64_t)c + f;
-    pages = c < 0 || f < 0 || n > capacity ? -1 : held_of(n) - held_of(c);
-  };
   // a thread sums a run of neighbouring sequences (one, in batches of up to 1024), the workgroup the runs.  Sequences
   // whose rows pass max_tokens may count in the sum of pages: all that come after them are refused or need none.
   const int run = (p.n_seqs + kThreads - 1) / kThreads;
@@ -54,10 +47,9 @@ __global__ __launch_bounds__(kThreads) void batch_pages_kernel(const BatchPagesL
   for (int b = b0; b < b1; ++b) {
     c0 = p.cached[b];
     f0 = p.fresh[b];
-    int r, g;
-    ask(c0, f0, r, g);
-    rows += r;
-    pages += max(g, 0);
+    const BatchAsk a = batch_ask(c0, f0, capacity);
+    rows += a.rows;
+    pages += max(a.pages, 0);
   }
   int64_t r0 = rows, g0 = pages;
   for (int off = 1; off < 64; off <<= 1) {
@@ -84,15 +76,14 @@ __global__ __launch_bounds__(kThreads) void batch_pages_kernel(const BatchPagesL
       c0 = p.cached[b];
       f0 = p.fresh[b];
     }
-    int r, g;
-    ask(c0, f0, r, g);
-    const bool ok = g >= 0 && (r == 0 || r0 + r <= p.max_tokens) && (g == 0 || g0 + g <= n_free);
-    if (ok && g > 0) most = (int)(g0 + g);
+    const BatchAsk a = batch_ask(c0, f0, capacity);
+    const bool ok = batch_grants(a, r0, g0, p.max_tokens, n_free);
+    if (ok && a.pages > 0) most = (int)(g0 + a.pages);
     // (of a sequence without rows neither is looked up)
     shift[b] = ok ? (int32_t)(c0 - min(r0, (int64_t)p.max_tokens)) : kRefused;
-    ahead[b] = ok && g > 0 ? (int32_t)(g0 - held_of(c0)) : 0;
-    r0 += r;
-    g0 += max(g, 0);
+    ahead[b] = ok && a.pages > 0 ? (int32_t)(g0 - batch_pages_of(c0)) : 0;
+    r0 += a.rows;
+    g0 += max(a.pages, 0);
     upto[b] = (int32_t)min(r0, (int64_t)p.max_tokens);
     if (blockIdx.x == 0) {
       p.seq_len[b] = ok ? c0 + f0 : 0;
@@ -122,7 +113,7 @@ __global__ __launch_bounds__(kThreads) void batch_pages_kernel(const BatchPagesL
       const int page = pos >> kPageShift;
       int32_t *entry = p.maps + (size_t)lo * p.map_stride + page;
       int32_t phys;
-      if (page < held_of(c)) {
+      if (page < batch_pages_of(c)) {
         phys = *entry;
       } else {
         phys = p.free_pages[n_free - 1 - (ahead[lo] + page)];

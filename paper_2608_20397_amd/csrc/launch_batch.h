@@ -10,6 +10,27 @@ namespace nexus {
 
 constexpr int kMaxBatchSeqs = 8192;    // sequences of a batch_pages launch (12 bytes of LDS each)
 
+// What a sequence of a layout asks for, and whether it gets it behind the rows and pages that the ones before it asked
+// for.  Rows are counted as they are asked for, not cut to the launch's: a sequence that alone is longer than the
+// launch is refused too.
+struct BatchAsk {
+  int64_t rows;           // its fresh tokens, a negative count as none
+  int32_t pages;          // new ones, or -1: its lengths are not valid
+};
+__host__ __device__ inline int32_t batch_pages_of(int64_t tokens) { return (int32_t)((tokens + 15) >> 4); }
+__host__ __device__ inline BatchAsk batch_ask(int32_t cached, int32_t fresh, int64_t capacity) {
+  BatchAsk a;
+  const int64_t n = (int64_t)cached + fresh;
+  a.rows = fresh > 0 ? fresh : 0;
+  a.pages = cached < 0 || fresh < 0 || n > capacity ? -1 : batch_pages_of(n) - batch_pages_of(cached);
+  return a;
+}
+__host__ __device__ inline bool batch_grants(const BatchAsk &a, int64_t rows_before, int64_t pages_before,
+                                             int32_t max_tokens, int32_t n_free) {
+  return a.pages >= 0 && (a.rows == 0 || rows_before + a.rows <= max_tokens) &&
+         (a.pages == 0 || pages_before + a.pages <= n_free);
+}
+
 struct BatchPagesLaunch {
   const int32_t *cached, *fresh;      // [n_seqs]
   const int32_t *free_pages, *n_free; // [free_capacity], [1]

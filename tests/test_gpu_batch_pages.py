@@ -85,3 +85,15 @@ def test_refusals():
         with pytest.raises(N.NexusError) as e:
             call()
         assert e.value.status == N.EINVAL
+
+
+@pytest.mark.parametrize("cached,fresh,n_free,max_tokens,stride", [
+    ([0], [40], 9, 32, 4), ([0], [33], 9, 32, 4), ([0], [100], 9, 50, 8), ([7], [26], 9, 25, 4),
+    ([0, 0], [0, 40], 9, 32, 4), ([3, 0, 0], [-2, 40, 1], 9, 32, 4), ([-1, 0], [0, 33], 9, 32, 4),
+    ([0, 5], [100, 1], 9, 50, 8), ([0, 5, 16], [100, 0, 0], 9, 50, 8), ([0, 5], [50, 1], 9, 50, 8),
+    ([0, 0, 0], [0, 51, 3], 9, 50, 8), ([100], [51], 0, 50, 16),
+])
+def test_a_sequence_longer_than_the_launch(cached, fresh, n_free, max_tokens, stride):
+    """More rows than the whole launch has, with none before them: refused, its map and the free list left as they are,
+    and all that comes after it and has rows."""
+    run(cached, fresh, n_free, max_tokens, stride)

@@ -253,3 +253,21 @@ def test_append_beside_rope_append():
         assert torch.equal(made[0].v, made[1].v)
         a, b = made[0].k.double(), made[1].k.double()
         assert ((a - b).abs() <= (0 if dtype == F else 2.0 ** -7) * b.abs()).all()
+
+
+@pytest.mark.parametrize("fresh", [[70, 1, 0, 2], [0, 65, 1, 0]])
+def test_a_round_whose_first_sequence_is_longer_than_the_launch(fresh):
+    """Its rows and those behind it are refused: nothing is appended, attention writes zeros and reads no page, and the
+    next round goes on from the state before."""
+    s = Server(4, 4, 2, 64, B, False, seed=5)
+    s.maps.fill_(-1)
+    s.stage(fresh)
+    s.launch()
+    torch.cuda.synchronize()
+    assert s.rows.seq_len.tolist() == [0] * 4 and s.rows.n_left.item() == s.n_free.item()
+    assert (s.rows.pos == -1).all() and (s.rows.slot == -1).all() and (s.maps == -1).all()
+    assert (s.out == 0).all() and torch.isnan(s.cache.k).all()
+    s.stage([20, 1, 0, 3])
+    s.launch()
+    torch.cuda.synchronize()
+    s.check([20, 1, 0, 3], "the round after")
