@@ -23,7 +23,7 @@ struct WindowArgs {
   const int32_t *lens;    // [n_seqs]
   // partial results of a split, [n_splits][n_rows * Hq]: O / l, fp32 or, of window_rows and window_d256, fp16 scaled by
   // 2^-e so that the row's largest magnitude lies in [2^14, 2^15) (11 bits, three more than P and the output have; a
-  // power of two costs no rounding and keeps any finite value in range); and (m, l, l 2^e, -), e = 0 in fp32
+  // power of two costs no rounding and keeps any finite value in range); and (m, l, e, -), e = 0 in fp32
   void *part;
   f32x4 *part_ml;
   int32_t map_stride, max_len, n_seqs, n_rows;
@@ -253,11 +253,11 @@ __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl
   l_out = (float)l;
 }
 
-// e of a row's fp16 partial, from its largest finite magnitude.
+// e of a row's fp16 partial, from its largest finite magnitude: -141 (subnormal ones) .. 113, so that 2^e itself may be
+// out of fp32's range; values take it by ldexpf.
 __device__ __forceinline__ int part_exponent(float amax) {
-  return amax > 0.f ? min(max((int)(__float_as_uint(amax) >> 23) - 127 - 14, -100), 100) : 0;
+  return amax > 0.f ? (int)(__float_as_uint(amax) >> 23) - 127 - 14 : 0;
 }
-__device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // Writes what row_again gave: to the output, or to the split's partial (HALF: in fp16).
 template <typename T, int D, bool HALF>
@@ -281,10 +281,10 @@ __device__ __forceinline__ void store_again(const WindowArgs &a, size_t row, int
     const float x = !direct && l == 0.f ? 0.f : res[i];
     if (direct && sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[row * D + d] = (uint16_t)pack_bf16x2(x, 0.f);
     else if (direct) reinterpret_cast<float *>(a.out)[row * D + d] = x;
-    else if (HALF) reinterpret_cast<uint16_t *>(a.part)[slot * D + d] = (uint16_t)pack_f16x2(x * two_to(-e), 0.f);
+    else if (HALF) reinterpret_cast<uint16_t *>(a.part)[slot * D + d] = (uint16_t)pack_f16x2(ldexpf(x, -e), 0.f);
     else reinterpret_cast<float *>(a.part)[slot * D + d] = x;
   }
-  if (!direct && lane == 0) a.part_ml[slot] = f32x4{part_max(m, true, split), l, l * two_to(e), 0.f};
+  if (!direct && lane == 0) a.part_ml[slot] = f32x4{part_max(m, true, split), l, (float)e, 0.f};
 }
 
 // The end of the 32x32 MFMA kernels, for a wave with rows: lane pair (j, j + 32) holds a pair's row, feature
@@ -331,17 +331,16 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
                     pack_bf16x2(o[db][4 * gq + 2], o[db][4 * gq + 3])};
     } else {
       const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
-      const float sc = two_to(-e);
       uint16_t *po = reinterpret_cast<uint16_t *>(a.part) + slot * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq)
           *reinterpret_cast<u32x2 *>(po + 32 * db + 8 * gq + 4 * hh) =
-              u32x2{pack_f16x2(o[db][4 * gq + 0] * sc, o[db][4 * gq + 1] * sc),
-                    pack_f16x2(o[db][4 * gq + 2] * sc, o[db][4 * gq + 3] * sc)};
+              u32x2{pack_f16x2(ldexpf(o[db][4 * gq + 0], -e), ldexpf(o[db][4 * gq + 1], -e)),
+                    pack_f16x2(ldexpf(o[db][4 * gq + 2], -e), ldexpf(o[db][4 * gq + 3], -e))};
       const float lw = empty ? 0.f : l_tot;
-      if (hh == 0) a.part_ml[slot] = f32x4{part_max(m_ref, pos >= 0, split), lw, lw * two_to(e), 0.f};
+      if (hh == 0) a.part_ml[slot] = f32x4{part_max(m_ref, pos >= 0, split), lw, (float)e, 0.f};
     }
   }
   uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && hh == 0);

@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void window_de
 #pragma unroll
       for (int t = 0; t < DT; ++t)
         *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.part) + slot * D + 16 * t + 4 * grp) = o[t];
-      if (grp == 0) a.part_ml[slot] = f32x4{part_max(m_ref, true, split), lsum, lsum, 0.f};
+      if (grp == 0) a.part_ml[slot] = f32x4{part_max(m_ref, true, split), lsum, 0.f, 0.f};
     }
   }
   // a stand-in's value that is infinite times its probability 0 is NaN

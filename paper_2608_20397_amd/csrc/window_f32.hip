@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 || RB == 2 ? 2 : D == 128 ? 3 : 4
 #pragma unroll
       for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(to + 16 * t + 4 * grp) = o[t];
       const float lw = empty ? 0.f : lsum;
-      if (!direct && grp == 0) a.part_ml[slot] = f32x4{part_max(m, pos >= 0, split), lw, lw, 0.f};
+      if (!direct && grp == 0) a.part_ml[slot] = f32x4{part_max(m, pos >= 0, split), lw, 0.f, 0.f};
     }
     uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(bad && grp == 0);
     while (left) {
@@ -303,7 +303,8 @@ hipError_t launch_window_f32(const WindowArgs &a, int head_dim, bool vt, bool ca
 
 namespace {
 
-// Merge of a row's splits: out = sum w_s O_s / sum w_s, w_s = l_s 2^(m_s - M), in a fixed order.  Rows of no sequence
+// Merge of a row's splits: out = sum w_s O_s, w_s = l_s 2^(m_s - M) / (their sum), in a fixed order.  The weights are
+// divided by their sum before a partial is multiplied, so that finite partials have a finite result.  Rows of no sequence
 // stay as they are.  A partial row lies in 2^lpr_shift lanes, 16 bytes each; 2^spr_shift neighbouring groups of them
 // share the splits of a row, and what is left of the wave takes other rows.  The first eight partials of a group are
 // loaded beside their (m, l): one round trip for rows of up to 16 splits.
@@ -339,47 +340,60 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a,
 #pragma unroll
   for (int i = 0; i < kPre; ++i)
     if (share + i * spr < S) M = fmaxf(M, ml[i][0]);
+#pragma unroll 8
   for (int s = share + kPre * spr; s < S; s += spr) M = fmaxf(M, a.part_ml[(size_t)s * n + row][0]);
   for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
-  float o[E], total = 0.f;
+  // l 2^(m - M); 0 where nothing is seen (l is NaN where scores were)
+  auto weight = [&](const f32x4 &r) { return r[1] == 0.f ? 0.f : r[1] * (M == -INFINITY ? 1.f : fast_exp2(r[0] - M)); };
+  float total = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  auto add = [&](const f32x4 &r, const u32x4 &x) {
-    if (r[1] == 0.f) return;                  // nothing seen: the partial holds nothing (l is NaN where scores were)
-    const float f = M == -INFINITY ? 1.f : fast_exp2(r[0] - M);
-    total = fmaf(r[1], f, total);
+  for (int i = 0; i < kPre; ++i) {
+    if (share + i * spr >= S) continue;
+    ml[i][3] = weight(ml[i]);
+    total += ml[i][3];
+  }
+#pragma unroll 8
+  for (int s = share + kPre * spr; s < S; s += spr) total += weight(a.part_ml[(size_t)s * n + row]);
+  for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) total += __shfl_xor(total, off);
+  if (M == -INFINITY && total == 0.f) total = 1.f;      // no key at all: zeros
+  const float inv = 1.0f / total;
+  float o[E];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+  for (int e = 0; e < E; ++e) o[e] = 0.f * inv;         // (NaN where every score is -inf: 0 / 0)
+  auto add = [&](const f32x4 &r, float w, const u32x4 &x) {
+    if (r[1] == 0.f) return;                            // nothing seen: the partial holds nothing
+    const int ex = (int)r[2];
+    w *= inv;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
       if constexpr (HALF) {
-        const f32x2 v = unpack_f16x2(x[w]);
-        o[2 * w] = fmaf(v[0], r[2] * f, o[2 * w]);
-        o[2 * w + 1] = fmaf(v[1], r[2] * f, o[2 * w + 1]);
+        const f32x2 v = unpack_f16x2(x[i]);
+        o[2 * i] = fmaf(ldexpf(v[0], ex), w, o[2 * i]);
+        o[2 * i + 1] = fmaf(ldexpf(v[1], ex), w, o[2 * i + 1]);
       } else {
-        o[w] = fmaf(__uint_as_float(x[w]), r[2] * f, o[w]);
+        o[i] = fmaf(__uint_as_float(x[i]), w, o[i]);
       }
     }
   };
 #pragma unroll
   for (int i = 0; i < kPre; ++i)
-    if (share + i * spr < S) add(ml[i], pre[i]);
-  for (int s = share + kPre * spr; s < S; s += spr) add(a.part_ml[(size_t)s * n + row], load(s));
+    if (share + i * spr < S) add(ml[i], ml[i][3], pre[i]);
+  for (int s = share + kPre * spr; s < S; s += spr) {
+    const f32x4 r = a.part_ml[(size_t)s * n + row];
+    add(r, weight(r), load(s));
+  }
   for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) {
-    total += __shfl_xor(total, off);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] += __shfl_xor(o[e], off);
   }
   if (share != 0 || !live) return;
-  if (M == -INFINITY && total == 0.f) total = 1.f;      // no key at all: zeros
-  const float inv = 1.0f / total;
   if constexpr (BF16) {
     uint16_t *out = reinterpret_cast<uint16_t *>(a.out) + (size_t)row * D + d;
 #pragma unroll
     for (int e = 0; e < E; e += 4)
-      *reinterpret_cast<u32x2 *>(out + e) =
-          u32x2{pack_bf16x2(o[e] * inv, o[e + 1] * inv), pack_bf16x2(o[e + 2] * inv, o[e + 3] * inv)};
+      *reinterpret_cast<u32x2 *>(out + e) = u32x2{pack_bf16x2(o[e], o[e + 1]), pack_bf16x2(o[e + 2], o[e + 3])};
   } else {
-    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + (size_t)row * D + d) =
-        f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + (size_t)row * D + d) = f32x4{o[0], o[1], o[2], o[3]};
   }
 }
 
