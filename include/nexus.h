@@ -487,7 +487,7 @@ nexus_status nexus_norm_rope_append(const nexus_kv_cache *cache, int32_t layer, 
  * anything.  bf16 caches: MFMA, probabilities rounded to bf16 as in nexus_suffix_attn, head_dim 64, 128 or 256.  f32
  * caches: fp32 MFMA, head_dim 16 .. 256.  Checks: the sizes and pointers above, positive n_rows and n_seqs
  * (NEXUS_EINVAL); layouts as nexus_decode_attn, 16-byte aligned caches (NEXUS_EINVAL), max_seq_len <= 2^29
- * (NEXUS_ERANGE), launches of fewer than 2^24 workgroups (NEXUS_ESHAPE).
+ * (NEXUS_ERANGE), launches of fewer than 2^24 workgroups, 2^23 of bf16 rows of head_dim 256 (NEXUS_ESHAPE).
  */
 nexus_status nexus_window_attn(const void *q, int32_t n_rows, int32_t n_q_heads, const nexus_kv_cache *cache,
                                const int32_t *maps, int32_t map_stride, const int32_t *q_start,

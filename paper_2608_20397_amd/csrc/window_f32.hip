@@ -502,7 +502,10 @@ int window_splits(const WindowLaunch &p) {
 
 bool plan_window(WindowLaunch &p) {
   p.n_splits = window_splits(p);
-  return window_units(p) * p.n_splits < (1 << 24);      // (one grid dimension holds fewer than 2^32 threads)
+  // one grid dimension holds fewer than 2^32 threads: 512 a workgroup of window_d256_kernel (and of 8 fp32 waves, which
+  // launches of up to 512 workgroups have), 256 of the others
+  const bool wide = p.is_bf16 && p.q_start != nullptr && p.head_dim == 256;
+  return window_units(p) * p.n_splits < (wide ? 1 << 23 : 1 << 24);
 }
 
 size_t window_workspace_bytes(const WindowLaunch &p) {

@@ -166,3 +166,17 @@ def test_binding_refuses_host_tensors():
         with pytest.raises(N.NexusError) as e:
             call()
         assert e.value.status == N.EINVAL
+
+
+def test_window_refuses_more_workgroups_than_a_grid_holds():
+    """A grid dimension has fewer than 2^32 threads: 2^24 workgroups of 256, 2^23 of 512 (bf16 rows of head_dim 256).
+    65000 sequences make that many with 130 to 258 KV heads."""
+    big = (1 << 64) - 1
+    for head_dim, dtype, hkv, fits in ((256, N.BF16, 129, True), (256, N.BF16, 130, False), (256, N.BF16, 200, False),
+                                       (128, N.BF16, 258, True), (128, N.BF16, 259, False), (64, N.BF16, 200, True),
+                                       (256, N.F32, 258, True), (256, N.F32, 259, False)):
+        c = _cache(head_dim=head_dim, dtype=dtype, n_kv_heads=hkv, n_phys_pages=1)
+        got = N.lib().nexus_window_attn_workspace(1, hkv, C.byref(c), 65000, 64, 16, 4)
+        assert (got == 0) if fits else (got == big), (head_dim, dtype, hkv)
+        if not fits:
+            assert rows(c=c, n_rows=1, hq=hkv, n=65000, max_len=64) == N.ESHAPE
