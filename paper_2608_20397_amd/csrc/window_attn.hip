@@ -26,7 +26,6 @@ namespace nexus {
 
 namespace {
 
-constexpr int kTileRows = 128;     // (token, head) pairs of a workgroup
 constexpr int kRing = 2048;        // entries of the page ring in LDS
 
 }  // namespace
@@ -34,6 +33,7 @@ constexpr int kRing = 2048;        // entries of the page ring in LDS
 template <int D, bool VT, bool CAP>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const WindowArgs a) {
   static_assert(D == 64 || D == 128, "head_dim");
+  static_assert(kMfmaRows == 4 * 32, "4 waves of 32 pairs");
   constexpr int KT = 64;
   constexpr int NKB = KT / 32, NDB = D / 32, NS = D / 16;
   constexpr int ROWB = D * 2;                 // bytes per K or V row
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
   const int split = a.n_splits == 1 ? 0 : rest % a.n_splits;
   // later tiles of a sequence see more keys (up to the window): the longest go first
   const uint32_t u = a.n_units / a.n_kv_heads - 1 - (a.n_splits == 1 ? rest : rest / a.n_splits);
-  const RowTile rt = find_tile<kTileRows>(a, u);
+  const RowTile rt = find_tile<kMfmaRows>(a, u);
   if (rt.b < 0) return;
   const int G = a.group;
   const bool direct = a.n_splits == 1;
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_rows_kernel(const
   const size_t row = (size_t)(rt.row0 + tok) * a.n_q_heads + qhead;
   const int pos = rt.past + tok;
   const bool row_ok = iw + j < rt.n;
-  const int p0 = rt.past + rt.i0 / G, p1 = rt.past + min(rt.i0 + kTileRows - 1, rt.n - 1) / G;
+  const int p0 = rt.past + rt.i0 / G, p1 = rt.past + min(rt.i0 + kMfmaRows - 1, rt.n - 1) / G;
   const int pa = __builtin_amdgcn_readfirstlane(rt.past + min(iw, rt.n - 1) / G);
   const int pb = __builtin_amdgcn_readfirstlane(rt.past + min(iw + 31, rt.n - 1) / G);
 

@@ -11,6 +11,9 @@
 
 namespace nexus {
 
+// (token, head) pairs of a workgroup, for the kernels and for the plan of their launches: window_rows_kernel,
+// window_d256_kernel, and a block of window_f32_kernel
+constexpr int kMfmaRows = 128, kWideRows = 256, kF32Rows = 16;
 constexpr int kNoPeriod = 1 << 28;      // no list has as many tiles: each is taken from its start
 
 struct WindowArgs {

@@ -21,7 +21,6 @@ namespace nexus {
 
 namespace {
 
-constexpr int kWideRows = 256;     // (token, head) pairs of a workgroup
 constexpr int kWideRing = 2048;    // entries of the page ring in LDS
 
 }  // namespace
@@ -29,6 +28,7 @@ constexpr int kWideRing = 2048;    // entries of the page ring in LDS
 template <bool VT, bool CAP>
 __global__ __launch_bounds__(512, 1) void window_d256_kernel(const WindowArgs a) {
   constexpr int W = 8;                        // waves
+  static_assert(kWideRows == 32 * W, "a wave takes 32 pairs");
   constexpr int D = 256, KT = 32;
   constexpr int NS = D / 16;                  // k-steps of Q K^T
   constexpr int NSR = 6;                      // k-steps whose Q operand stays in registers

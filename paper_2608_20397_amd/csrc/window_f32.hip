@@ -18,9 +18,6 @@ namespace nexus {
 
 namespace {
 
-constexpr int kF32Rows = 16;       // (token, head) pairs of an fp32 workgroup
-constexpr int kMfmaRows = 128;     // of a bf16 one (window_attn.hip)
-constexpr int kWideRows = 256;     // of one of head_dim 256 (window_d256.hip)
 constexpr int kPre = 8;            // partials of a row that a lane of the merge loads at once
 constexpr int kMaxSplits = 64;     // of a row's keys: the merge holds one in each lane
 
@@ -41,7 +38,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 || RB == 2 ? 2 : D == 128 ? 3 : 4
   const uint32_t rest = blockIdx.x / a.n_kv_heads;
   const int split = rest % a.n_splits;
   const uint32_t u = a.n_units / a.n_kv_heads - 1 - rest / a.n_splits;
-  constexpr int R = 16 * RB;          // pairs of the workgroup, in RB blocks
+  static_assert(kF32Rows == 16, "columns of the MFMA");
+  constexpr int R = kF32Rows * RB;    // pairs of the workgroup, in RB blocks
   const RowTile rt = find_tile<R>(a, u);
   if (rt.b < 0) return;
   const int G = a.group;
