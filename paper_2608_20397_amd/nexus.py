@@ -770,6 +770,11 @@ _TOP = (1 << 31) - 1                                 # of an int32 argument: no 
 _pack_cache = struct.Struct("PPiiiiiiiid").pack      # nexus_kv_cache
 
 
+def _int32(x: int) -> int:
+    """x, or the end of an int32's range that it lies behind: ctypes would bring it round to a number that is allowed."""
+    return x if -_TOP <= x <= _TOP else _TOP if x > 0 else -_TOP
+
+
 def _descriptor(cache: PagedKVCache) -> bytes:
     """The cache as the C calls take it, checked as PagedKVCache.c() does but for the devices, which the caller checks
     with its other operands (1 us of host time a call less)."""
@@ -814,6 +819,9 @@ def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, f
     dev = _current_of(maps, cached, fresh, free_pages, n_free)
     if dev < 0:
         _here(maps=maps, cached=cached, fresh=fresh, free_pages=free_pages, n_free=n_free)
+    if max_tokens > 1 << 30:
+        raise NexusError(ERANGE, "max_tokens must be at most 2^30")
+    max_tokens = _int32(max_tokens)
     if out is None:
         out = BatchRows.empty(n, max(0, max_tokens), maps.device)
     else:
@@ -868,7 +876,7 @@ def norm_rope_append(cache: PagedKVCache, layer: int, q: torch.Tensor, k: torch.
         _here(cache_k=ck, cache_v=cv, q=q, k=k, v=v, out=out, q_weight=q_weight, k_weight=k_weight, pos=pos, slot=slot)
     if out is None:
         out = torch.empty(q.shape, dtype=dt, device=q.device)
-    st = lib().nexus_norm_rope_append(desc, layer, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, rows,
+    st = lib().nexus_norm_rope_append(desc, _int32(layer), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, rows,
                                       q.shape[1], _ptr(q_weight), _ptr(k_weight), eps, pos.data_ptr(),
                                       slot.data_ptr(), out.data_ptr(), _stream_of(dev))
     if st != OK:
@@ -927,7 +935,7 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
     """Attention of a ragged batch in a sliding window with ``n_sink`` first tokens in sight: rows q_start[b] ..
     q_start[b + 1] - 1 of q [rows][n_q_heads][D] are the last ones of sequence b, of seq_len[b] tokens behind row b of
     ``maps`` (device int32 tensors).  Rows of no sequence are left as they are in out (without ``out``: undefined)."""
-    window, n_sink = window if window < _TOP else _TOP, n_sink if n_sink < _TOP else _TOP
+    window, n_sink, max_seq_len, layer = _int32(window), _int32(n_sink), _int32(max_seq_len), _int32(layer)
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, q_start, seq_len, out, workspace)
     rows, hq, _ = q.shape
@@ -941,8 +949,8 @@ def window_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor, q_star
 
 def window_attn_workspace_bytes(cache: PagedKVCache, n_rows: int, n_q_heads: int, n_seqs: int, max_seq_len: int,
                                 window: int, n_sink: int) -> int:
-    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
-    n = lib().nexus_window_attn_workspace(n_rows, n_q_heads, _descriptor(cache), n_seqs, max_seq_len, window, n_sink)
+    n = lib().nexus_window_attn_workspace(_int32(n_rows), _int32(n_q_heads), _descriptor(cache), _int32(n_seqs),
+                                          _int32(max_seq_len), _int32(window), _int32(n_sink))
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_attn_workspace")
     return n
@@ -953,7 +961,7 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
                        v_layout: int | None = None, scale: float = 0.0, out: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None):
     """decode_attn in a sliding window with ``n_sink`` first tokens in sight."""
-    window, n_sink = window if window < _TOP else _TOP, n_sink if n_sink < _TOP else _TOP
+    window, n_sink, max_seq_len, layer = _int32(window), _int32(n_sink), _int32(max_seq_len), _int32(layer)
     L = lib()
     c, out, n, stream = _window_operands(q, cache, maps, None, seq_len, out, workspace)
     hq = q.shape[1]
@@ -967,8 +975,8 @@ def window_decode_attn(q: torch.Tensor, cache: PagedKVCache, maps: torch.Tensor,
 
 def window_decode_attn_workspace_bytes(cache: PagedKVCache, n_seqs: int, n_q_heads: int, max_seq_len: int,
                                        window: int, n_sink: int) -> int:
-    window, n_sink = min(window, _TOP), min(n_sink, _TOP)
-    n = lib().nexus_window_decode_attn_workspace(n_seqs, n_q_heads, _descriptor(cache), max_seq_len, window, n_sink)
+    n = lib().nexus_window_decode_attn_workspace(_int32(n_seqs), _int32(n_q_heads), _descriptor(cache),
+                                                 _int32(max_seq_len), _int32(window), _int32(n_sink))
     if n == (1 << 64) - 1:
         raise NexusError(EINVAL, "nexus_window_decode_attn_workspace")
     return n

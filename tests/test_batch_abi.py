@@ -180,3 +180,26 @@ def test_window_refuses_more_workgroups_than_a_grid_holds():
         assert (got == 0) if fits else (got == big), (head_dim, dtype, hkv)
         if not fits:
             assert rows(c=c, n_rows=1, hq=hkv, n=65000, max_len=64) == N.ESHAPE
+
+
+@pytest.mark.parametrize("at", range(4))
+@pytest.mark.parametrize("value", [(1 << 32) + 8, 1 << 40, -(1 << 32) + 8, -(1 << 40) + 1])
+def test_workspace_sizes_past_32_bits_are_refused(at, value):
+    """... where an int32 argument would come round to sizes that are allowed; (a window has no such end)."""
+    cache = N.PagedKVCache(*(torch.zeros((1, 4, 2, 16, 128), dtype=torch.bfloat16) for _ in range(2)),
+                           torch.zeros(4, dtype=torch.int32), 1e4)
+    args = [8, 4, 2, 64]                                   # rows, query heads, sequences, longest
+    args[at] = value
+    with pytest.raises(N.NexusError) as e:
+        N.window_attn_workspace_bytes(cache, *args, 16, 4)
+    assert e.value.status == N.EINVAL
+    if at != 0:
+        with pytest.raises(N.NexusError) as e:
+            N.window_decode_attn_workspace_bytes(cache, args[2], args[1], args[3], 16, 4)
+        assert e.value.status == N.EINVAL
+    if value > 0:
+        assert N.window_attn_workspace_bytes(cache, 8, 4, 2, 64, value, value) == 0
+    else:
+        for window, sinks in ((value, 4), (16, value)):
+            with pytest.raises(N.NexusError):
+                N.window_attn_workspace_bytes(cache, 8, 4, 2, 64, window, sinks)

@@ -271,3 +271,29 @@ def test_a_round_whose_first_sequence_is_longer_than_the_launch(fresh):
     s.launch()
     torch.cuda.synchronize()
     s.check([20, 1, 0, 3], "the round after")
+
+
+def test_arguments_past_32_bits_are_refused():
+    """... and not brought round to ones that are allowed."""
+    s = Server(4, 4, 2, 64, B, False, seed=6)
+    s.stage([5, 1, 9, 0])
+    s.launch()
+    torch.cuda.synchronize()
+    s.check([5, 1, 9, 0], "a round")
+    q, k, v = s.qkv.split((4, 2, 2), 1)
+    top = s.stride * PAGE
+    pages = lambda n: N.batch_pages(s.maps, s.cached, s.fresh, s.free, s.n_free, n)  # noqa: E731
+    append = lambda layer: N.norm_rope_append(s.cache, layer, q, k, v, s.rows.pos, s.rows.slot)  # noqa: E731
+    rows = lambda n=top, layer=0, window=40: N.window_attn(s.q, s.cache, s.maps, s.rows.q_start,  # noqa: E731
+                                                           s.rows.seq_len, n, window, 3, layer)
+    step = lambda n=top, layer=0, window=40: N.window_decode_attn(s.q[:4], s.cache, s.maps, s.rows.seq_len,  # noqa: E731
+                                                                  n, window, 3, layer)
+    far = 1 << 32
+    for call, status in ((lambda: pages(far + 64), N.ERANGE), (lambda: pages(-far + 64), N.EINVAL),
+                         (lambda: append(far), N.ERANGE), (lambda: append(-far), N.ERANGE),
+                         (lambda: rows(n=far + top), N.ERANGE), (lambda: rows(layer=far), N.ERANGE),
+                         (lambda: rows(window=-far + 40), N.EINVAL), (lambda: step(n=far + top), N.ERANGE),
+                         (lambda: step(layer=-far), N.ERANGE), (lambda: step(window=-far + 40), N.EINVAL)):
+        with pytest.raises(N.NexusError) as e:
+            call()
+        assert e.value.status == status
