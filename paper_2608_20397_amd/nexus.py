@@ -829,8 +829,9 @@ def batch_pages(maps: torch.Tensor, cached: torch.Tensor, fresh: torch.Tensor, f
             _vector(name, getattr(out, name), size)
         if not _all_here(out.q_start, out.seq_len, out.pos, out.slot, out.n_left):
             _here(q_start=out.q_start, seq_len=out.seq_len, pos=out.pos, slot=out.slot, n_left=out.n_left)
-    st = lib().nexus_batch_pages(cached.data_ptr(), fresh.data_ptr(), n, free_pages.data_ptr(), n_free.data_ptr(),
-                                 free_pages.shape[0], maps.data_ptr(), maps.shape[1], max_tokens,
+    # (a list of no entries has no address, and none of it is read: any will do)
+    st = lib().nexus_batch_pages(cached.data_ptr(), fresh.data_ptr(), n, free_pages.data_ptr() or n_free.data_ptr(),
+                                 n_free.data_ptr(), free_pages.shape[0], maps.data_ptr(), maps.shape[1], max_tokens,
                                  out.q_start.data_ptr(), out.seq_len.data_ptr(), out.pos.data_ptr(),
                                  out.slot.data_ptr(), out.n_left.data_ptr(), _stream_of(dev))
     if st != OK:

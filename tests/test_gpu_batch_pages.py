@@ -97,3 +97,9 @@ def test_a_sequence_longer_than_the_launch(cached, fresh, n_free, max_tokens, st
     """More rows than the whole launch has, with none before them: refused, its map and the free list left as they are,
     and all that comes after it and has rows."""
     run(cached, fresh, n_free, max_tokens, stride)
+
+
+@pytest.mark.parametrize("n_free", [0, 5])
+def test_a_free_list_without_entries(n_free):
+    """Every page is given out: sequences that need none go on, those that do are refused."""
+    run([5, 15, 16, 3], [3, 1, 2, 1], n_free, 20, 4, capacity=0)
