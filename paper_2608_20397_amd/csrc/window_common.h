@@ -257,10 +257,11 @@ __device__ __forceinline__ void row_again(const WindowArgs &a, const KeyList &kl
 }
 
 // e of a row's fp16 partial, from its largest finite magnitude: -141 (subnormal ones) .. 113, so that 2^e itself may be
-// out of fp32's range; values take it by ldexpf.
+// out of fp32's range; values take it by ldexpf, or where they are many by a product with two_to (-126 .. 127).
 __device__ __forceinline__ int part_exponent(float amax) {
   return amax > 0.f ? (int)(__float_as_uint(amax) >> 23) - 127 - 14 : 0;
 }
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // Writes what row_again gave: to the output, or to the split's partial (HALF: in fp16).
 template <typename T, int D, bool HALF>
@@ -334,14 +335,16 @@ __device__ __forceinline__ void store_rows(const WindowArgs &a, const KeyList &k
                     pack_bf16x2(o[db][4 * gq + 2], o[db][4 * gq + 3])};
     } else {
       const size_t slot = (size_t)split * a.n_rows * a.n_q_heads + row;
+      const int e1 = min(-e, 127);
+      const float s1 = two_to(e1), s2 = two_to(-e - e1);
       uint16_t *po = reinterpret_cast<uint16_t *>(a.part) + slot * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq)
           *reinterpret_cast<u32x2 *>(po + 32 * db + 8 * gq + 4 * hh) =
-              u32x2{pack_f16x2(ldexpf(o[db][4 * gq + 0], -e), ldexpf(o[db][4 * gq + 1], -e)),
-                    pack_f16x2(ldexpf(o[db][4 * gq + 2], -e), ldexpf(o[db][4 * gq + 3], -e))};
+              u32x2{pack_f16x2(o[db][4 * gq + 0] * s1 * s2, o[db][4 * gq + 1] * s1 * s2),
+                    pack_f16x2(o[db][4 * gq + 2] * s1 * s2, o[db][4 * gq + 3] * s1 * s2)};
       const float lw = empty ? 0.f : l_tot;
       if (hh == 0) a.part_ml[slot] = f32x4{part_max(m_ref, pos >= 0, split), lw, (float)e, 0.f};
     }

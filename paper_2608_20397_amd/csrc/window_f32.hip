@@ -312,6 +312,7 @@ namespace {
 template <bool BF16, bool HALF>
 __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a, int D, int lpr_shift, int spr_shift) {
   constexpr int E = HALF ? 8 : 4;
+  constexpr int kRest = HALF ? 1 : 8;      // records of further splits at a time (rows in fp16 have 16 splits at most)
   const int lane = threadIdx.x & 63;
   const uint32_t n = (uint32_t)a.n_rows * a.n_q_heads;
   const uint32_t group = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a,
 #pragma unroll
   for (int i = 0; i < kPre; ++i)
     if (share + i * spr < S) M = fmaxf(M, ml[i][0]);
-#pragma unroll 8
+#pragma unroll kRest
   for (int s = share + kPre * spr; s < S; s += spr) M = fmaxf(M, a.part_ml[(size_t)s * n + row][0]);
   for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
   // l 2^(m - M); 0 where nothing is seen (l is NaN where scores were)
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a,
     ml[i][3] = weight(ml[i]);
     total += ml[i][3];
   }
-#pragma unroll 8
+#pragma unroll kRest
   for (int s = share + kPre * spr; s < S; s += spr) total += weight(a.part_ml[(size_t)s * n + row]);
   for (int off = 1 << lpr_shift; off < 1 << (lpr_shift + spr_shift); off <<= 1) total += __shfl_xor(total, off);
   if (M == -INFINITY && total == 0.f) total = 1.f;      // no key at all: zeros
