@@ -453,10 +453,12 @@ nexus_status nexus_batch_pages(const int32_t *cached, const int32_t *fresh, int3
  *   eps       > 0: every head of q and k becomes x / sqrt(mean(x^2) + eps) * weight, weights fp32 [head_dim] on the
  *             device (NULL: ones); 0: no norm, and no weights.
  *   pos, slot DEVICE int32 [n_tokens], as nexus_batch_pages writes them: the rotation's position (the cache's base and
- *             pairing, arithmetic of nexus_rephase_k) and the place of the key and value.  A row whose slot is outside
- *             the cache (-1 among them) writes nothing, its q_out row included.  Other slots must differ.
+ *             pairing) and the place of the key and value.  A row whose slot is outside the cache (-1 among them) writes
+ *             nothing, its q_out row included.  Other slots must differ.
  *   q_out     [n_tokens][n_q_heads][head_dim]; may be q itself where q_stride is n_q_heads * head_dim.
- * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.
+ * Norms and rotations are fp32 (angles fp64), rounded once to the cache dtype; values are copied as they are.  fp32 rows
+ * turn by the compensated products of nexus_rephase_k, bf16 rows by plain ones: a key without a norm has the bits that
+ * nexus_rope_append gives it in fp32, and may be a step away in bf16.
  * Checks: non-NULL q, k, v, pos, slot, q_out, n_tokens > 0, pointers (cache, rows) 16-byte aligned and strides in
  * multiples of 16 bytes that cover a row, eps finite and >= 0, no weights without a norm, q_out apart from the rows
  * read and both apart from the layer's K and V (NEXUS_EINVAL); layer (NEXUS_ERANGE); n_q_heads a positive multiple of

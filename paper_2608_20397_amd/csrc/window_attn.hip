@@ -12,8 +12,9 @@
 // those of attn_bf16_dma_kernel.
 // 4096 rows of 40 heads over 8 of 128 at depth 12288, window 4096, 4 sinks: 331 us, 1040 TFLOP/s, MFMA busy 53%, 107 MB
 // read (at the board's power limit; the loop is that of suffix attention).  head_dim 64, 16 sequences of up to 517 rows,
-// 32 heads over 8, window 1024: 55 us; the vector work of the softmax bounds it (exponentials at a quarter rate), MFMA
-// busy 31%, and four and a quarter workgroups a CU where three run together.
+// 32 heads over 8, window 1024: 56 us, MFMA busy 31%.  Vector instructions, a fifth of them exponentials at a quarter
+// rate, take some 30 us of it; 15 are rounds (four and a quarter workgroups a CU where three run together) and edges,
+// which a prefill that fills the chip (757 TFLOP/s) does not have.
 // Keys that no row of the tile sees (before the window, past the end, between sinks and window) are replaced by one
 // that is seen (transposed V: zeroed) and masked; where a key is seen by some rows only and its value is not finite,
 // row_again forms the rows that came out not finite.

@@ -5,8 +5,9 @@
 // (f32_waves) take the pages of the list in turn, S^T = K.Q^T and O^T += V^T.P^T on 16x16x4 fp32 MFMA straight from
 // global memory (a page's values and the next one's keys are loading while a page's scores are formed), and merge their
 // (m, l, O) through LDS.  Scores, probabilities and sums are fp32 throughout.  122 rows of 4 heads of 64 in a window of
-// 256: 8.3 us, a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s, five workgroups a
-// CU of which four run together.
+// 256: 8.3 us, a chain of round trips; 512 rows of 40 heads of 128 in one of 1024: 143 us, 76 TFLOP/s: a page serves 16
+// pairs, 8 operations a byte, so keys and values come out of the caches at 9.5 TB/s; and five workgroups a CU of which
+// four run together.  A decode step of 32 sequences, window 4096, 8 KV heads of 128: 184 us, 5.8 TB/s (transposed V 265).
 #include "decode_common.h"
 #include "window_common.h"
 
@@ -19,9 +20,9 @@ namespace nexus {
 namespace {
 
 constexpr int kPre = 8;            // partials of a row that a lane of the merge loads at once
-// Of a row's keys, where rows are few: bounds the workspace (64 fp32 rows and records for each) and the merge, which takes
-// about 0.7 us a split once a row's splits are more than its first loads (a sequence of 17473 fp32 keys, 2 KV heads of 128
-// in 64 splits: 37 us, 23 of them the merge; 8 of bf16 256 in 32: 49, 23).
+// Of a row's keys, where rows are few: bounds the workspace (64 fp32 rows and records for each) and the merge, whose lanes
+// take 0.7 us for each split beyond their first eight (a sequence of 17473 fp32 keys, 2 KV heads of 128 in 64 splits: 37
+// us, 23 of them the merge; bf16, 8 of 256 in 32: 49, 23).
 constexpr int kMaxSplits = 64;
 
 }  // namespace
@@ -308,7 +309,7 @@ namespace {
 // divided by their sum before a partial is multiplied, so that finite partials have a finite result.  Rows of no sequence
 // stay as they are.  A partial row lies in 2^lpr_shift lanes, 16 bytes each; 2^spr_shift neighbouring groups of them
 // share the splits of a row, and what is left of the wave takes other rows.  The first eight partials of a group are
-// loaded beside their (m, l): one round trip for rows of up to 16 splits.
+// loaded beside their (m, l), in one round trip; the ones behind them come one after another.
 template <bool BF16, bool HALF>
 __global__ __launch_bounds__(256) void window_combine_kernel(const WindowArgs a, int D, int lpr_shift, int spr_shift) {
   constexpr int E = HALF ? 8 : 4;
